@@ -366,6 +366,101 @@ const char *dg_gemm_kernel_name(const dg_lut *lut, int64_t M, int64_t N, int64_t
                                 dg_kernel variant);
 const char *dg_conv_kernel_name(const dg_lut *lut, const dg_conv_desc *desc, dg_kernel variant);
 
+/* ---- a quantised decoder layer around the tables ------------------------------------------------------------------------ */
+
+/*
+ * What a layer of a quantised language model has besides low-bit products: layers kept at 8 bits, and attention over a cache of keys
+ * and values in few bits.  The conventions are the ones above, with three differences that serving needs: the number of tokens (N, T),
+ * of sequences (B) or max_q may be 0 (DG_OK, nothing is launched), rows may lie apart (strides, in elements, the innermost axis
+ * contiguous), and element types are arguments.  Every arithmetic step below is binary32 unless stated, rounded to nearest even;
+ * results are rounded once to their type.
+ */
+typedef enum { DG_F32 = 0, DG_F16 = 1, DG_BF16 = 2 } dg_dtype;
+
+/*
+ * 8-bit codes with a scale for each row (a token's activations, or an output channel's weights, offline):
+ *     scale[n] = max_k |x[n][k]| / 127,   codes[n][k] = clip(round(x[n][k] / scale[n]), -127, 127)       (0 where scale[n] = 0).
+ * A row with an infinity or a NaN gets the scale NaN and codes 0: whatever is computed from it is NaN.
+ * x_dev: [N][K] of `type`, rows stride_n apart.  codes_dev: rows stride_codes bytes apart (bytes past K are not written).  1 <= K < 2^17.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (N < 0, K <= 0, a stride below K); DG_ERR_RANGE (K); DG_ERR_UNSUPPORTED (type).
+ */
+dg_status dg_quantize_tokens(const void *x_dev, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, int8_t *codes_dev,
+                             int64_t stride_codes, float *scale_n_dev, void *hip_stream);
+
+/*
+ * Matrix product in 8-bit integers with a scale for each token n and each output channel m:
+ *     out[n][m] = (float)(sum_{k<K} W[m][k] * A[n][k]) * scale_m[m] * scale_n[n] + bias[m]
+ * The sum is exact (int32, K < 2^17, any int8 codes); it is converted once, multiplied twice, left to right, then the bias (bias_m_dev may be
+ * NULL) is added, and the result rounded to out_type.  W_dev: rows stride_w bytes apart; A_dev: stride_a; out_dev: rows stride_out elements
+ * apart.  Any K, stride and alignment; rows that begin on 16 bytes are fastest.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, a stride below its row); DG_ERR_RANGE (K); DG_ERR_UNSUPPORTED (type).
+ */
+dg_status dg_gemm_i8(const int8_t *W_dev, int64_t stride_w, const int8_t *A_dev, int64_t stride_a, int64_t M, int64_t N, int64_t K,
+                     const float *scale_m_dev, const float *scale_n_dev, const float *bias_m_dev, void *out_dev, dg_dtype out_type,
+                     int64_t stride_out, void *hip_stream);
+/*
+ * The layer from activations that are not quantised yet: dg_quantize_tokens and dg_gemm_i8 as one call, with their results.
+ * work_dev: work_bytes >= dg_linear_i8_work_bytes(N, K) (else DG_ERR_BUFFER), 16-byte aligned; its contents are the library's.
+ */
+size_t dg_linear_i8_work_bytes(int64_t N, int64_t K);
+dg_status dg_linear_i8(const int8_t *W_dev, int64_t stride_w, const void *x_dev, dg_dtype x_type, int64_t stride_x, int64_t M, int64_t N,
+                       int64_t K, const float *scale_m_dev, const float *bias_m_dev, void *work_dev, size_t work_bytes, void *out_dev,
+                       dg_dtype out_type, int64_t stride_out, void *hip_stream);
+
+/*
+ * A cache of keys and values in 8 or 4 bits, in pages of page_size tokens (a multiple of 16); dim = channels of a head: 64, 128 or 256.
+ * Each (token, head) is quantised by itself, keys and values apart:
+ *     8 bits   s = max|x| / 127,              code = clip(round(x / s), -127, 127),      value = s * code
+ *     4 bits   z = min x, s = max x / 15 - z / 15,  code = clip(round((x - z) / s), 0, 15),  value = s * code + z
+ * (code 0 where s = 0; a vector with an infinity or a NaN gets s = NaN, so that whatever reads it is NaN).
+ * Layout (public, so that pages can be moved, shared or built elsewhere; everything little-endian): page after page, in a page head after
+ * head; a page's head holds the keys' codes, the values' codes, then page_size binary32 numbers each of key s, value s and, with 4 bits,
+ * key z and value z.  An 8-bit code is stored plus 128.  Token t of a page, channel d, b = bits:
+ *     key    byte (t/16) * 2*b*dim + (d/16) * 32*b + (t%16) * 2*b + (d%16)*b/8
+ *     value  byte (t/4) * b*dim/2 + (d*b/8) * 4 + t%4
+ * and of a 4-bit byte the even channel has the low half.  (Both are the matrix instructions' operands as they lie.)
+ * A slot is page * page_size + token; pages * page_size < 2^31.
+ */
+typedef struct {
+    int32_t pages, page_size, heads, dim, bits;
+} dg_cache_desc;
+/* Bytes of a cache; 0 on a description that the calls below refuse.  The buffer must be 16-byte aligned; it needs no clearing. */
+size_t dg_cache_bytes(const dg_cache_desc *desc);
+/*
+ * Quantise T tokens' keys and values ([T][heads][dim] of `type`, token and head strides apart, channels contiguous) into slots_dev[T].  A
+ * negative slot, or one past the cache, is skipped; the other slots must differ from one another.  Nothing else in the cache changes.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE; DG_ERR_RANGE (slots beyond 32 bits); DG_ERR_UNSUPPORTED (bits, dim, type); DG_ERR_BUFFER
+ * (cache_bytes, alignment).
+ */
+dg_status dg_cache_write(const dg_cache_desc *desc, void *cache_dev, size_t cache_bytes, const void *k_dev, const void *v_dev, dg_dtype type,
+                         int64_t T, int64_t stride_kt, int64_t stride_kh, int64_t stride_vt, int64_t stride_vh, const int32_t *slots_dev,
+                         void *hip_stream);
+/* The values that slots_dev[T] hold, to contiguous [T][heads][dim]; either output may be NULL.  A slot that is none gives zeros.  Errors as above. */
+dg_status dg_cache_read(const dg_cache_desc *desc, const void *cache_dev, size_t cache_bytes, const int32_t *slots_dev, int64_t T, void *k_dev,
+                        void *v_dev, dg_dtype type, void *hip_stream);
+
+/*
+ * Attention of a batch's new tokens over the cache.  Sequence b has the query tokens q_start[b] ... q_start[b + 1] - 1 of q_dev ([T][Hq][dim],
+ * binary16 or bfloat16), in order, and ctx_len[b] tokens in the cache, token p at place p % page_size of page table[b * table_width +
+ * p / page_size].  Its new tokens are the last ones of these: dg_cache_write has put them there before.  Query head j reads cached head
+ * j / (Hq / heads).  With `causal` new token i of n sees p <= ctx_len - n + i, otherwise all; out = sum_p softmax_p(scale * q . k_p) v_p over what
+ * it sees, 0 if that is nothing.  One new token each is a decode step; a prompt, a chunk of one, drafted tokens, or queries over an
+ * encoder's states (causal = 0) are the same call.
+ * q_start[B + 1], ctx_len[B] and the table are device memory and are not checked on the host: token numbers are held to 0 ... T, a context
+ * to the table's width, and a page number that is none of the cache's hides its tokens, as does nothing else.  max_q: no sequence has more new tokens
+ * (later ones get no output).  max_ctx: about the longest context; how the work is cut goes by it, results are right whatever it is.
+ * Codes enter the matrix instructions exactly; scores, softmax and sums are binary32; weights are rounded once, to binary16 with a scale of
+ * their own.  Rows of no sequence are not written.  work_dev: dg_paged_attention_work_bytes(...) bytes, 16-byte aligned (0 bytes: may be NULL).
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (Hq no multiple of heads, negative sizes); DG_ERR_RANGE (rows beyond 32 bits); DG_ERR_UNSUPPORTED;
+ * DG_ERR_BUFFER.
+ */
+size_t dg_paged_attention_work_bytes(const dg_cache_desc *desc, int64_t B, int64_t Hq, int64_t max_q, int64_t max_ctx);
+dg_status dg_paged_attention(const dg_cache_desc *desc, const void *cache_dev, size_t cache_bytes, const void *q_dev, dg_dtype type, int64_t T,
+                             int64_t Hq, int64_t stride_qt, int64_t stride_qh, const int32_t *q_start_dev, const int32_t *ctx_len_dev,
+                             const int32_t *table_dev, int64_t B, int64_t table_width, int64_t max_q, int64_t max_ctx, float scale,
+                             int32_t causal, void *out_dev, int64_t stride_ot, int64_t stride_oh, void *work_dev, size_t work_bytes,
+                             void *hip_stream);
+
 #pragma GCC visibility pop
 #ifdef __cplusplus
 }

@@ -36,12 +36,19 @@ EXPORTS = (
     "dg_conv2d_lut_codes", "dg_conv_codes_kernel_name", "dg_gemm_lut_codes", "dg_gemm_codes_kernel_name",
     "dg_launch_empty", "dg_dequantize", "dg_conv2d_lut_requant",
     "dg_static_work_bytes", "dg_conv2d_lut_codes_static",
+    "dg_quantize_tokens", "dg_gemm_i8", "dg_linear_i8_work_bytes", "dg_linear_i8", "dg_cache_bytes", "dg_cache_write", "dg_cache_read",
+    "dg_paged_attention_work_bytes", "dg_paged_attention",
 )
 
 
 class ConvDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "H", "W", "Cin", "Cout", "KH", "KW", "stride_h", "stride_w", "pad_h", "pad_w")]
+
+
+class CacheDesc(ctypes.Structure):
+    """A paged cache of quantised keys and values: its pages, their tokens, the heads, their channels, the bits of a code."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("pages", "page_size", "heads", "dim", "bits")]
 
 
 class DgError(RuntimeError):
@@ -110,6 +117,21 @@ def lib() -> ctypes.CDLL:
     L.dg_conv2d_lut_requant.argtypes = [c_vp, c_vp, c_vp, ctypes.POINTER(ConvDesc), c_vp, ctypes.c_float, ctypes.c_float,
                                         ctypes.c_int32, c_vp, ctypes.c_size_t, c_int, c_vp]
     L.dg_conv2d_lut_requant.restype = c_int
+    c_f, c_i32, desc = ctypes.c_float, ctypes.c_int32, ctypes.POINTER(CacheDesc)
+    L.dg_quantize_tokens.argtypes, L.dg_quantize_tokens.restype = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_i64, c_vp, c_vp], c_int
+    L.dg_gemm_i8.argtypes = [c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_vp, c_int, c_i64, c_vp]
+    L.dg_gemm_i8.restype = c_int
+    L.dg_linear_i8_work_bytes.argtypes, L.dg_linear_i8_work_bytes.restype = [c_i64, c_i64], c_sz
+    L.dg_linear_i8.argtypes = [c_vp, c_i64, c_vp, c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_sz, c_vp, c_int, c_i64, c_vp]
+    L.dg_linear_i8.restype = c_int
+    L.dg_cache_bytes.argtypes, L.dg_cache_bytes.restype = [desc], c_sz
+    L.dg_cache_write.argtypes = [desc, c_vp, c_sz, c_vp, c_vp, c_int, c_i64, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp]
+    L.dg_cache_write.restype = c_int
+    L.dg_cache_read.argtypes, L.dg_cache_read.restype = [desc, c_vp, c_sz, c_vp, c_i64, c_vp, c_vp, c_int, c_vp], c_int
+    L.dg_paged_attention_work_bytes.argtypes, L.dg_paged_attention_work_bytes.restype = [desc, c_i64, c_i64, c_i64, c_i64], c_sz
+    L.dg_paged_attention.argtypes = [desc, c_vp, c_sz, c_vp, c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_i64, c_i64, c_i64, c_i64,
+                                     c_f, c_i32, c_vp, c_i64, c_i64, c_vp, c_sz, c_vp]
+    L.dg_paged_attention.restype = c_int
     _lib = L
     return L
 
@@ -125,7 +147,7 @@ def _load_native():
     if not os.path.exists(NATIVE_PATH):
         raise ImportError(f"{NATIVE_PATH} is missing: build it with `python -m paper_2304_09049_amd.build`.")
     from . import _native as module
-    module.use_desc(ConvDesc)
+    module.use_desc(ConvDesc, CacheDesc)
     _native = module
     return module
 
@@ -395,6 +417,105 @@ def dg_conv2d_lut_requant(lut: Lut, Wp, Xp, desc: ConvDesc, scale, q_scale: floa
         out = torch.empty(dg_packed_activation_bytes(B * OH * OW, Cout), dtype=torch.uint8, device=Wp.device)
     status = (_native or _load_native()).conv2d_lut_requant(lut, Wp, Xp, desc, scale, q_scale, q_zero, lo, out,
                                                             _kernel(variant), stream)
+    if status:
+        _check(status)
+    return out
+
+
+# ---- a quantised decoder layer around the tables ----------------------------------------------------------------------------
+
+
+def dg_quantize_tokens(x, codes=None, scale=None, stream=None):
+    """x: float32, float16 or bfloat16 device tensor [N][K] (rows may lie apart) -> (int8 codes [N][K], float32 scale [N]): scale =
+    max|x| / 127 of the row.  The codes made here are rows of whole 16 bytes (a view), as the product reads them fastest."""
+    if codes is None:
+        import torch
+        codes = torch.empty((x.shape[0], -(-x.shape[1] // 16) * 16), dtype=torch.int8, device=x.device)[:, :x.shape[1]]
+    if scale is None:
+        import torch
+        scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    status = (_native or _load_native()).quantize_tokens(x, codes, scale, stream)
+    if status:
+        _check(status)
+    return codes, scale
+
+
+def dg_gemm_i8(W, A, scale_m, scale_n, bias=None, out=None, dtype=None, stream=None):
+    """W: int8 [M][K]; A: int8 [N][K] -> [N][M] of `dtype` (or out's; default float32): the exact sums times scale_m[m] times scale_n[n], plus
+    the float32 bias[m] if one is given."""
+    if out is None:
+        import torch
+        out = torch.empty((A.shape[0], W.shape[0]), dtype=dtype or torch.float32, device=W.device)
+    status = (_native or _load_native()).gemm_i8(W, A, scale_m, scale_n, bias, out, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def dg_linear_i8_work_bytes(N: int, K: int) -> int:
+    return int(lib().dg_linear_i8_work_bytes(N, K))
+
+
+def dg_linear_i8(W, x, scale_m, bias=None, work=None, out=None, stream=None):
+    """dg_quantize_tokens and dg_gemm_i8 as one call: x [N][K] -> [N][M] of x's dtype (or out's).  `work`: uint8, dg_linear_i8_work_bytes(N, K)."""
+    if out is None:
+        import torch
+        out = torch.empty((x.shape[0], W.shape[0]), dtype=x.dtype, device=W.device)
+    if work is None:
+        import torch
+        work = torch.empty(dg_linear_i8_work_bytes(x.shape[0], x.shape[1]), dtype=torch.uint8, device=W.device)
+    status = (_native or _load_native()).linear_i8(W, x, scale_m, bias, work, out, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def cache_desc(pages: int, page_size: int, heads: int, dim: int, bits: int = 8) -> CacheDesc:
+    return CacheDesc(pages, page_size, heads, dim, bits)
+
+
+def dg_cache_bytes(desc: CacheDesc) -> int:
+    return int(lib().dg_cache_bytes(ctypes.byref(desc)))
+
+
+def dg_cache_write(desc: CacheDesc, cache, k, v, slots, stream=None) -> None:
+    """k, v: [T][heads][dim] device tensors (tokens and heads may lie apart), quantised into `slots` (int32 [T]) of `cache` (uint8)."""
+    status = (_native or _load_native()).cache_write(desc, cache, k, v, slots, stream)
+    if status:
+        _check(status)
+
+
+def dg_cache_read(desc: CacheDesc, cache, slots, k_out=None, v_out=None, dtype=None, stream=None):
+    """The keys and values that `slots` hold, [T][heads][dim] each, of `dtype` (default float32) or the outputs' own."""
+    if k_out is None and v_out is None:
+        import torch
+        k_out, v_out = (torch.empty((slots.numel(), desc.heads, desc.dim), dtype=dtype or torch.float32, device=cache.device) for _ in range(2))
+    status = (_native or _load_native()).cache_read(desc, cache, slots, k_out, v_out, stream)
+    if status:
+        _check(status)
+    return k_out, v_out
+
+
+def dg_paged_attention_work_bytes(desc: CacheDesc, B: int, Hq: int, max_q: int, max_ctx: int) -> int:
+    return int(lib().dg_paged_attention_work_bytes(ctypes.byref(desc), B, Hq, max_q, max_ctx))
+
+
+def dg_paged_attention(desc: CacheDesc, cache, q, q_start, ctx_len, table, max_q: int, max_ctx: int, scale: Optional[float] = None,
+                       causal: bool = True, out=None, work=None, stream=None):
+    """Attention of a batch's new tokens over the cache.  q: [T][Hq][dim] float16 or bfloat16; sequence b has the rows q_start[b] ...
+    q_start[b + 1] - 1 (int32 [B + 1]) and ctx_len[b] tokens (int32 [B], the new ones included) in the pages of table[b] (int32 [B][width]).
+    max_q: the most new tokens of a sequence; max_ctx: about the longest context.  scale: default dim ** -0.5.  `work`: uint8,
+    dg_paged_attention_work_bytes(desc, B, Hq, max_q, max_ctx)."""
+    if out is None:
+        import torch
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if work is None:
+        need = dg_paged_attention_work_bytes(desc, table.shape[0], q.shape[1], max_q, max_ctx)
+        if need:
+            import torch
+            work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    status = (_native or _load_native()).paged_attention(desc, cache, q, q_start, ctx_len, table, max_q, max_ctx,
+                                                         desc.dim ** -0.5 if scale is None else scale, causal, out, work, stream)
     if status:
         _check(status)
     return out

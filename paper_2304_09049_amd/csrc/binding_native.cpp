@@ -23,6 +23,7 @@ PyObject *g_raw_stream = nullptr;        // torch._C._cuda_getCurrentRawStream
 PyObject *g_stream_attr = nullptr;       // "cuda_stream"
 PyObject *g_address_attr = nullptr;      // "_address"
 PyTypeObject *g_desc_type = nullptr;     // binding.ConvDesc, from use_desc
+PyTypeObject *g_cache_type = nullptr;    // binding.CacheDesc, the same
 
 struct Failed {};                        // a Python error is set
 
@@ -137,25 +138,28 @@ void *stream_of(PyObject *o)
     return s;
 }
 
-// The convolution's geometry out of a binding.ConvDesc (a ctypes structure lends its memory as a buffer).
-dg_conv_desc geometry(PyObject *o)
+// A binding.ConvDesc or CacheDesc as C has it (a ctypes structure lends its memory as a buffer).
+template <class Desc>
+Desc structure(PyObject *o, PyTypeObject *type, const char *name)
 {
-    if (!g_desc_type || !PyObject_TypeCheck(o, g_desc_type)) {
-        PyErr_SetString(PyExc_TypeError, "desc must be a ConvDesc");
+    if (!type || !PyObject_TypeCheck(o, type)) {
+        PyErr_Format(PyExc_TypeError, "desc must be a %s", name);
         throw Failed();
     }
     Py_buffer view;
     if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Failed();
-    dg_conv_desc d;
+    Desc d;
     const bool fits = view.len >= (Py_ssize_t)sizeof(d);
     if (fits) memcpy(&d, view.buf, sizeof(d));
     PyBuffer_Release(&view);
     if (!fits) {
-        PyErr_SetString(PyExc_TypeError, "desc must be a ConvDesc");
+        PyErr_Format(PyExc_TypeError, "desc must be a %s", name);
         throw Failed();
     }
     return d;
 }
+dg_conv_desc geometry(PyObject *o) { return structure<dg_conv_desc>(o, g_desc_type, "ConvDesc"); }
+dg_cache_desc cache_geometry(PyObject *o) { return structure<dg_cache_desc>(o, g_cache_type, "CacheDesc"); }
 
 // The table's address: a number, or a binding.Lut's, or the handle of another object that owns a table (a number or a ctypes
 // pointer, whose value is None where it is NULL).
@@ -380,17 +384,231 @@ PyObject *dequantize(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (type): binding.ConvDesc, whose instances alone are taken for a geometry
+// ---- a quantised decoder layer: tensors with strides and of several types
+
+// A tensor on the device of `dims` axes, the innermost contiguous.
+const at::Tensor &strided(PyObject *o, int dims, const char *name)
+{
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
+        throw Failed();
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) {
+        PyErr_Format(PyExc_ValueError, "%s must live in device memory", name);
+        throw Failed();
+    }
+    if (t.dim() != dims) {
+        PyErr_Format(PyExc_ValueError, "%s must have %d dimensions, got %d", name, dims, (int)t.dim());
+        throw Failed();
+    }
+    if (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1) {
+        PyErr_Format(PyExc_ValueError, "%s must be contiguous along its last dimension", name);
+        throw Failed();
+    }
+    return t;
+}
+
+// Elements from one index of axis `i` to the next; where there is one index at most, what it would be in a contiguous tensor.
+int64_t step(const at::Tensor &t, int i)
+{
+    if (t.size(i) > 1) return t.stride(i);
+    int64_t s = 1;
+    for (int64_t k = i + 1; k < t.dim(); ++k) s *= t.size(k);
+    return s;
+}
+
+dg_dtype element_type(const at::Tensor &t, const char *name)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: return DG_F32;
+    case at::kHalf: return DG_F16;
+    case at::kBFloat16: return DG_BF16;
+    default:
+        PyErr_Format(PyExc_ValueError, "%s must have dtype float32, float16 or bfloat16, got %S", name, (PyObject *)torch::getTHPDtype(t.scalar_type()));
+        throw Failed();
+    }
+}
+
+void expect(bool ok, const char *what)
+{
+    if (ok) return;
+    PyErr_SetString(PyExc_ValueError, what);
+    throw Failed();
+}
+
+const at::Tensor &of_type(const at::Tensor &t, at::ScalarType type, const char *name)
+{
+    if (t.scalar_type() != type) {
+        PyErr_Format(PyExc_ValueError, "%s must have dtype %S, got %S", name, (PyObject *)torch::getTHPDtype(type),
+                     (PyObject *)torch::getTHPDtype(t.scalar_type()));
+        throw Failed();
+    }
+    return t;
+}
+
+// A contiguous vector of `count` elements at least, or NULL for None where that is allowed.
+template <class T>
+T *vector(PyObject *o, at::ScalarType type, int64_t count, const char *name, bool optional = false)
+{
+    if (optional && o == Py_None) return nullptr;
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor", name);
+        throw Failed();
+    }
+    T *p = (T *)device_ptr(o, type, name);
+    const int64_t have = THPVariable_Unpack(o).numel();
+    if (have < count) {
+        PyErr_Format(PyExc_ValueError, "%s must have %lld elements, got %lld", name, (long long)count, (long long)have);
+        throw Failed();
+    }
+    return p;
+}
+
+// (x, codes, scale, stream)
+PyObject *quantize_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&] {
+        const at::Tensor &x = strided(a[0], 2, "x"), &codes = of_type(strided(a[1], 2, "codes"), at::kChar, "codes");
+        const dg_dtype type = element_type(x, "x");
+        expect(codes.sizes() == x.sizes(), "codes must have x's shape");
+        float *scale = vector<float>(a[2], at::kFloat, x.size(0), "scale");
+        void *s = stream_of(a[3]);
+        const void *px = x.data_ptr();
+        int8_t *pc = (int8_t *)codes.data_ptr();
+        const int64_t N = x.size(0), K = x.size(1), sx = step(x, 0), sc = step(codes, 0);
+        RUN(dg_quantize_tokens(px, type, N, K, sx, pc, sc, scale, s));
+    });
+}
+
+// (W, A, scale_m, scale_n, bias, out, stream)
+PyObject *gemm_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const at::Tensor &W = of_type(strided(a[0], 2, "W"), at::kChar, "W"), &A = of_type(strided(a[1], 2, "A"), at::kChar, "A");
+        const at::Tensor &out = strided(a[5], 2, "out");
+        const int64_t M = W.size(0), K = W.size(1), N = A.size(0);
+        expect(A.size(1) == K, "A and W must have the same number of columns");
+        expect(out.size(0) == N && out.size(1) == M, "out must be [tokens][channels]");
+        const float *sm = vector<float>(a[2], at::kFloat, M, "scale_m"), *sn = vector<float>(a[3], at::kFloat, N, "scale_n");
+        const float *bias = vector<float>(a[4], at::kFloat, M, "bias", true);
+        const dg_dtype type = element_type(out, "out");
+        void *s = stream_of(a[6]), *po = out.data_ptr();
+        const int8_t *pw = (const int8_t *)W.data_ptr(), *pa = (const int8_t *)A.data_ptr();
+        const int64_t sw = step(W, 0), sa = step(A, 0), so = step(out, 0);
+        RUN(dg_gemm_i8(pw, sw, pa, sa, M, N, K, sm, sn, bias, po, type, so, s));
+    });
+}
+
+// (W, x, scale_m, bias, work, out, stream)
+PyObject *linear_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const at::Tensor &W = of_type(strided(a[0], 2, "W"), at::kChar, "W"), &x = strided(a[1], 2, "x"), &out = strided(a[5], 2, "out");
+        const int64_t M = W.size(0), K = W.size(1), N = x.size(0);
+        expect(x.size(1) == K, "x and W must have the same number of columns");
+        expect(out.size(0) == N && out.size(1) == M, "out must be [tokens][channels]");
+        const float *sm = vector<float>(a[2], at::kFloat, M, "scale_m"), *bias = vector<float>(a[3], at::kFloat, M, "bias", true);
+        void *work = device_ptr(a[4], at::kByte, "work");
+        const size_t bytes = bytes_of(a[4]);
+        const dg_dtype xt = element_type(x, "x"), type = element_type(out, "out");
+        void *s = stream_of(a[6]), *po = out.data_ptr();
+        const void *px = x.data_ptr();
+        const int8_t *pw = (const int8_t *)W.data_ptr();
+        const int64_t sw = step(W, 0), sx = step(x, 0), so = step(out, 0);
+        RUN(dg_linear_i8(pw, sw, px, xt, sx, M, N, K, sm, bias, work, bytes, po, type, so, s));
+    });
+}
+
+// (desc, cache, k, v, slots, stream)
+PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 6, [&] {
+        const dg_cache_desc d = cache_geometry(a[0]);
+        void *cache = device_ptr(a[1], at::kByte, "cache");
+        const size_t bytes = bytes_of(a[1]);
+        const at::Tensor &k = strided(a[2], 3, "k"), &v = strided(a[3], 3, "v");
+        const dg_dtype type = element_type(k, "k");
+        expect(element_type(v, "v") == type && v.sizes() == k.sizes(), "k and v must have one shape and dtype");
+        expect(k.size(1) == d.heads && k.size(2) == d.dim, "k and v must be [tokens][heads][dim]");
+        const int64_t T = k.size(0), kt = step(k, 0), kh = step(k, 1), vt = step(v, 0), vh = step(v, 1);
+        const int32_t *slots = vector<int32_t>(a[4], at::kInt, T, "slots");
+        void *s = stream_of(a[5]);
+        const void *pk = k.data_ptr(), *pv = v.data_ptr();
+        RUN(dg_cache_write(&d, cache, bytes, pk, pv, type, T, kt, kh, vt, vh, slots, s));
+    });
+}
+
+// (desc, cache, slots, k_out, v_out, stream)
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 6, [&] {
+        const dg_cache_desc d = cache_geometry(a[0]);
+        void *cache = device_ptr(a[1], at::kByte, "cache");
+        const size_t bytes = bytes_of(a[1]);
+        const int32_t *slots = vector<int32_t>(a[2], at::kInt, 0, "slots");
+        const int64_t T = THPVariable_Unpack(a[2]).numel();
+        void *out[2] = {nullptr, nullptr};
+        dg_dtype type = DG_F32;
+        bool first = true;
+        for (int i = 0; i < 2; ++i) {
+            if (a[3 + i] == Py_None) continue;
+            const at::Tensor &t = strided(a[3 + i], 3, i ? "v_out" : "k_out");
+            const dg_dtype its = element_type(t, i ? "v_out" : "k_out");
+            expect(first || its == type, "k_out and v_out must have one dtype");
+            expect(t.is_contiguous() && t.size(0) == T && t.size(1) == d.heads && t.size(2) == d.dim,
+                   "k_out and v_out must be contiguous [slots][heads][dim]");
+            type = its;
+            first = false;
+            out[i] = t.data_ptr();
+        }
+        void *s = stream_of(a[5]);
+        RUN(dg_cache_read(&d, cache, bytes, slots, T, out[0], out[1], type, s));
+    });
+}
+
+// (desc, cache, q, q_start, ctx_len, table, max_q, max_ctx, scale, causal, out, work, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 13, [&] {
+        const dg_cache_desc d = cache_geometry(a[0]);
+        void *cache = device_ptr(a[1], at::kByte, "cache");
+        const size_t bytes = bytes_of(a[1]);
+        const at::Tensor &q = strided(a[2], 3, "q"), &out = strided(a[10], 3, "out"), &table = of_type(strided(a[5], 2, "table"), at::kInt, "table");
+        const dg_dtype type = element_type(q, "q");
+        expect(element_type(out, "out") == type && out.sizes() == q.sizes(), "out must have q's shape and dtype");
+        expect(q.size(2) == d.dim, "q must be [tokens][query heads][dim]");
+        expect(table.is_contiguous(), "table must be contiguous");
+        const int64_t T = q.size(0), Hq = q.size(1), B = table.size(0), width = table.size(1);
+        const int32_t *start = vector<int32_t>(a[3], at::kInt, B + 1, "q_start"), *ctx = vector<int32_t>(a[4], at::kInt, B, "ctx_len");
+        const int64_t max_q = integer(a[6]), max_ctx = integer(a[7]);
+        const float scale = (float)real(a[8]);
+        const int32_t causal = is_true(a[9]);
+        void *work = device_ptr(a[11], at::kByte, "work");
+        const size_t work_bytes = bytes_of(a[11]);
+        void *s = stream_of(a[12]), *po = out.data_ptr();
+        const void *pq = q.data_ptr();
+        const int32_t *pt = (const int32_t *)table.data_ptr();
+        const int64_t qt = step(q, 0), qh = step(q, 1), ot = step(out, 0), oh = step(out, 1);
+        RUN(dg_paged_attention(&d, cache, bytes, pq, type, T, Hq, qt, qh, start, ctx, pt, B, width, max_q, max_ctx, scale, causal, po, ot, oh, work,
+                               work_bytes, s));
+    });
+}
+
+// (ConvDesc, CacheDesc): binding's types, whose instances alone are taken for a geometry
 PyObject *use_desc(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return guarded(n, 1, [&] {
-        if (!PyType_Check(a[0])) {
+    return guarded(n, 2, [&] {
+        if (!PyType_Check(a[0]) || !PyType_Check(a[1])) {
             PyErr_SetString(PyExc_TypeError, "a type is needed");
             throw Failed();
         }
         Py_INCREF(a[0]);
         Py_XDECREF((PyObject *)g_desc_type);
         g_desc_type = (PyTypeObject *)a[0];
+        Py_INCREF(a[1]);
+        Py_XDECREF((PyObject *)g_cache_type);
+        g_cache_type = (PyTypeObject *)a[1];
         return 0;
     });
 }
@@ -402,6 +620,8 @@ PyMethodDef methods[] = {
     METHOD("gemm_lut", gemm_lut), METHOD("gemm_lut_codes", gemm_lut_codes), METHOD("pack_codes_bits", pack_codes_bits),
     METHOD("pack_weights", pack<dg_pack_weights>), METHOD("pack_activations", pack<dg_pack_activations>),
     METHOD("quantize_pack_activations", quantize_pack_activations), METHOD("dequantize", dequantize),
+    METHOD("quantize_tokens", quantize_tokens), METHOD("gemm_i8", gemm_i8), METHOD("linear_i8", linear_i8),
+    METHOD("cache_write", cache_write), METHOD("cache_read", cache_read), METHOD("paged_attention", paged_attention),
     METHOD("use_desc", use_desc),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Tensors in, the C ABI's status out.", -1, methods,

@@ -1,0 +1,131 @@
+// What the kernels of a quantised decoder layer share (8-bit products, the paged cache, the attention on it): element types, the
+// cache's layout and the launchers.  Internal; the public ABI is include/deepgemm_hip.h.
+#pragma once
+
+#include "dg_common.h"
+
+// ---- element types -----------------------------------------------------------------------------------------------------
+
+template <class T>
+__device__ __forceinline__ float dg_to_float(T x) { return (float)x; }
+// One rounding to nearest even (none for binary32).
+template <class T>
+__device__ __forceinline__ T dg_from_float(float x) { return (T)x; }
+
+// COUNT neighbouring elements; the address needs the element's alignment only (the hardware takes vector accesses at any).
+template <class T, int COUNT>
+struct DgVec {
+    T e[COUNT];
+};
+template <class T, int COUNT>
+__device__ __forceinline__ DgVec<T, COUNT> dg_load_vec(const T *p)
+{
+    DgVec<T, COUNT> v;
+    __builtin_memcpy(&v, p, sizeof(v));
+    return v;
+}
+template <class T, int COUNT>
+__device__ __forceinline__ void dg_store_vec(T *p, const DgVec<T, COUNT> &v)
+{
+    __builtin_memcpy(p, &v, sizeof(v));
+}
+
+// f(element type) for a dg_dtype that the API layer has checked.
+template <class F>
+auto dg_with_type(dg_dtype type, F f)
+{
+    if (type == DG_F32) return f(float{});
+    if (type == DG_F16) return f((_Float16){});
+    return f((__bf16){});
+}
+inline int64_t dg_type_size(dg_dtype type) { return type == DG_F32 ? 4 : 2; }
+
+// ---- quantisers (binary32, operation by operation; divisions are correctly rounded) --------------------------------------
+
+// A code of the symmetric 8-bit quantiser; s = max|x| / 127.  s = 0 (or NaN): 0.
+__device__ __forceinline__ int dg_code8(float x, float s)
+{
+    if (!(s > 0.0f)) return 0;
+    return (int)fminf(fmaxf(rintf(x / s), -127.0f), 127.0f);
+}
+// The scale for a row whose largest magnitude is `most`; a row with an infinity or a NaN (`most` not finite) gets a NaN, so that
+// whatever is computed from it shows it.
+__device__ __forceinline__ float dg_scale8(float most) { return most < __builtin_inff() ? most / 127.0f : __builtin_nanf(""); }
+// A code of the 4-bit quantiser: x is about s * code + z.
+__device__ __forceinline__ int dg_code4(float x, float s, float z)
+{
+    if (!(s > 0.0f)) return 0;
+    return (int)fminf(fmaxf(rintf((x - z) / s), 0.0f), 15.0f);
+}
+
+// ---- the cache ---------------------------------------------------------------------------------------------------------
+
+// A cache as the kernels take it.  A page holds `heads` blocks of `head` bytes: keys' codes (`part` bytes), values' codes (`part`),
+// then `page_size` binary32 numbers each of key scale, value scale and, 4 bits, key z and value z.
+struct DgCache {
+    uint8_t *base;
+    int32_t pages, page_size, heads, dim, bits;
+    int32_t part, head;
+    DgFastDiv by_page;                  // token number / page_size
+    __host__ __device__ int64_t page_bytes() const { return (int64_t)head * heads; }
+};
+
+inline DgCache dg_cache_of(const dg_cache_desc *d, void *base)
+{
+    DgCache c;
+    c.base = (uint8_t *)base;
+    c.pages = d->pages;
+    c.page_size = d->page_size;
+    c.heads = d->heads;
+    c.dim = d->dim;
+    c.bits = d->bits;
+    c.part = d->page_size * d->dim * d->bits / 8;
+    c.head = 2 * c.part + d->page_size * (d->bits == 8 ? 8 : 16);
+    c.by_page = dg_make_div((uint32_t)d->page_size);
+    return c;
+}
+
+// Where the byte of channel d (4 bits: of channels d and d + 1, d even) of a page's token t lies in the keys' or the values' codes.
+template <int BITS>
+__device__ __forceinline__ uint32_t dg_key_byte(uint32_t t, uint32_t d, uint32_t dim)
+{
+    return (t >> 4) * (2 * BITS * dim) + (d >> 4) * (32 * BITS) + (t & 15) * (2 * BITS) + (d & 15) * BITS / 8;
+}
+template <int BITS>
+__device__ __forceinline__ uint32_t dg_value_byte(uint32_t t, uint32_t d, uint32_t dim)
+{
+    return (t >> 2) * (BITS * dim / 2) + (d * BITS / 8) * 4 + (t & 3);
+}
+
+// ---- launchers (each validates nothing: the API layer has done that) ---------------------------------------------------
+
+dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, int8_t *codes,
+                                    int64_t stride_codes, float *scale, hipStream_t stream);
+
+struct DgGemmI8 {
+    const int8_t *W, *A;
+    int64_t stride_w, stride_a;          // bytes from row to row
+    int32_t M, N, K;
+    const float *scale_m, *scale_n, *bias;
+    void *out;
+    int64_t stride_out;                  // elements from token to token
+};
+dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream);
+
+dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t T, const int64_t strides[4],
+                                const int32_t *slots, hipStream_t stream);
+dg_status dg_launch_cache_read(const DgCache &c, const int32_t *slots, int64_t T, void *k, void *v, dg_dtype type, hipStream_t stream);
+
+struct DgAttention {
+    DgCache cache;
+    const void *q;
+    void *out;
+    int64_t q_token, q_head, out_token, out_head;        // element strides
+    const int32_t *q_start, *ctx_len, *table;
+    int32_t T, Hq, B, table_width, max_q, max_ctx;
+    float scale;
+    int32_t causal;
+    void *work;
+};
+int64_t dg_attention_work_bytes(const DgAttention &p);
+dg_status dg_launch_attention(const DgAttention &p, dg_dtype type, hipStream_t stream);
