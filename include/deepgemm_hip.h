@@ -393,7 +393,7 @@ dg_status dg_quantize_tokens(const void *x_dev, dg_dtype type, int64_t N, int64_
  * The sum is exact (int32, K < 2^17, any int8 codes); it is converted once, multiplied twice, left to right, then the bias (bias_m_dev may be
  * NULL) is added, and the result rounded to out_type.  W_dev: rows stride_w bytes apart; A_dev: stride_a; out_dev: rows stride_out elements
  * apart.  Any K, stride and alignment; rows that begin on 16 bytes are fastest.
- * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, a stride below its row); DG_ERR_RANGE (K); DG_ERR_UNSUPPORTED (type).
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, a stride below its row); DG_ERR_RANGE (K; M * N of 2^43 and more); DG_ERR_UNSUPPORTED (type).
  */
 dg_status dg_gemm_i8(const int8_t *W_dev, int64_t stride_w, const int8_t *A_dev, int64_t stride_a, int64_t M, int64_t N, int64_t K,
                      const float *scale_m_dev, const float *scale_n_dev, const float *bias_m_dev, void *out_dev, dg_dtype out_type,

@@ -28,6 +28,7 @@ dg_status check_product(const char *what, const int8_t *W, int64_t stride_w, int
     if (M <= 0 || N < 0 || K <= 0 || M > MOST_ROWS || N > MOST_ROWS)
         return dg_fail(DG_ERR_SHAPE, "%s: M=%lld N=%lld K=%lld", what, (long long)M, (long long)N, (long long)K);
     if (K > MOST_K) return dg_fail(DG_ERR_RANGE, "%s: K=%lld could overflow int32 (at most %lld)", what, (long long)K, (long long)MOST_K);
+    if ((M + 63) / 64 * ((N + 63) / 64) > MOST_ROWS) return dg_fail(DG_ERR_RANGE, "%s: M=%lld N=%lld is too large for one call", what, (long long)M, (long long)N);
     if (!known_type(type)) return dg_fail(DG_ERR_UNSUPPORTED, "%s: unknown element type %d", what, (int)type);
     if (!W || !scale_m || (N > 0 && !out)) return dg_fail(DG_ERR_NULL, "%s: NULL argument", what);
     if (stride_w < K) return dg_fail(DG_ERR_SHAPE, "%s: weight rows of %lld bytes every %lld", what, (long long)K, (long long)stride_w);
