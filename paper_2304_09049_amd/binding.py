@@ -425,15 +425,24 @@ def dg_conv2d_lut_requant(lut: Lut, Wp, Xp, desc: ConvDesc, scale, q_scale: floa
 # ---- a quantised decoder layer around the tables ----------------------------------------------------------------------------
 
 
+def _new(shape, dtype: str, device, stream):
+    """A tensor for a call on `stream` (None: the current one), from that stream's memory: what the call leaves behind there, or drops before it
+    has run, is given to no other stream's work."""
+    import torch
+    dtype = getattr(torch, dtype) if isinstance(dtype, str) else dtype
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def dg_quantize_tokens(x, codes=None, scale=None, stream=None):
     """x: float32, float16 or bfloat16 device tensor [N][K] (rows may lie apart) -> (int8 codes [N][K], float32 scale [N]): scale =
     max|x| / 127 of the row.  The codes made here are rows of whole 16 bytes (a view), as the product reads them fastest."""
     if codes is None:
-        import torch
-        codes = torch.empty((x.shape[0], -(-x.shape[1] // 16) * 16), dtype=torch.int8, device=x.device)[:, :x.shape[1]]
+        codes = _new((x.shape[0], -(-x.shape[1] // 16) * 16), "int8", x.device, stream)[:, :x.shape[1]]
     if scale is None:
-        import torch
-        scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        scale = _new(x.shape[0], "float32", x.device, stream)
     status = (_native or _load_native()).quantize_tokens(x, codes, scale, stream)
     if status:
         _check(status)
@@ -444,8 +453,7 @@ def dg_gemm_i8(W, A, scale_m, scale_n, bias=None, out=None, dtype=None, stream=N
     """W: int8 [M][K]; A: int8 [N][K] -> [N][M] of `dtype` (or out's; default float32): the exact sums times scale_m[m] times scale_n[n], plus
     the float32 bias[m] if one is given."""
     if out is None:
-        import torch
-        out = torch.empty((A.shape[0], W.shape[0]), dtype=dtype or torch.float32, device=W.device)
+        out = _new((A.shape[0], W.shape[0]), dtype or "float32", W.device, stream)
     status = (_native or _load_native()).gemm_i8(W, A, scale_m, scale_n, bias, out, stream)
     if status:
         _check(status)
@@ -459,11 +467,9 @@ def dg_linear_i8_work_bytes(N: int, K: int) -> int:
 def dg_linear_i8(W, x, scale_m, bias=None, work=None, out=None, stream=None):
     """dg_quantize_tokens and dg_gemm_i8 as one call: x [N][K] -> [N][M] of x's dtype (or out's).  `work`: uint8, dg_linear_i8_work_bytes(N, K)."""
     if out is None:
-        import torch
-        out = torch.empty((x.shape[0], W.shape[0]), dtype=x.dtype, device=W.device)
+        out = _new((x.shape[0], W.shape[0]), x.dtype, W.device, stream)
     if work is None:
-        import torch
-        work = torch.empty(dg_linear_i8_work_bytes(x.shape[0], x.shape[1]), dtype=torch.uint8, device=W.device)
+        work = _new(dg_linear_i8_work_bytes(x.shape[0], x.shape[1]), "uint8", W.device, stream)
     status = (_native or _load_native()).linear_i8(W, x, scale_m, bias, work, out, stream)
     if status:
         _check(status)
@@ -488,8 +494,7 @@ def dg_cache_write(desc: CacheDesc, cache, k, v, slots, stream=None) -> None:
 def dg_cache_read(desc: CacheDesc, cache, slots, k_out=None, v_out=None, dtype=None, stream=None):
     """The keys and values that `slots` hold, [T][heads][dim] each, of `dtype` (default float32) or the outputs' own."""
     if k_out is None and v_out is None:
-        import torch
-        k_out, v_out = (torch.empty((slots.numel(), desc.heads, desc.dim), dtype=dtype or torch.float32, device=cache.device) for _ in range(2))
+        k_out, v_out = (_new((slots.numel(), desc.heads, desc.dim), dtype or "float32", cache.device, stream) for _ in range(2))
     status = (_native or _load_native()).cache_read(desc, cache, slots, k_out, v_out, stream)
     if status:
         _check(status)
@@ -507,13 +512,11 @@ def dg_paged_attention(desc: CacheDesc, cache, q, q_start, ctx_len, table, max_q
     max_q: the most new tokens of a sequence; max_ctx: about the longest context.  scale: default dim ** -0.5.  `work`: uint8,
     dg_paged_attention_work_bytes(desc, B, Hq, max_q, max_ctx)."""
     if out is None:
-        import torch
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _new(q.shape, q.dtype, q.device, stream)
     if work is None:
         need = dg_paged_attention_work_bytes(desc, table.shape[0], q.shape[1], max_q, max_ctx)
         if need:
-            import torch
-            work = torch.empty(need, dtype=torch.uint8, device=q.device)
+            work = _new(need, "uint8", q.device, stream)
     status = (_native or _load_native()).paged_attention(desc, cache, q, q_start, ctx_len, table, max_q, max_ctx,
                                                          desc.dim ** -0.5 if scale is None else scale, causal, out, work, stream)
     if status:

@@ -3,14 +3,6 @@
 
 namespace {
 
-// Reductions over a wavefront.
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int i = 32; i; i >>= 1) v = fmaxf(v, __shfl_xor(v, i));
-    return v;
-}
-
 struct WriteArgs {
     DgCache c;
     const void *k, *v;

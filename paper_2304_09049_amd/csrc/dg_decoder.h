@@ -48,6 +48,30 @@ __device__ __forceinline__ int dg_code8(float x, float s)
     if (!(s > 0.0f)) return 0;
     return (int)fminf(fmaxf(rintf(x / s), -127.0f), 127.0f);
 }
+// COUNT neighbouring codes of one scale, the same without a division each: x / s is taken as x * (1 / s), off by less than 127 * 2^-22, and
+// where that comes within 2^-14 of a half (one value in eight thousand) the group's quotients are divided out.  `inverse`: 1 / s, 0 where s is below
+// 2^-100 or NaN (what is not 0 there is divided too: the inverse would not hold it).
+__device__ __forceinline__ float dg_inverse8(float s) { return s >= 0x1p-100f ? 1.0f / s : 0.0f; }
+template <int COUNT>
+__device__ __forceinline__ void dg_codes8(const float (&x)[COUNT], float s, float inverse, int (&code)[COUNT])
+{
+    float near = inverse == 0.0f ? 1.0f : 0.0f;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const float q = x[i] * inverse, whole = rintf(q);
+        near = fmaxf(near, fabsf(q - whole));
+        code[i] = (int)whole;
+    }
+    if (near > 0.5f - 0x1p-14f)
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) code[i] = dg_code8(x[i], s);
+}
+// Four codes as bytes, the first lowest.
+__device__ __forceinline__ uint32_t dg_bytes(const int *code)
+{
+    const uint32_t a = __builtin_amdgcn_perm((uint32_t)code[1], (uint32_t)code[0], 0x0C0C0400u);
+    return __builtin_amdgcn_perm((uint32_t)code[3], (uint32_t)code[2], 0x04000C0Cu) | a;
+}
 // The scale for a row whose largest magnitude is `most`; a row with an infinity or a NaN (`most` not finite) gets a NaN, so that
 // whatever is computed from it shows it.
 __device__ __forceinline__ float dg_scale8(float most) { return most < __builtin_inff() ? most / 127.0f : __builtin_nanf(""); }
@@ -99,8 +123,9 @@ __device__ __forceinline__ uint32_t dg_value_byte(uint32_t t, uint32_t d, uint32
 
 // ---- launchers (each validates nothing: the API layer has done that) ---------------------------------------------------
 
+// pad: K, or up to where a row's codes are cleared
 dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, int8_t *codes,
-                                    int64_t stride_codes, float *scale, hipStream_t stream);
+                                    int64_t stride_codes, int64_t pad, float *scale, hipStream_t stream);
 
 struct DgGemmI8 {
     const int8_t *W, *A;
@@ -111,6 +136,9 @@ struct DgGemmI8 {
     int64_t stride_out;                  // elements from token to token
 };
 dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream);
+// The product's kernel for few tokens quantising them itself (p.A and p.scale_n are not used), and whether it holds them.
+bool dg_linear_i8_fuses(int64_t N, int64_t K);
+dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, int64_t stride_x, dg_dtype type, hipStream_t stream);
 
 dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t T, const int64_t strides[4],
                                 const int32_t *slots, hipStream_t stream);

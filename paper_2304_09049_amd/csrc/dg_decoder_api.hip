@@ -93,7 +93,7 @@ dg_status dg_quantize_tokens(const void *x_dev, dg_dtype type, int64_t N, int64_
     if (stride_codes < K) return dg_fail(DG_ERR_SHAPE, "dg_quantize_tokens: rows of %lld codes every %lld", (long long)K, (long long)stride_codes);
     if (N == 0) return DG_OK;
     if (!codes_dev || !scale_n_dev) return dg_fail(DG_ERR_NULL, "dg_quantize_tokens: NULL output");
-    return dg_launch_quantize_tokens(x_dev, type, N, K, stride_n, codes_dev, stride_codes, scale_n_dev, (hipStream_t)hip_stream);
+    return dg_launch_quantize_tokens(x_dev, type, N, K, stride_n, codes_dev, stride_codes, K, scale_n_dev, (hipStream_t)hip_stream);
 }
 
 dg_status dg_gemm_i8(const int8_t *W_dev, int64_t stride_w, const int8_t *A_dev, int64_t stride_a, int64_t M, int64_t N, int64_t K,
@@ -125,9 +125,10 @@ dg_status dg_linear_i8(const int8_t *W_dev, int64_t stride_w, const void *x_dev,
     int8_t *codes = (int8_t *)work_dev;
     const int64_t pitch = codes_pitch(K);
     float *scale_n = (float *)(codes + N * pitch);
-    s = dg_launch_quantize_tokens(x_dev, x_type, N, K, stride_x, codes, pitch, scale_n, (hipStream_t)hip_stream);
-    if (s) return s;
     const DgGemmI8 p = {W_dev, codes, stride_w, pitch, (int32_t)M, (int32_t)N, (int32_t)K, scale_m_dev, scale_n, bias_m_dev, out_dev, stride_out};
+    if (dg_linear_i8_fuses(N, K)) return dg_launch_linear_i8_fused(p, x_dev, x_type, stride_x, out_type, (hipStream_t)hip_stream);
+    s = dg_launch_quantize_tokens(x_dev, x_type, N, K, stride_x, codes, pitch, pitch, scale_n, (hipStream_t)hip_stream);
+    if (s) return s;
     return dg_launch_gemm_i8(p, out_type, (hipStream_t)hip_stream);
 }
 

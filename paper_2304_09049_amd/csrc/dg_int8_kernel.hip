@@ -6,35 +6,94 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 
-// ---- quantising tokens: one workgroup per token, two passes over its row (the second finds it in the caches) --------------
+// ---- quantising tokens ---------------------------------------------------------------------------------------------------
+//
+// A workgroup a token.  Its row is read once, into registers, 16 bytes a lane and load (HELD loads), where it fits; a longer one is read twice,
+// the second time from the caches.  Bytes from K to PAD (a multiple of 16, or K) are cleared.
 
-template <class T>
-__global__ __launch_bounds__(256) void quantize_tokens_kernel(const T *x, int32_t K, int64_t stride_n, int8_t *codes, int64_t stride_codes,
-                                                               float *scale)
+// The largest magnitude over a workgroup; an infinity if any value was an infinity or a NaN (a NaN compares false, so it is counted apart).
+template <int WAVES>
+__device__ __forceinline__ float workgroup_most(float most, bool finite, float *part)
 {
-    __shared__ float part[4];
-    __shared__ int whole[4];
-    const T *row = x + (int64_t)blockIdx.x * stride_n;
-    int8_t *out = codes + (int64_t)blockIdx.x * stride_codes;
-    float most = 0.0f;
-    bool finite = true;
-    for (int k = threadIdx.x; k < K; k += 256) {
-        const float f = fabsf(dg_to_float(row[k]));
+    most = finite ? most : __builtin_inff();
+#pragma unroll
+    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+    __syncthreads();
+    most = part[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) most = fmaxf(most, part[i]);
+    return most;
+}
+
+template <class T, int COUNT>
+__device__ __forceinline__ void look_at(const DgVec<T, COUNT> &v, float &most, bool &finite)
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const float f = fabsf(dg_to_float(v.e[i]));
         most = fmaxf(most, f);
         finite = finite && f < __builtin_inff();
     }
+}
+
+// COUNT elements from position k of a row of K; those at K and beyond are 0 and are not read.
+template <class T, int COUNT>
+__device__ __forceinline__ DgVec<T, COUNT> elements(const T *row, int32_t k, int32_t K)
+{
+    if (k + COUNT <= K) return dg_load_vec<T, COUNT>(row + k);
+    DgVec<T, COUNT> v = {};
+    for (int i = 0; k + i < K; ++i) v.e[i] = row[k + i];
+    return v;
+}
+
+// The codes of COUNT elements to position k of a row whose bytes up to `end` are this kernel's.
+template <class T, int COUNT>
+__device__ __forceinline__ void store_codes(int8_t *row, int32_t k, int32_t end, const DgVec<T, COUNT> &v, float s, float inverse)
+{
+    float x[COUNT];
+    int code[COUNT];
+    uint32_t words[COUNT / 4];
 #pragma unroll
-    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
-    finite = __all(finite);
-    if ((threadIdx.x & 63) == 0) {
-        part[threadIdx.x >> 6] = most;
-        whole[threadIdx.x >> 6] = finite;
+    for (int i = 0; i < COUNT; ++i) x[i] = dg_to_float(v.e[i]);
+    dg_codes8<COUNT>(x, s, inverse, code);
+#pragma unroll
+    for (int i = 0; i < COUNT / 4; ++i) words[i] = dg_bytes(code + 4 * i);
+    if (k + COUNT <= end)
+        __builtin_memcpy(row + k, words, COUNT);
+    else
+        for (int i = 0; k + i < end; ++i) row[k + i] = (int8_t)(words[i / 4] >> (8 * (i & 3)));
+}
+
+template <class T, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void quantize_tokens_kernel(const T *x, int32_t K, int32_t pad, int64_t stride_n, int8_t *codes,
+                                                                  int64_t stride_codes, float *scale)
+{
+    constexpr int COUNT = 16 / sizeof(T), STEP = THREADS * COUNT;
+    __shared__ float part[THREADS / 64];
+    const T *row = x + (int64_t)blockIdx.x * stride_n;
+    int8_t *out = codes + (int64_t)blockIdx.x * stride_codes;
+    const int32_t mine = threadIdx.x * COUNT;
+    DgVec<T, COUNT> held[HELD ? HELD : 1];
+    float most = 0.0f;
+    bool finite = true;
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = elements<T, COUNT>(row, mine + i * STEP, K);
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) look_at(held[i], most, finite);
+    } else {
+        for (int32_t k = mine; k < K; k += STEP) look_at(elements<T, COUNT>(row, k, K), most, finite);
     }
-    __syncthreads();
-    most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    const float s = whole[0] && whole[1] && whole[2] && whole[3] ? dg_scale8(most) : __builtin_nanf("");
+    const float s = dg_scale8(workgroup_most<THREADS / 64>(most, finite, part)), inverse = dg_inverse8(s);
     if (threadIdx.x == 0) scale[blockIdx.x] = s;
-    for (int k = threadIdx.x; k < K; k += 256) out[k] = (int8_t)dg_code8(dg_to_float(row[k]), s);
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+            if (mine + i * STEP < pad) store_codes(out, mine + i * STEP, pad, held[i], s, inverse);
+    } else {
+        for (int32_t k = mine; k < pad; k += STEP) store_codes(out, k, pad, elements<T, COUNT>(row, k, K), s, inverse);
+    }
 }
 
 // ---- the product ------------------------------------------------------------------------------------------------------
@@ -76,52 +135,123 @@ __device__ __forceinline__ void store4(const DgGemmI8 &p, int32_t m, int32_t n, 
     }
 }
 
-// 16 channels x 16 TOKENS tokens by a workgroup whose eight wavefronts share K; their sums meet in LDS.
-template <class T, int TOKENS>
-__global__ __launch_bounds__(512) void gemm_i8_few_kernel(DgGemmI8 p)
+// ---- few tokens ---------------------------------------------------------------------------------------------------------
+//
+// A workgroup computes 16 ROWS channels x 16 TOKENS tokens; its eight wavefronts share K in pieces of 128 positions, a cache line of a row, and
+// their sums meet in LDS.  The weights are read once, straight into the matrix instructions' operands, STEPS pieces in flight a wavefront.
+// FUSED: the tokens are quantised here too, by every workgroup for itself, into LDS, while the first weights are on their way: for a token
+// or two that is less than another launch.
+
+constexpr int FEW_WAVES = 8, FEW_PIECE = 128 * FEW_WAVES;
+constexpr int FUSED_BYTES = 32768;       // codes that FUSED holds in LDS
+
+template <class X>
+struct Fused {
+    const X *x;
+    int64_t stride_x;
+    int32_t pitch;                       // of a token's codes in LDS: K rounded up to 128
+};
+
+template <class T, class X, int ROWS, int TOKENS, bool FUSED>
+__global__ __launch_bounds__(64 * FEW_WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
 {
-    __shared__ v4i sums[7][TOKENS][64];
+    constexpr int STEPS = TOKENS == 1 ? 4 : 2;
+    __shared__ v4i sums[FEW_WAVES][ROWS][TOKENS][64];
+    extern __shared__ int8_t quantized[];
+    __shared__ float part[FUSED ? 4 : 1][FEW_WAVES], scales[FUSED ? 4 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int32_t m0 = blockIdx.x * 16, n0 = blockIdx.y * (16 * TOKENS);
-    const int8_t *w = p.W + (int64_t)min(m0 + r, p.M - 1) * p.stride_w + 16 * g;
-    const int8_t *a[TOKENS];
+    const int32_t m0 = blockIdx.x * (16 * ROWS), last = p.N - 1;
+    const int8_t *w[ROWS], *a[TOKENS];
 #pragma unroll
-    for (int t = 0; t < TOKENS; ++t) a[t] = p.A + (int64_t)min(n0 + 16 * t + r, p.N - 1) * p.stride_a + 16 * g;
-    v4i acc[TOKENS] = {};
-    constexpr int AHEAD = TOKENS == 1 ? 4 : 2;              // steps whose loads are in flight together
-    int32_t k = 64 * wave;
-    for (; k + 512 * (AHEAD - 1) + 64 <= p.K; k += 512 * AHEAD) {
-        v4i wk[AHEAD], ak[AHEAD][TOKENS];
+    for (int i = 0; i < ROWS; ++i) w[i] = p.W + (int64_t)min(m0 + 16 * i + r, p.M - 1) * p.stride_w;
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            __builtin_memcpy(&wk[u], w + k + 512 * u, 16);
+    for (int t = 0; t < TOKENS; ++t) a[t] = FUSED ? quantized + min(r, last) * f.pitch : p.A + (int64_t)min(16 * t + r, last) * p.stride_a;
+    // a wavefront's place in its piece: two instructions of 64 positions, 16 a lane
+    int32_t k = 128 * wave + 16 * g;
+    v4i wk[STEPS][ROWS][2];
+    const auto fetch_weights = [&] {
 #pragma unroll
-            for (int t = 0; t < TOKENS; ++t) __builtin_memcpy(&ak[u][t], a[t] + k + 512 * u, 16);
+        for (int u = 0; u < STEPS; ++u)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) __builtin_memcpy(&wk[u][i][h], w[i] + k + FEW_PIECE * u + 64 * h, 16);
+    };
+    // whether all of a round's pieces lie in the row
+    const auto whole = [&] { return k - 16 * g + FEW_PIECE * (STEPS - 1) + 128 <= p.K; };
+    const bool begun = whole();
+    if (begun) fetch_weights();
+    if constexpr (FUSED) {
+        constexpr int COUNT = 16 / sizeof(X), STEP = 64 * FEW_WAVES * COUNT;
+        for (int n = 0; n <= last; ++n) {
+            const X *row = f.x + n * f.stride_x;
+            float most = 0.0f;
+            bool finite = true;
+            for (int32_t at = threadIdx.x * COUNT; at < p.K; at += STEP) look_at(elements<X, COUNT>(row, at, p.K), most, finite);
+            const float s = dg_scale8(workgroup_most<FEW_WAVES>(most, finite, part[n])), inverse = dg_inverse8(s);
+            if (threadIdx.x == 0) scales[n] = s;
+            for (int32_t at = threadIdx.x * COUNT; at < f.pitch; at += STEP)
+                store_codes(quantized + n * f.pitch, at, f.pitch, elements<X, COUNT>(row, at, p.K), s, inverse);
         }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int t = 0; t < TOKENS; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[u], ak[u][t], acc[t], 0, 0, 0);
+        __syncthreads();
     }
-    for (; k < p.K; k += 512) {
-        const v4i wk = codes16(w - 16 * g, k + 16 * g, p.K);
+    v4i acc[ROWS][TOKENS] = {};
+    const auto multiply = [&] {
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t)
-            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk, codes16(a[t] - 16 * g, k + 16 * g, p.K), acc[t], 0, 0, 0);
+        for (int u = 0; u < STEPS; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) {
+                    v4i ak;
+                    __builtin_memcpy(&ak, a[t] + k + FEW_PIECE * u + 64 * h, 16);
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[u][i][h], ak, acc[i][t], 0, 0, 0);
+                }
+    };
+    if (begun) {
+        multiply();
+        k += FEW_PIECE * STEPS;
+        for (; whole(); k += FEW_PIECE * STEPS) {
+            fetch_weights();
+            multiply();
+        }
     }
-    if (wave)
+    for (; k - 16 * g < p.K; k += FEW_PIECE)
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t) sums[wave - 1][t][lane] = acc[t];
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                const v4i ak = codes16(a[t], k + 64 * h, p.K);
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i)
+                    acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(codes16(w[i], k + 64 * h, p.K), ak, acc[i][t], 0, 0, 0);
+            }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) sums[wave][i][t][lane] = acc[i][t];
     __syncthreads();
-    if (wave) return;
+    // the blocks of 16 x 16 are dealt out to the wavefronts
 #pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-        v4i s = acc[t];
+    for (int block = 0; block < ROWS * TOKENS; ++block) {
+        if (block % FEW_WAVES != wave) continue;
+        const int i = block % ROWS, t = block / ROWS;
+        v4i s = sums[0][i][t][lane];
 #pragma unroll
-        for (int i = 0; i < 7; ++i) s += sums[i][t][lane];
-        const int32_t n = n0 + 16 * t + r;
-        if (n < p.N) store4<T>(p, m0 + 4 * g, n, p.scale_n[n], {s[0], s[1], s[2], s[3]});
+        for (int k = 1; k < FEW_WAVES; ++k) s += sums[k][i][t][lane];
+        const int32_t n = 16 * t + r;
+        if (n <= last) store4<T>(p, m0 + 16 * i + 4 * g, n, FUSED ? scales[n] : p.scale_n[n], {s[0], s[1], s[2], s[3]});
     }
+}
+
+template <class T, int TOKENS>
+void launch_few(const DgGemmI8 &p, hipStream_t stream)
+{
+    const Fused<float> none = {nullptr, 0, 0};
+    // 32 channels a workgroup share the tokens' loads; with too few channels for that, 16
+    if (p.M >= 16 * dg_simd_count() / 4 * 2) gemm_i8_few_kernel<T, float, 2, TOKENS, false><<<(p.M + 31) / 32, 64 * FEW_WAVES, 0, stream>>>(p, none);
+    else gemm_i8_few_kernel<T, float, 1, TOKENS, false><<<(p.M + 15) / 16, 64 * FEW_WAVES, 0, stream>>>(p, none);
 }
 
 // ---- many tokens: tiles ------------------------------------------------------------------------------------------------
@@ -261,23 +391,54 @@ void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
 }   // namespace
 
 dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, int8_t *codes,
-                                    int64_t stride_codes, float *scale, hipStream_t stream)
+                                    int64_t stride_codes, int64_t pad, float *scale, hipStream_t stream)
 {
     dg_with_type(type, [&](auto t) {
-        quantize_tokens_kernel<<<(uint32_t)N, 256, 0, stream>>>((const decltype(t) *)x, (int32_t)K, stride_n, codes, stride_codes, scale);
+        typedef decltype(t) T;
+        const auto launch = [&](auto threads, auto held) {
+            constexpr int THREADS = decltype(threads)::value;
+            quantize_tokens_kernel<T, THREADS, decltype(held)::value><<<(uint32_t)N, THREADS, 0, stream>>>((const T *)x, (int32_t)K, (int32_t)pad, stride_n,
+                                                                                                         codes, stride_codes, scale);
+        };
+        const auto by_length = [&](auto threads) {
+            const int64_t step = decltype(threads)::value * (16 / sizeof(T));
+            if (K <= step) launch(threads, std::integral_constant<int, 1>{});
+            else if (K <= 2 * step) launch(threads, std::integral_constant<int, 2>{});
+            else if (K <= 4 * step) launch(threads, std::integral_constant<int, 4>{});
+            else if (K <= 8 * step) launch(threads, std::integral_constant<int, 8>{});
+            else launch(threads, std::integral_constant<int, 0>{});
+        };
+        // few tokens: as many threads as there are, so that each has little to do; many: workgroups that others can stand beside
+        if (N <= 256) by_length(std::integral_constant<int, 1024>{});
+        else by_length(std::integral_constant<int, 256>{});
         return 0;
     });
     return dg_check_launch("dg_quantize_tokens");
+}
+
+bool dg_linear_i8_fuses(int64_t N, int64_t K) { return N <= 4 && N * ((K + 127) / 128 * 128) <= FUSED_BYTES; }
+
+dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, int64_t stride_x, dg_dtype type, hipStream_t stream)
+{
+    dg_with_type(type, [&](auto t) {
+        dg_with_type(x_type, [&](auto s) {
+            const Fused<decltype(s)> f = {(const decltype(s) *)x, stride_x, (p.K + 127) / 128 * 128};
+            gemm_i8_few_kernel<decltype(t), decltype(s), 1, 1, true><<<(p.M + 15) / 16, 64 * FEW_WAVES, (uint32_t)(p.N * f.pitch), stream>>>(p, f);
+            return 0;
+        });
+        return 0;
+    });
+    return dg_check_launch("dg_linear_i8");
 }
 
 dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream)
 {
     dg_with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const uint32_t rows = (uint32_t)((p.M + 15) / 16);
         const auto tiles = [&](int64_t side) { return ((p.M + side - 1) / side) * ((p.N + side - 1) / side); };
-        if (p.N <= 16) gemm_i8_few_kernel<T, 1><<<rows, 512, 0, stream>>>(p);
-        else if (p.N <= 64) gemm_i8_few_kernel<T, 4><<<rows, 512, 0, stream>>>(p);
+        if (p.N <= 16) launch_few<T, 1>(p, stream);
+        else if (p.N <= 32) launch_few<T, 2>(p, stream);
+        else if (p.N <= 64) launch_few<T, 4>(p, stream);
         else if (tiles(256) >= 192) launch_tiles<T, 2, 4, 4, 2>(p, stream);
         else if (tiles(128) >= 192) launch_tiles<T, 2, 2, 2, 2>(p, stream);
         else launch_tiles<T, 2, 2, 1, 1>(p, stream);
