@@ -49,17 +49,19 @@ __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a)
     uint8_t *codes = block + (values ? a.c.part : 0);
     if constexpr (BITS == 8) {
         const float s = finite ? dg_scale8(fmaxf(fabsf(lo), fabsf(hi))) : __builtin_nanf("");
+        const DgDivisor by = dg_divisor(s);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint8_t code = (uint8_t)(dg_code8(dg_to_float(x.e[i]), s) + 128);
+            const uint8_t code = (uint8_t)((dg_code8(dg_to_float(x.e[i]), by) & by.keep) + 128);
             codes[values ? dg_value_byte<8>(t, d + i, DIM) : dg_key_byte<8>(t, d + i, DIM)] = code;
         }
         if ((lane & 31) == 0) numbers[values ? a.c.page_size : 0] = s;
     } else {
         const float s = finite ? hi / 15.0f - lo / 15.0f : __builtin_nanf("");
+        const DgDivisor by = dg_divisor(s);
 #pragma unroll
         for (int i = 0; i < PER; i += 2) {
-            const int low = dg_code4(dg_to_float(x.e[i]), s, lo), high = dg_code4(dg_to_float(x.e[i + 1]), s, lo);
+            const int low = dg_code4(dg_to_float(x.e[i]), lo, by) & by.keep, high = dg_code4(dg_to_float(x.e[i + 1]), lo, by) & by.keep;
             codes[values ? dg_value_byte<4>(t, d + i, DIM) : dg_key_byte<4>(t, d + i, DIM)] = (uint8_t)(low | high << 4);
         }
         if ((lane & 31) == 0) {

@@ -42,27 +42,35 @@ template <class T, int COUNT>
 __device__ __forceinline__ DgVec<T, COUNT> elements(const T *row, int32_t k, int32_t K)
 {
     if (k + COUNT <= K) return dg_load_vec<T, COUNT>(row + k);
-    DgVec<T, COUNT> v = {};
-    for (int i = 0; k + i < K; ++i) v.e[i] = row[k + i];
+    uint64_t word[2] = {0, 0};
+    for (int i = 0; k + i < K; ++i) {                   // (a loop: code that is short arrives soon, and few lanes come here)
+        uint64_t bits = 0;
+        __builtin_memcpy(&bits, row + k + i, sizeof(T));
+        (i * (int)sizeof(T) < 8 ? word[0] : word[1]) |= bits << (8 * sizeof(T) * i & 63);
+    }
+    DgVec<T, COUNT> v;
+    static_assert(sizeof(v) == sizeof(word), "16 bytes");
+    __builtin_memcpy(&v, word, sizeof(v));
     return v;
 }
 
 // The codes of COUNT elements to position k of a row whose bytes up to `end` are this kernel's.
 template <class T, int COUNT>
-__device__ __forceinline__ void store_codes(int8_t *row, int32_t k, int32_t end, const DgVec<T, COUNT> &v, float s, float inverse)
+__device__ __forceinline__ void store_codes(int8_t *row, int32_t k, int32_t end, const DgVec<T, COUNT> &v, const DgDivisor &d)
 {
-    float x[COUNT];
     int code[COUNT];
     uint32_t words[COUNT / 4];
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) x[i] = dg_to_float(v.e[i]);
-    dg_codes8<COUNT>(x, s, inverse, code);
+    for (int i = 0; i < COUNT; ++i) code[i] = dg_code8(dg_to_float(v.e[i]), d);
 #pragma unroll
-    for (int i = 0; i < COUNT / 4; ++i) words[i] = dg_bytes(code + 4 * i);
-    if (k + COUNT <= end)
+    for (int i = 0; i < COUNT / 4; ++i) words[i] = dg_bytes(code + 4 * i) & d.keep;
+    if (k + COUNT <= end) {
         __builtin_memcpy(row + k, words, COUNT);
-    else
-        for (int i = 0; k + i < end; ++i) row[k + i] = (int8_t)(words[i / 4] >> (8 * (i & 3)));
+    } else {
+        uint64_t all = 0;
+        __builtin_memcpy(&all, words, COUNT);
+        for (; k < end; ++k, all >>= 8) row[k] = (int8_t)all;
+    }
 }
 
 template <class T, int THREADS, int HELD>
@@ -85,14 +93,15 @@ __global__ __launch_bounds__(THREADS) void quantize_tokens_kernel(const T *x, in
     } else {
         for (int32_t k = mine; k < K; k += STEP) look_at(elements<T, COUNT>(row, k, K), most, finite);
     }
-    const float s = dg_scale8(workgroup_most<THREADS / 64>(most, finite, part)), inverse = dg_inverse8(s);
+    const float s = dg_scale8(workgroup_most<THREADS / 64>(most, finite, part));
+    const DgDivisor by = dg_divisor(s);
     if (threadIdx.x == 0) scale[blockIdx.x] = s;
     if constexpr (HELD) {
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
-            if (mine + i * STEP < pad) store_codes(out, mine + i * STEP, pad, held[i], s, inverse);
+            if (mine + i * STEP < pad) store_codes(out, mine + i * STEP, pad, held[i], by);
     } else {
-        for (int32_t k = mine; k < pad; k += STEP) store_codes(out, k, pad, elements<T, COUNT>(row, k, K), s, inverse);
+        for (int32_t k = mine; k < pad; k += STEP) store_codes(out, k, pad, elements<T, COUNT>(row, k, K), by);
     }
 }
 
@@ -101,11 +110,14 @@ __global__ __launch_bounds__(THREADS) void quantize_tokens_kernel(const T *x, in
 // 16 codes from position k of a row of K; those at K and beyond count as 0 and are not read.
 __device__ __forceinline__ v4i codes16(const int8_t *row, int32_t k, int32_t K)
 {
-    v4i v = {0, 0, 0, 0};
-    if (k + 16 <= K)
+    v4i v;
+    if (k + 16 <= K) {
         __builtin_memcpy(&v, row + k, 16);
-    else
-        for (int i = 0; k + i < K; ++i) v[i >> 2] |= (int)(uint8_t)row[k + i] << (8 * (i & 3));
+        return v;
+    }
+    uint64_t word[2] = {0, 0};
+    for (int i = 0; k + i < K; ++i) (i < 8 ? word[0] : word[1]) |= (uint64_t)(uint8_t)row[k + i] << (8 * i & 63);
+    __builtin_memcpy(&v, word, 16);
     return v;
 }
 
@@ -188,10 +200,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_i8_few_kernel(DgGemmI8 p,
             float most = 0.0f;
             bool finite = true;
             for (int32_t at = threadIdx.x * COUNT; at < p.K; at += STEP) look_at(elements<X, COUNT>(row, at, p.K), most, finite);
-            const float s = dg_scale8(workgroup_most<FEW_WAVES>(most, finite, part[n])), inverse = dg_inverse8(s);
+            const float s = dg_scale8(workgroup_most<FEW_WAVES>(most, finite, part[n]));
+            const DgDivisor by = dg_divisor(s);
             if (threadIdx.x == 0) scales[n] = s;
             for (int32_t at = threadIdx.x * COUNT; at < f.pitch; at += STEP)
-                store_codes(quantized + n * f.pitch, at, f.pitch, elements<X, COUNT>(row, at, p.K), s, inverse);
+                store_codes(quantized + n * f.pitch, at, f.pitch, elements<X, COUNT>(row, at, p.K), by);
         }
         __syncthreads();
     }
@@ -277,7 +290,9 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128;
     constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);       // loads of 8 rows a wavefront makes of a stage
     static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole loads, and the same places in each");
-    __shared__ __align__(1024) uint8_t stages[2][STAGE];
+    constexpr int RESULTS = WAVES * 32 * (32 * TM + 4) * 4;
+    __shared__ __align__(1024) uint8_t room[2 * STAGE > RESULTS ? 2 * STAGE : RESULTS];
+    uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room;
     const DgGemmI8 &p = args.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -305,7 +320,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     }
     const dg_v4i buffer_w = dg_buffer((const uint8_t *)rows_w, DIRECT ? (uint32_t)((have_w - 1) * (uint32_t)p.stride_w + p.K) : 0u);
     const dg_v4i buffer_a = dg_buffer((const uint8_t *)rows_a, DIRECT ? (uint32_t)((have_a - 1) * (uint32_t)p.stride_a + p.K) : 0u);
-    const uint32_t lds = dg_lds_address(stages) + 1024 * wave;
+    const uint32_t lds = dg_lds_address(room) + 1024 * wave;
     v4i held[DIRECT ? 1 : LOADS];
 
     auto fetch = [&](int32_t k, int to) {
@@ -359,18 +374,43 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
         }
         if (more) arrive(now ^ 1);
     }
+    // The results go by way of LDS, a wavefront's 32 tokens at a time: rows of channels leave side by side, and a loop does it (written out
+    // it was 20 KB of instructions, which a small product waited for as they arrived).
+    constexpr int PITCH = 32 * TM + 4, LANES = 8 * TM, ROWS = 64 / LANES;
+    __syncthreads();
+    int *mine = (int *)room + wave * (32 * PITCH);
+    const int32_t m = m0 + wm * (32 * TM) + 4 * (lane % LANES), have = min(p.M - m, 4);
+    float sm[4], bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        sm[e] = e < have ? p.scale_m[m + e] : 0.0f;
+        bias[e] = p.bias && e < have ? p.bias[m + e] : 0.0f;
+    }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        const int32_t n = n0 + (wn * TN + j) * 32 + r;
-        if (n >= p.N) continue;
-        const float sn = p.scale_n[n];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *(v4i *)(mine + r * PITCH + 32 * i + 8 * e + 4 * g) = (v4i){acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        const int32_t first_n = n0 + (wn * TN + j) * 32, end = min(p.N - first_n, 32);
+#pragma unroll 1
+        for (int t = lane / LANES; t < end; t += ROWS) {
+            const v4i sum = *(const v4i *)(mine + t * PITCH + 4 * (lane % LANES));
+            const float sn = p.scale_n[first_n + t];
+            T *out = (T *)p.out + (int64_t)(first_n + t) * p.stride_out + m;
+            DgVec<T, 4> y;
+#pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int32_t m = m0 + (wm * TM + i) * 32 + 8 * e + 4 * g;
-                store4<T>(p, m, n, sn, {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+                const float x = (float)sum[e] * sm[e] * sn;
+                y.e[e] = dg_from_float<T>(p.bias ? x + bias[e] : x);
             }
+            if (have == 4) dg_store_vec<T, 4>(out, y);
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) out[e] = y.e[e];
+        }
     }
 }
 
