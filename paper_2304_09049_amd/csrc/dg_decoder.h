@@ -139,9 +139,9 @@ struct DgGemmI8 {
     int64_t stride_out;                  // elements from token to token
 };
 dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream);
-// The product's kernel for few tokens quantising them itself (p.A and p.scale_n are not used), and whether it holds them.
+// The product's kernel for few tokens quantising one itself (p.A and p.scale_n are not used), and whether it does.
 bool dg_linear_i8_fuses(int64_t N, int64_t K);
-dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, int64_t stride_x, dg_dtype type, hipStream_t stream);
+dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, dg_dtype type, hipStream_t stream);
 
 dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t T, const int64_t strides[4],
                                 const int32_t *slots, hipStream_t stream);

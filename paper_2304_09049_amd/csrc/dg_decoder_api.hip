@@ -126,7 +126,7 @@ dg_status dg_linear_i8(const int8_t *W_dev, int64_t stride_w, const void *x_dev,
     const int64_t pitch = codes_pitch(K);
     float *scale_n = (float *)(codes + N * pitch);
     const DgGemmI8 p = {W_dev, codes, stride_w, pitch, (int32_t)M, (int32_t)N, (int32_t)K, scale_m_dev, scale_n, bias_m_dev, out_dev, stride_out};
-    if (dg_linear_i8_fuses(N, K)) return dg_launch_linear_i8_fused(p, x_dev, x_type, stride_x, out_type, (hipStream_t)hip_stream);
+    if (dg_linear_i8_fuses(N, K)) return dg_launch_linear_i8_fused(p, x_dev, x_type, out_type, (hipStream_t)hip_stream);
     s = dg_launch_quantize_tokens(x_dev, x_type, N, K, stride_x, codes, pitch, pitch, scale_n, (hipStream_t)hip_stream);
     if (s) return s;
     return dg_launch_gemm_i8(p, out_type, (hipStream_t)hip_stream);

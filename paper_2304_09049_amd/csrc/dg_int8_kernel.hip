@@ -1,4 +1,6 @@
 // Tokens quantised to 8 bits, and products of 8-bit codes with a scale for each token and each channel.
+#include <cstdlib>
+
 #include "dg_decoder.h"
 #include "dg_lds_dma.h"
 
@@ -149,35 +151,34 @@ __device__ __forceinline__ void store4(const DgGemmI8 &p, int32_t m, int32_t n, 
 
 // ---- few tokens ---------------------------------------------------------------------------------------------------------
 //
-// A workgroup computes 16 ROWS channels x 16 TOKENS tokens; its eight wavefronts share K in pieces of 128 positions, a cache line of a row, and
+// A workgroup computes 16 ROWS channels x 16 TOKENS tokens; its wavefronts share K in pieces of 128 positions, a cache line of a row, and
 // their sums meet in LDS.  The weights are read once, straight into the matrix instructions' operands, STEPS pieces in flight a wavefront.
-// FUSED: the tokens are quantised here too, by every workgroup for itself, into LDS, while the first weights are on their way: for a token
-// or two that is less than another launch.
+// FUSED: a single token is quantised here too, by every workgroup for itself, into LDS, while the first weights are on their way (4096 x 4096
+// 6.5 us for 8.1 as two launches; four tokens 11.3 for 8.5).
 
-constexpr int FEW_WAVES = 8, FEW_PIECE = 128 * FEW_WAVES;
 constexpr int FUSED_BYTES = 32768;       // codes that FUSED holds in LDS
 
 template <class X>
 struct Fused {
     const X *x;
-    int64_t stride_x;
-    int32_t pitch;                       // of a token's codes in LDS: K rounded up to 128
+    int32_t pitch;                       // its codes' bytes in LDS: K rounded up to 128
 };
 
-template <class T, class X, int ROWS, int TOKENS, bool FUSED>
-__global__ __launch_bounds__(64 * FEW_WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
+template <class T, class X, int WAVES, int ROWS, int TOKENS, bool FUSED>
+__global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
 {
-    constexpr int STEPS = TOKENS == 1 ? 4 : 2;
-    __shared__ v4i sums[FEW_WAVES][ROWS][TOKENS][64];
+    constexpr int STEPS = TOKENS == 1 ? 4 : 2, FEW_PIECE = 128 * WAVES;
+    __shared__ v4i sums[WAVES][ROWS][TOKENS][64];
     extern __shared__ int8_t quantized[];
-    __shared__ float part[FUSED ? 4 : 1][FEW_WAVES], scales[FUSED ? 4 : 1];
+    __shared__ float part[WAVES];
+    float own_scale = 0.0f;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
     const int32_t m0 = blockIdx.x * (16 * ROWS), last = p.N - 1;
     const int8_t *w[ROWS], *a[TOKENS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) w[i] = p.W + (int64_t)min(m0 + 16 * i + r, p.M - 1) * p.stride_w;
 #pragma unroll
-    for (int t = 0; t < TOKENS; ++t) a[t] = FUSED ? quantized + min(r, last) * f.pitch : p.A + (int64_t)min(16 * t + r, last) * p.stride_a;
+    for (int t = 0; t < TOKENS; ++t) a[t] = FUSED ? quantized : p.A + (int64_t)min(16 * t + r, last) * p.stride_a;
     // a wavefront's place in its piece: two instructions of 64 positions, 16 a lane
     int32_t k = 128 * wave + 16 * g;
     v4i wk[STEPS][ROWS][2];
@@ -194,18 +195,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_i8_few_kernel(DgGemmI8 p,
     const bool begun = whole();
     if (begun) fetch_weights();
     if constexpr (FUSED) {
-        constexpr int COUNT = 16 / sizeof(X), STEP = 64 * FEW_WAVES * COUNT;
-        for (int n = 0; n <= last; ++n) {
-            const X *row = f.x + n * f.stride_x;
-            float most = 0.0f;
-            bool finite = true;
-            for (int32_t at = threadIdx.x * COUNT; at < p.K; at += STEP) look_at(elements<X, COUNT>(row, at, p.K), most, finite);
-            const float s = dg_scale8(workgroup_most<FEW_WAVES>(most, finite, part[n]));
-            const DgDivisor by = dg_divisor(s);
-            if (threadIdx.x == 0) scales[n] = s;
-            for (int32_t at = threadIdx.x * COUNT; at < f.pitch; at += STEP)
-                store_codes(quantized + n * f.pitch, at, f.pitch, elements<X, COUNT>(row, at, p.K), by);
-        }
+        constexpr int COUNT = 16 / sizeof(X), STEP = 64 * WAVES * COUNT;
+        float most = 0.0f;
+        bool finite = true;
+        for (int32_t at = threadIdx.x * COUNT; at < p.K; at += STEP) look_at(elements<X, COUNT>(f.x, at, p.K), most, finite);
+        own_scale = dg_scale8(workgroup_most<WAVES>(most, finite, part));
+        const DgDivisor by = dg_divisor(own_scale);
+        for (int32_t at = threadIdx.x * COUNT; at < f.pitch; at += STEP)
+            store_codes(quantized, at, f.pitch, elements<X, COUNT>(f.x, at, p.K), by);
         __syncthreads();
     }
     v4i acc[ROWS][TOKENS] = {};
@@ -248,29 +245,32 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_i8_few_kernel(DgGemmI8 p,
     // the blocks of 16 x 16 are dealt out to the wavefronts
 #pragma unroll
     for (int block = 0; block < ROWS * TOKENS; ++block) {
-        if (block % FEW_WAVES != wave) continue;
+        if (block % WAVES != wave) continue;
         const int i = block % ROWS, t = block / ROWS;
         v4i s = sums[0][i][t][lane];
 #pragma unroll
-        for (int k = 1; k < FEW_WAVES; ++k) s += sums[k][i][t][lane];
+        for (int k = 1; k < WAVES; ++k) s += sums[k][i][t][lane];
         const int32_t n = 16 * t + r;
-        if (n <= last) store4<T>(p, m0 + 16 * i + 4 * g, n, FUSED ? scales[n] : p.scale_n[n], {s[0], s[1], s[2], s[3]});
+        if (n <= last) store4<T>(p, m0 + 16 * i + 4 * g, n, FUSED ? own_scale : p.scale_n[n], {s[0], s[1], s[2], s[3]});
     }
 }
 
 template <class T, int TOKENS>
 void launch_few(const DgGemmI8 &p, hipStream_t stream)
 {
-    const Fused<float> none = {nullptr, 0, 0};
-    // 32 channels a workgroup share the tokens' loads; with too few channels for that, 16
-    if (p.M >= 16 * dg_simd_count() / 4 * 2) gemm_i8_few_kernel<T, float, 2, TOKENS, false><<<(p.M + 31) / 32, 64 * FEW_WAVES, 0, stream>>>(p, none);
-    else gemm_i8_few_kernel<T, float, 1, TOKENS, false><<<(p.M + 15) / 16, 64 * FEW_WAVES, 0, stream>>>(p, none);
+    const Fused<float> none = {nullptr, 0};
+    const int units = dg_simd_count() / 4;
+    // 32 channels a workgroup share the tokens' loads; with too few channels for that, 16, and where that leaves half of the compute units
+    // without a workgroup, twice the wavefronts
+    if (p.M >= 32 * units) gemm_i8_few_kernel<T, float, 8, 2, TOKENS, false><<<(p.M + 31) / 32, 512, 0, stream>>>(p, none);
+    else if (p.M > 8 * units || p.K <= 2048) gemm_i8_few_kernel<T, float, 8, 1, TOKENS, false><<<(p.M + 15) / 16, 512, 0, stream>>>(p, none);
+    else gemm_i8_few_kernel<T, float, 16, 1, TOKENS, false><<<(p.M + 15) / 16, 1024, 0, stream>>>(p, none);
 }
 
 // ---- many tokens: tiles ------------------------------------------------------------------------------------------------
 //
 // A workgroup of WM x WN wavefronts computes 32 WM TM channels x 32 WN TN tokens, TM x TN blocks of 32 x 32 a wavefront, 128 positions of
-// K at a time, in two LDS stages: the next stage's loads are in flight while this one is multiplied.  A row's 128 bytes lie in LDS as eight pieces
+// K at a time, in a ring of LDS stages: the next ones' loads are in flight while one is multiplied.  A row's 128 bytes lie in LDS as eight pieces
 // of 16, piece c of row r at place c ^ (r / 2 % 8), so that the 16 lanes that an LDS read serves together find 16 different ones.
 // DIRECT: rows begin on 16 bytes and K is whole pieces: the loads write LDS themselves.  Otherwise they go through registers.
 
@@ -284,14 +284,14 @@ struct TileArgs {
 };
 constexpr int GROUP = 4;
 
-template <class T, int WM, int WN, int TM, int TN, bool DIRECT>
+template <class T, int WM, int WN, int TM, int TN, int RING, bool DIRECT>
 __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs args)
 {
-    constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128;
+    constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128, STAGES = DIRECT ? RING : 2;
     constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);       // loads of 8 rows a wavefront makes of a stage
     static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole loads, and the same places in each");
     constexpr int RESULTS = WAVES * 32 * (32 * TM + 4) * 4;
-    __shared__ __align__(1024) uint8_t room[2 * STAGE > RESULTS ? 2 * STAGE : RESULTS];
+    __shared__ __align__(1024) uint8_t room[STAGES * STAGE > RESULTS ? STAGES * STAGE : RESULTS];
     uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room;
     const DgGemmI8 &p = args.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -340,24 +340,10 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
             }
         }
     };
-    auto arrive = [&](int to) {
-        if constexpr (DIRECT) {
-            dg_wait_for_loads<0>();
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) *(v4i *)(stages[to] + 1024 * (wave + WAVES * i) + 16 * lane) = held[i];
-        }
-        __syncthreads();
-    };
-
     const int r = lane & 31, g = lane >> 5, wm = wave % WM, wn = wave / WM;
     const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
     v16i acc[TM][TN] = {};
-    fetch(0, 0);
-    arrive(0);
-    for (int32_t k = 0, now = 0; k < p.K; k += 128, now ^= 1) {
-        const bool more = k + 128 < p.K;
-        if (more) fetch(k + 128, now ^ 1);
+    const auto multiply = [&](int now) {
         const uint8_t *w = stages[now] + wm * (TM * 4096), *a = stages[now] + BM * 128 + wn * (TN * 4096);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -372,7 +358,36 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wk[i], ak[j], acc[i][j], 0, 0, 0);
         }
-        if (more) arrive(now ^ 1);
+    };
+    if constexpr (DIRECT) {
+        // A stage's loads are waited for when its turn comes; the barrier after that says that every wavefront's are in, and that all are done with
+        // the stage before, whose place the loads of STAGES - 1 ahead then take.  (Past the end of K there is nothing to load; the waits count on
+        // loads, so they go on, from outside the buffers: zeros, which nothing reads.)
+        for (int i = 0; i < STAGES - 1; ++i) fetch(128 * i, i);
+        int now = 0, to = STAGES - 1;
+        for (int32_t k = 0; k < p.K; k += 128) {
+            dg_wait_for_loads<(STAGES - 2) * LOADS>();
+            __syncthreads();
+            fetch(k + 128 * (STAGES - 1), to);
+            multiply(now);
+            now = now + 1 == STAGES ? 0 : now + 1;
+            to = to + 1 == STAGES ? 0 : to + 1;
+        }
+        dg_wait_for_loads<0>();
+    } else {
+        const auto put = [&](int to) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) *(v4i *)(stages[to] + 1024 * (wave + WAVES * i) + 16 * lane) = held[i];
+            __syncthreads();
+        };
+        fetch(0, 0);
+        put(0);
+        for (int32_t k = 0, now = 0; k < p.K; k += 128, now ^= 1) {
+            const bool more = k + 128 < p.K;
+            if (more) fetch(k + 128, now ^ 1);
+            multiply(now);
+            if (more) put(now ^ 1);
+        }
     }
     // The results go by way of LDS, a wavefront's 32 tokens at a time: rows of channels leave side by side, and a loop does it (written out
     // it was 20 KB of instructions, which a small product waited for as they arrived).
@@ -414,7 +429,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     }
 }
 
-template <class T, int WM, int WN, int TM, int TN>
+template <class T, int WM, int WN, int TM, int TN, int RING>
 void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
 {
     TileArgs a = {p, (p.M + 32 * WM * TM - 1) / (32 * WM * TM), (p.N + 32 * WN * TN - 1) / (32 * WN * TN), {}, {}, 0};
@@ -424,8 +439,8 @@ void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n;
     const bool direct = p.K % 16 == 0 && p.stride_w % 16 == 0 && p.stride_a % 16 == 0 && (uintptr_t)p.W % 16 == 0 && (uintptr_t)p.A % 16 == 0 &&
                         p.stride_w < (1 << 22) && p.stride_a < (1 << 22);          // (a tile's rows lie within 2^30 bytes)
-    if (direct) gemm_i8_tile_kernel<T, WM, WN, TM, TN, true><<<tiles, 64 * WM * WN, 0, stream>>>(a);
-    else gemm_i8_tile_kernel<T, WM, WN, TM, TN, false><<<tiles, 64 * WM * WN, 0, stream>>>(a);
+    if (direct) gemm_i8_tile_kernel<T, WM, WN, TM, TN, RING, true><<<tiles, 64 * WM * WN, 0, stream>>>(a);
+    else gemm_i8_tile_kernel<T, WM, WN, TM, TN, 2, false><<<tiles, 64 * WM * WN, 0, stream>>>(a);
 }
 
 }   // namespace
@@ -456,14 +471,14 @@ dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int
     return dg_check_launch("dg_quantize_tokens");
 }
 
-bool dg_linear_i8_fuses(int64_t N, int64_t K) { return N <= 4 && N * ((K + 127) / 128 * 128) <= FUSED_BYTES; }
+bool dg_linear_i8_fuses(int64_t N, int64_t K) { return N == 1 && K <= FUSED_BYTES; }
 
-dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, int64_t stride_x, dg_dtype type, hipStream_t stream)
+dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, dg_dtype type, hipStream_t stream)
 {
     dg_with_type(type, [&](auto t) {
         dg_with_type(x_type, [&](auto s) {
-            const Fused<decltype(s)> f = {(const decltype(s) *)x, stride_x, (p.K + 127) / 128 * 128};
-            gemm_i8_few_kernel<decltype(t), decltype(s), 1, 1, true><<<(p.M + 15) / 16, 64 * FEW_WAVES, (uint32_t)(p.N * f.pitch), stream>>>(p, f);
+            const Fused<decltype(s)> f = {(const decltype(s) *)x, (p.K + 127) / 128 * 128};
+            gemm_i8_few_kernel<decltype(t), decltype(s), 8, 1, 1, true><<<(p.M + 15) / 16, 512, (uint32_t)f.pitch, stream>>>(p, f);
             return 0;
         });
         return 0;
@@ -476,12 +491,14 @@ dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream
     dg_with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const auto tiles = [&](int64_t side) { return ((p.M + side - 1) / side) * ((p.N + side - 1) / side); };
-        if (p.N <= 16) launch_few<T, 1>(p, stream);
+        const char *forced = dg_override("DG_GEMM_I8_TILE");
+        const int side = forced ? atoi(forced) : p.N <= 64 ? 0 : tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
+        if (side == 256) launch_tiles<T, 2, 4, 4, 2, 2>(p, stream);
+        else if (side == 128) launch_tiles<T, 2, 2, 2, 2, 4>(p, stream);
+        else if (side == 64) launch_tiles<T, 2, 2, 1, 1, 6>(p, stream);
+        else if (p.N <= 16) launch_few<T, 1>(p, stream);
         else if (p.N <= 32) launch_few<T, 2>(p, stream);
-        else if (p.N <= 64) launch_few<T, 4>(p, stream);
-        else if (tiles(256) >= 192) launch_tiles<T, 2, 4, 4, 2>(p, stream);
-        else if (tiles(128) >= 192) launch_tiles<T, 2, 2, 2, 2>(p, stream);
-        else launch_tiles<T, 2, 2, 1, 1>(p, stream);
+        else launch_few<T, 4>(p, stream);
         return 0;
     });
     return dg_check_launch("dg_gemm_i8");
