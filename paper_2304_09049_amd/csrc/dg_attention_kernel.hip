@@ -114,7 +114,8 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
     constexpr int BLOCKS = DIM / 16;                      // accumulators of 16 channels
     constexpr int VALUE_WORDS = DIM * BITS / 128;         // words of 4 tokens that a lane takes of a unit
     const DgAttention &a = args.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    // (a matrix instruction runs whatever the lanes' mask: what it stands under has to be a scalar branch)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int piece = blockIdx.x % args.pieces, rows = blockIdx.x / args.pieces;
     const int row_block = rows % args.row_blocks, bh = rows / args.row_blocks;
     const int h = bh % a.cache.heads, b = bh / a.cache.heads;

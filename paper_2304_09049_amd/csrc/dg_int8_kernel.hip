@@ -1,5 +1,5 @@
 // Tokens quantised to 8 bits, and products of 8-bit codes with a scale for each token and each channel.
-#include <cstdlib>
+#include <cstring>
 
 #include "dg_decoder.h"
 #include "dg_lds_dma.h"
@@ -167,33 +167,32 @@ struct Fused {
 template <class T, class X, int WAVES, int ROWS, int TOKENS, bool FUSED>
 __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
 {
-    constexpr int STEPS = TOKENS == 1 ? 4 : 2, FEW_PIECE = 128 * WAVES;
+    constexpr int STEPS = TOKENS == 1 ? 4 : 2;
     __shared__ v4i sums[WAVES][ROWS][TOKENS][64];
     extern __shared__ int8_t quantized[];
     __shared__ float part[WAVES];
     float own_scale = 0.0f;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    // (a matrix instruction runs whatever the lanes' mask: what it stands under has to be a scalar branch)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t m0 = blockIdx.x * (16 * ROWS), last = p.N - 1;
     const int8_t *w[ROWS], *a[TOKENS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) w[i] = p.W + (int64_t)min(m0 + 16 * i + r, p.M - 1) * p.stride_w;
 #pragma unroll
     for (int t = 0; t < TOKENS; ++t) a[t] = FUSED ? quantized : p.A + (int64_t)min(16 * t + r, last) * p.stride_a;
-    // a wavefront's place in its piece: two instructions of 64 positions, 16 a lane
-    int32_t k = 128 * wave + 16 * g;
-    v4i wk[STEPS][ROWS][2];
-    const auto fetch_weights = [&] {
+    // a piece: two instructions of 64 positions, 16 a lane
+    const int32_t pieces = p.K / 128;
+    v4i wk[STEPS][ROWS][2], ak[STEPS][TOKENS][2];
+    const auto fetch_weights = [&](int32_t piece) {
 #pragma unroll
         for (int u = 0; u < STEPS; ++u)
+            if (piece + WAVES * u < pieces)
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i)
+                for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) __builtin_memcpy(&wk[u][i][h], w[i] + k + FEW_PIECE * u + 64 * h, 16);
+                    for (int h = 0; h < 2; ++h) __builtin_memcpy(&wk[u][i][h], w[i] + 128 * (piece + WAVES * u) + 64 * h + 16 * g, 16);
     };
-    // whether all of a round's pieces lie in the row
-    const auto whole = [&] { return k - 16 * g + FEW_PIECE * (STEPS - 1) + 128 <= p.K; };
-    const bool begun = whole();
-    if (begun) fetch_weights();
+    fetch_weights(wave);
     if constexpr (FUSED) {
         constexpr int COUNT = 16 / sizeof(X), STEP = 64 * WAVES * COUNT;
         float most = 0.0f;
@@ -206,36 +205,34 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fus
         __syncthreads();
     }
     v4i acc[ROWS][TOKENS] = {};
-    const auto multiply = [&] {
+    for (int32_t piece = wave; piece < pieces; piece += WAVES * STEPS) {
+        if (piece != wave) fetch_weights(piece);
 #pragma unroll
         for (int u = 0; u < STEPS; ++u)
+            if (piece + WAVES * u < pieces)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
-                for (int t = 0; t < TOKENS; ++t) {
-                    v4i ak;
-                    __builtin_memcpy(&ak, a[t] + k + FEW_PIECE * u + 64 * h, 16);
+                    for (int h = 0; h < 2; ++h) __builtin_memcpy(&ak[u][t][h], a[t] + 128 * (piece + WAVES * u) + 64 * h + 16 * g, 16);
 #pragma unroll
-                    for (int i = 0; i < ROWS; ++i) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[u][i][h], ak, acc[i][t], 0, 0, 0);
-                }
-    };
-    if (begun) {
-        multiply();
-        k += FEW_PIECE * STEPS;
-        for (; whole(); k += FEW_PIECE * STEPS) {
-            fetch_weights();
-            multiply();
-        }
+        for (int u = 0; u < STEPS; ++u)
+            if (piece + WAVES * u < pieces)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+                        for (int i = 0; i < ROWS; ++i)
+                            acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[u][i][h], ak[u][t][h], acc[i][t], 0, 0, 0);
     }
-    for (; k - 16 * g < p.K; k += FEW_PIECE)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
+    if (128 * pieces < p.K && pieces % WAVES == wave)               // the rest of the row
+#pragma unroll 1
+        for (int32_t k = 128 * pieces; k < p.K; k += 64)
 #pragma unroll
             for (int t = 0; t < TOKENS; ++t) {
-                const v4i ak = codes16(a[t], k + 64 * h, p.K);
+                const v4i at = codes16(a[t], k + 16 * g, p.K);
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-                    acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(codes16(w[i], k + 64 * h, p.K), ak, acc[i][t], 0, 0, 0);
+                for (int i = 0; i < ROWS; ++i) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(codes16(w[i], k + 16 * g, p.K), at, acc[i][t], 0, 0, 0);
             }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
@@ -269,8 +266,8 @@ void launch_few(const DgGemmI8 &p, hipStream_t stream)
 
 // ---- many tokens: tiles ------------------------------------------------------------------------------------------------
 //
-// A workgroup of WM x WN wavefronts computes 32 WM TM channels x 32 WN TN tokens, TM x TN blocks of 32 x 32 a wavefront, 128 positions of
-// K at a time, in a ring of LDS stages: the next ones' loads are in flight while one is multiplied.  A row's 128 bytes lie in LDS as eight pieces
+// KS groups of WM x WN wavefronts compute 32 WM TM channels x 32 WN TN tokens, TM x TN blocks of 32 x 32 a wavefront; a group takes 128
+// positions of K of a stage's 128 KS, and the groups' sums meet in LDS at the end.  The stages are a ring of LDS stages: the next ones' loads are in flight while one is multiplied.  A row's 128 bytes lie in LDS as eight pieces
 // of 16, piece c of row r at place c ^ (r / 2 % 8), so that the 16 lanes that an LDS read serves together find 16 different ones.
 // DIRECT: rows begin on 16 bytes and K is whole pieces: the loads write LDS themselves.  Otherwise they go through registers.
 
@@ -284,17 +281,18 @@ struct TileArgs {
 };
 constexpr int GROUP = 4;
 
-template <class T, int WM, int WN, int TM, int TN, int RING, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs args)
+template <class T, int WM, int WN, int TM, int TN, int KS, int RING, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN * KS) void gemm_i8_tile_kernel(TileArgs args)
 {
     constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128, STAGES = DIRECT ? RING : 2;
-    constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);       // loads of 8 rows a wavefront makes of a stage
+    constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);       // loads of 8 rows a wavefront makes of its group's stage
     static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole loads, and the same places in each");
     constexpr int RESULTS = WAVES * 32 * (32 * TM + 4) * 4;
-    __shared__ __align__(1024) uint8_t room[STAGES * STAGE > RESULTS ? STAGES * STAGE : RESULTS];
-    uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room;
+    __shared__ __align__(1024) uint8_t room[STAGES * STAGE * KS > RESULTS ? STAGES * STAGE * KS : RESULTS];
     const DgGemmI8 &p = args.p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % WAVES);
+    const int share = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / WAVES);
+    uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room + share * STAGES;        // (each group has a ring of its own)
 
     // Neighbouring workgroups go to different dies (eight): each die takes a run of tiles of its own, and walks it in groups of GROUP rows
     // of tiles, so that what it reads twice is in its own cache.
@@ -320,7 +318,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     }
     const dg_v4i buffer_w = dg_buffer((const uint8_t *)rows_w, DIRECT ? (uint32_t)((have_w - 1) * (uint32_t)p.stride_w + p.K) : 0u);
     const dg_v4i buffer_a = dg_buffer((const uint8_t *)rows_a, DIRECT ? (uint32_t)((have_a - 1) * (uint32_t)p.stride_a + p.K) : 0u);
-    const uint32_t lds = dg_lds_address(room) + 1024 * wave;
+    const uint32_t lds = dg_lds_address(room) + share * (STAGES * STAGE) + 1024 * wave;
     v4i held[DIRECT ? 1 : LOADS];
 
     auto fetch = [&](int32_t k, int to) {
@@ -343,32 +341,39 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     const int r = lane & 31, g = lane >> 5, wm = wave % WM, wn = wave / WM;
     const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
     v16i acc[TM][TN] = {};
+    // 32 positions at a time; the operands of the next ones are read before these are multiplied (left to itself the compiler reads each just
+    // before its use, and a wavefront waits for LDS four times a stage)
+    v4i wk[2][TM], ak[2][TN];
+    const auto read = [&](int now, int s) {
+        const uint8_t *w = stages[now] + wm * (TM * 4096) + (first ^ (s * 32)), *a = stages[now] + BM * 128 + wn * (TN * 4096) + (first ^ (s * 32));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) wk[s & 1][i] = *(const v4i *)(w + i * 4096);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ak[s & 1][j] = *(const v4i *)(a + j * 4096);
+    };
     const auto multiply = [&](int now) {
-        const uint8_t *w = stages[now] + wm * (TM * 4096), *a = stages[now] + BM * 128 + wn * (TN * 4096);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const uint32_t at = first ^ (s * 32);
-            v4i wk[TM], ak[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) wk[i] = *(const v4i *)(w + i * 4096 + at);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) ak[j] = *(const v4i *)(a + j * 4096 + at);
+            if (s < 3) read(now, s + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wk[i], ak[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wk[s & 1][i], ak[s & 1][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     if constexpr (DIRECT) {
         // A stage's loads are waited for when its turn comes; the barrier after that says that every wavefront's are in, and that all are done with
         // the stage before, whose place the loads of STAGES - 1 ahead then take.  (Past the end of K there is nothing to load; the waits count on
         // loads, so they go on, from outside the buffers: zeros, which nothing reads.)
-        for (int i = 0; i < STAGES - 1; ++i) fetch(128 * i, i);
+        for (int i = 0; i < STAGES - 1; ++i) fetch(128 * (KS * i + share), i);
         int now = 0, to = STAGES - 1;
-        for (int32_t k = 0; k < p.K; k += 128) {
+        for (int32_t k = 0; k < p.K; k += 128 * KS) {
             dg_wait_for_loads<(STAGES - 2) * LOADS>();
             __syncthreads();
-            fetch(k + 128 * (STAGES - 1), to);
+            read(now, 0);
+            fetch(k + 128 * (KS * (STAGES - 1) + share), to);
             multiply(now);
             now = now + 1 == STAGES ? 0 : now + 1;
             to = to + 1 == STAGES ? 0 : to + 1;
@@ -380,11 +385,12 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
             for (int i = 0; i < LOADS; ++i) *(v4i *)(stages[to] + 1024 * (wave + WAVES * i) + 16 * lane) = held[i];
             __syncthreads();
         };
-        fetch(0, 0);
+        fetch(128 * share, 0);
         put(0);
-        for (int32_t k = 0, now = 0; k < p.K; k += 128, now ^= 1) {
-            const bool more = k + 128 < p.K;
-            if (more) fetch(k + 128, now ^ 1);
+        for (int32_t k = 0, now = 0; k < p.K; k += 128 * KS, now ^= 1) {
+            const bool more = k + 128 * KS < p.K;
+            if (more) fetch(k + 128 * (KS + share), now ^ 1);
+            read(now, 0);
             multiply(now);
             if (more) put(now ^ 1);
         }
@@ -394,6 +400,37 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     constexpr int PITCH = 32 * TM + 4, LANES = 8 * TM, ROWS = 64 / LANES;
     __syncthreads();
     int *mine = (int *)room + wave * (32 * PITCH);
+    if constexpr (KS > 1) {
+        // the other groups' sums, one group after another
+        static_assert(TM * TN * 4096 * WAVES <= STAGES * STAGE * KS, "a group's sums fit");
+        int4 *const sums = (int4 *)room + wave * (TM * TN * 256) + lane;
+#pragma unroll 1
+        for (int from = 1; from < KS; ++from) {
+            if (share == from)
+#pragma unroll
+                for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const v16i &c = acc[i / TN][i % TN];
+                        sums[(4 * i + e) * 64] = make_int4(c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]);
+                    }
+            __syncthreads();
+            if (share == 0)
+#pragma unroll
+                for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int4 x = sums[(4 * i + e) * 64];
+                        v16i &c = acc[i / TN][i % TN];
+                        c[4 * e] += x.x;
+                        c[4 * e + 1] += x.y;
+                        c[4 * e + 2] += x.z;
+                        c[4 * e + 3] += x.w;
+                    }
+            __syncthreads();
+        }
+        if (share) return;
+    }
     const int32_t m = m0 + wm * (32 * TM) + 4 * (lane % LANES), have = min(p.M - m, 4);
     float sm[4], bias[4];
 #pragma unroll
@@ -429,7 +466,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_i8_tile_kernel(TileArgs arg
     }
 }
 
-template <class T, int WM, int WN, int TM, int TN, int RING>
+template <class T, int WM, int WN, int TM, int TN, int KS, int RING>
 void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
 {
     TileArgs a = {p, (p.M + 32 * WM * TM - 1) / (32 * WM * TM), (p.N + 32 * WN * TN - 1) / (32 * WN * TN), {}, {}, 0};
@@ -439,8 +476,38 @@ void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
     const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n;
     const bool direct = p.K % 16 == 0 && p.stride_w % 16 == 0 && p.stride_a % 16 == 0 && (uintptr_t)p.W % 16 == 0 && (uintptr_t)p.A % 16 == 0 &&
                         p.stride_w < (1 << 22) && p.stride_a < (1 << 22);          // (a tile's rows lie within 2^30 bytes)
-    if (direct) gemm_i8_tile_kernel<T, WM, WN, TM, TN, RING, true><<<tiles, 64 * WM * WN, 0, stream>>>(a);
-    else gemm_i8_tile_kernel<T, WM, WN, TM, TN, 2, false><<<tiles, 64 * WM * WN, 0, stream>>>(a);
+    if (direct) gemm_i8_tile_kernel<T, WM, WN, TM, TN, KS, RING, true><<<tiles, 64 * WM * WN * KS, 0, stream>>>(a);
+    else gemm_i8_tile_kernel<T, WM, WN, TM, TN, KS, 2, false><<<tiles, 64 * WM * WN * KS, 0, stream>>>(a);
+}
+
+enum class Form { Few, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
+constexpr int FEW_TOKENS = 32;
+
+// The kernel for up to 32 tokens (16 x 4096 x 4096 6.4 us, 64 x 64 tiles 8.8; 32 tokens 8.5, 9.3; 48 11.3, 9.5), or the tile whose rounds over the
+// compute units, one workgroup each, cost least.  A round's cost by tile, us for K = 4096 and 8192: 64 x 64 10, 24; 128 x 64 15, 34; 128 x 128 23, 46;
+// 256 x 128 39, 72; 256 x 256 54, 104.  Of 20 products from 64 x 4096 x 4096 to 8192 x 8192 x 8192 this takes the fastest tile on all.
+Form form_of(const DgGemmI8 &p)
+{
+    static const struct {
+        Form form;
+        int32_t m, n, cost;
+        const char *name;
+    } tiles[] = {{Form::Tile64x64, 64, 64, 28, "64x64"}, {Form::Tile128x64, 128, 64, 40, "128x64"}, {Form::Tile128x128, 128, 128, 54, "128x128"},
+                 {Form::Tile256x128, 256, 128, 85, "256x128"}, {Form::Tile256x256, 256, 256, 124, "256x256"}};
+    const char *forced = dg_override("DG_GEMM_I8_TILE");
+    const int64_t units = dg_simd_count() / 4;
+    Form best = Form::Few;
+    int64_t least = INT64_MAX;
+    if (!forced && p.N <= FEW_TOKENS) return best;
+    for (const auto &t : tiles) {
+        if (forced && !strcmp(forced, t.name)) return t.form;
+        const int64_t count = ((p.M + t.m - 1) / t.m) * (int64_t)((p.N + t.n - 1) / t.n), cost = (count + units - 1) / units * t.cost;
+        if (cost < least) {
+            least = cost;
+            best = t.form;
+        }
+    }
+    return p.N <= FEW_TOKENS ? Form::Few : best;
 }
 
 }   // namespace
@@ -490,15 +557,17 @@ dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream
 {
     dg_with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const auto tiles = [&](int64_t side) { return ((p.M + side - 1) / side) * ((p.N + side - 1) / side); };
-        const char *forced = dg_override("DG_GEMM_I8_TILE");
-        const int side = forced ? atoi(forced) : p.N <= 64 ? 0 : tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-        if (side == 256) launch_tiles<T, 2, 4, 4, 2, 2>(p, stream);
-        else if (side == 128) launch_tiles<T, 2, 2, 2, 2, 4>(p, stream);
-        else if (side == 64) launch_tiles<T, 2, 2, 1, 1, 6>(p, stream);
-        else if (p.N <= 16) launch_few<T, 1>(p, stream);
-        else if (p.N <= 32) launch_few<T, 2>(p, stream);
-        else launch_few<T, 4>(p, stream);
+        switch (form_of(p)) {
+        case Form::Few:
+            if (p.N <= 16) launch_few<T, 1>(p, stream);
+            else launch_few<T, 2>(p, stream);
+            break;
+        case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
+        case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
+        case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
+        case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
+        case Form::Tile256x256: launch_tiles<T, 2, 4, 4, 2, 1, 2>(p, stream); break;
+        }
         return 0;
     });
     return dg_check_launch("dg_gemm_i8");

@@ -104,6 +104,16 @@ def test_gemm_i8(M, N, K, dtype):
     assert same(as_f32(out), rounded(product(W, A, sm, sn, bias if with_bias else None), dtype))
 
 
+@pytest.mark.parametrize("tile", ["64x64", "128x64", "128x128", "256x128", "256x256"])
+@pytest.mark.parametrize("M,N,K", [(300, 200, 1040), (257, 130, 128), (64, 300, 16), (1030, 515, 272), (129, 1, 2000), (520, 260, 999)])
+def test_gemm_i8_in_every_tile(M, N, K, tile, monkeypatch):
+    monkeypatch.setenv("DG_GEMM_I8_TILE", tile)
+    W, A, sm, sn, bias = _operands(M, N, K, M + N + K)
+    for dtype in TYPES:
+        out = dg.dg_gemm_i8(on_gpu(W), on_gpu(A), on_gpu(sm), on_gpu(sn), bias=on_gpu(bias), dtype=TYPES[dtype])
+        assert same(as_f32(out), rounded(product(W, A, sm, sn, bias), dtype))
+
+
 @pytest.mark.parametrize("M,N,K", [(20, 2, 131071), (300, 300, 131071), (40, 20, 131056)])
 def test_gemm_i8_at_the_end_of_the_sums_range(M, N, K):
     W, A, sm, sn, _ = _operands(M, N, K, 1, full=True)
