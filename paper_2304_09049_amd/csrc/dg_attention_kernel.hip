@@ -11,9 +11,11 @@
 // a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  The maximum is
 // raised only when a score passes it by 2^4, so that p <= 16 and the weights stay below 2^15.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "dg_decoder.h"
+#include "dg_lds_dma.h"
 
 namespace {
 
@@ -94,25 +96,40 @@ struct Args {
 struct Sequence {
     int32_t first, count, ctx, past;      // past: the context before its new tokens (negative if these are more than the context)
 };
+// (b is the same in every lane of a wavefront)
 __device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
 {
+    const auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     Sequence s;
-    s.first = min(max(a.q_start[b], 0), a.T);
-    s.count = min(max(a.q_start[b + 1], s.first), a.T) - s.first;
-    s.ctx = (int32_t)min((int64_t)max(a.ctx_len[b], 0), (int64_t)a.table_width * a.cache.page_size);
+    const int start = scalar(a.q_start[b]), stop = scalar(a.q_start[b + 1]), ctx = scalar(a.ctx_len[b]);
+    s.first = min(max(start, 0), a.T);
+    s.count = min(max(stop, s.first), a.T) - s.first;
+    s.ctx = (int32_t)min((int64_t)max(ctx, 0), (int64_t)a.table_width * a.cache.page_size);
     s.past = s.ctx - s.count;
     s.count = min(s.count, a.max_q);
     return s;
 }
 
-constexpr int WAVES = 4, TILE = 32;      // tokens per step of a wavefront
+constexpr int TILE = 32;      // tokens per step of a wavefront
 
-template <class T, int BITS, int DIM>
-__global__ __launch_bounds__(256) void attention_kernel(Args args)
+// A tile -- two units of 16 tokens -- as a wavefront keeps it in LDS: keys, values, and 64 numbers (unit 0's key and value scales, unit 1's), with 4
+// bits 64 more (z).  A wavefront has DEPTH tiles of its own on the way, by loads that write LDS: HBM answers after one or two microseconds, and
+// registers hold half a tile at most beside the sums (loads into registers, issued as soon as the tile before had left them: 131071 tokens of 8 bits
+// 63 us, 64 contexts of up to 8192 of 4 bits 162).
+template <int BITS, int DIM>
+struct Tile {
+    static constexpr int PART = 4 * DIM * BITS, NUMBERS = BITS == 8 ? 256 : 512, BYTES = 2 * PART + NUMBERS;
+    static constexpr int LOADS = 2 * PART / 1024 + NUMBERS / 256;
+    static constexpr int DEPTH = DIM == 256 ? 2 : BITS == 8 ? (DIM == 128 ? 2 : 3) : 3;
+};
+
+template <class T, int BITS, int DIM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
 {
     constexpr int STEPS = DIM / 32;                       // products of 32 channels
     constexpr int BLOCKS = DIM / 16;                      // accumulators of 16 channels
     constexpr int VALUE_WORDS = DIM * BITS / 128;         // words of 4 tokens that a lane takes of a unit
+    constexpr bool TWICE = std::is_same<T, _Float16>::value;        // weights in two halves, see below
     const DgAttention &a = args.a;
     // (a matrix instruction runs whatever the lanes' mask: what it stands under has to be a scalar branch)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
@@ -120,18 +137,71 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
     const int row_block = rows % args.row_blocks, bh = rows / args.row_blocks;
     const int h = bh % a.cache.heads, b = bh / a.cache.heads;
     const Sequence seq = sequence(a, b);
+    const int have = min(seq.count * args.group - row_block * 16, 16);                      // rows of the block that are there
+    if (have <= 0) return;
     const int row = row_block * 16 + r;
     const int i = (int)dg_fdiv((uint32_t)row, args.by_group), j = row - i * args.group;     // new token, head of the group
-    const bool there = i < seq.count;
-    if (row_block * 16 >= seq.count * args.group) return;                                   // (no row of the block is there)
-    const int last_i = min((row_block * 16 + 15) / args.group, seq.count - 1);
-    const int past = seq.past;
-    // tokens that the row sees: those before `end`; any row of the block: before `block_end`; every row: before `all_end`
-    const int end = !there ? 0 : a.causal ? max(past + i + 1, 0) : seq.ctx;
-    const int block_end = a.causal ? max(past + last_i + 1, 0) : seq.ctx;
-    const int all_end = row_block * 16 + 15 >= seq.count * args.group ? 0 : a.causal ? max(past + (int)dg_fdiv((uint32_t)row_block * 16, args.by_group) + 1, 0) : seq.ctx;
+    const bool there = r < have;
+    const int first_i = (int)dg_fdiv((uint32_t)row_block * 16, args.by_group), last_i = (int)dg_fdiv((uint32_t)(row_block * 16 + have - 1), args.by_group);
+    // tokens that the row sees: those before `end`; any row of the block: before `block_end`; every one of 16: before `all_end`
+    const int end = !there ? 0 : a.causal ? max(seq.past + i + 1, 0) : seq.ctx;
+    const int block_end = a.causal ? max(seq.past + last_i + 1, 0) : seq.ctx;
+    const int all_end = have < 16 ? 0 : a.causal ? max(seq.past + first_i + 1, 0) : seq.ctx;
     const int from = piece * args.piece_tokens;
     const int to = piece == args.pieces - 1 ? block_end : min(block_end, from + args.piece_tokens);
+
+    const uint8_t *const heads = a.cache.base + (int64_t)h * a.cache.head;
+    // (through the scalar cache: a vector load would be waited for together with the tiles on the way)
+    const auto table = (const __attribute__((address_space(4))) int32_t *)(a.table + (int64_t)b * a.table_width);
+    typedef Tile<BITS, DIM> Kept;
+    constexpr int SHARES = WAVES * 16 * (DIM + 4) * 4, RINGS = WAVES * Kept::DEPTH * Kept::BYTES;
+    __shared__ __align__(1024) uint8_t room[SHARES > RINGS ? SHARES : RINGS];
+    const uint8_t *const ring = room + wave * (Kept::DEPTH * Kept::BYTES);
+    const uint32_t ring_lds = dg_lds_address(ring);
+    // A unit past the context, or whose page is none of the cache's, is read from the first page instead and its tokens count as unseen.
+    const auto page_of = [&](int t) { return t < seq.ctx ? table[dg_fdiv((uint32_t)t, a.cache.by_page)] : -1; };
+    const auto is_page = [&](int page) { return (uint32_t)page < (uint32_t)a.cache.pages; };
+    const auto fetch = [&](int t0, const int (&page)[2], int slot) {
+        const uint8_t *block[2];
+        uint32_t in_page[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t t = (uint32_t)(t0 + 16 * u);
+            in_page[u] = is_page(page[u]) ? t - dg_fdiv(t, a.cache.by_page) * a.cache.page_size : 0;
+            block[u] = heads + (is_page(page[u]) ? (int64_t)page[u] : 0) * a.cache.page_bytes();
+        }
+        const uint32_t lds = ring_lds + slot * Kept::BYTES;
+        constexpr int CHUNKS = DIM * BITS / 8;                  // of 16 bytes, of a unit's keys or values
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int n = 0; n < Kept::PART / 1024; ++n) {
+                const uint32_t to = lds + which * Kept::PART + 1024 * n;
+                if constexpr (CHUNKS >= 64) {
+                    const int u = 64 * n / CHUNKS;
+                    dg_load16_to_lds(block[u] + which * a.cache.part + in_page[u] * (DIM * BITS / 8), 1024 * (n % (CHUNKS / 64)) + 16 * lane, to);
+                } else {
+                    const bool u = lane >= 32;
+                    dg_load16_to_lds((u ? block[1] : block[0]) + which * a.cache.part + (u ? in_page[1] : in_page[0]) * (DIM * BITS / 8) + 16 * (lane & 31), to);
+                }
+            }
+        const bool u = lane >= 32;
+        const uint8_t *numbers = (u ? block[1] : block[0]) + 2 * a.cache.part + 4 * ((u ? in_page[1] : in_page[0]) + (lane & 16 ? a.cache.page_size : 0) + (lane & 15));
+#pragma unroll
+        for (int n = 0; n < Kept::NUMBERS / 256; ++n) dg_load4_to_lds(numbers + 8 * n * a.cache.page_size, lds + 2 * Kept::PART + 256 * n);
+    };
+    // the pages of the DEPTH tiles on the way; those of the one after are asked for a tile ahead
+    constexpr int DEPTH = Kept::DEPTH, STRIDE = TILE * WAVES;
+    int t0 = from + TILE * wave;
+    int page[DEPTH + 1][2];
+#pragma unroll
+    for (int n = 0; n <= DEPTH; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) page[n][u] = page_of(t0 + n * STRIDE + 16 * u);
+#pragma unroll
+    for (int n = 0; n < DEPTH; ++n)
+        if (t0 + n * STRIDE < to) fetch(t0 + n * STRIDE, page[n], n);
+    int slot = 0;
 
     // the row's query
     v8h q[STEPS];
@@ -168,62 +238,42 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
 
     v4f o[BLOCKS] = {};
     float m = -__builtin_inff(), shift = 0.0f, l = 0.0f, oz = 0.0f, R = 0.0f, per_R = 0.0f;
-    const uint8_t *const heads = a.cache.base + (int64_t)h * a.cache.head;
-    const int32_t *const table = a.table + (int64_t)b * a.table_width;
-
-    for (int t0 = from + TILE * wave; t0 < to; t0 += TILE * WAVES) {
-        // the two units' places; a unit past the context, or whose page is none of the cache's, is not read: its tokens count as unseen
-        const uint8_t *unit[2];
-        uint32_t in_page[2];
-        int unit_end[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int t = t0 + 16 * u;
-            const bool in = t < seq.ctx;
-            const uint32_t entry = in ? dg_fdiv((uint32_t)t, a.cache.by_page) : 0;
-            const int32_t page = in ? table[entry] : -1;
-            const bool ok = (uint32_t)page < (uint32_t)a.cache.pages;
-            in_page[u] = ok ? (uint32_t)t - entry * a.cache.page_size : 0;
-            unit[u] = heads + (ok ? (int64_t)page : 0) * a.cache.page_bytes();
-            unit_end[u] = ok ? end : 0;
-        }
-        const bool all_seen = t0 + TILE <= all_end && unit_end[0] && unit_end[1];
-        v4f score[2], ks[2], vs[2], kz[2], vz[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float *numbers = (const float *)(unit[u] + 2 * a.cache.part) + in_page[u] + 4 * g;
-            ks[u] = *(const v4f *)numbers;
-            vs[u] = *(const v4f *)(numbers + a.cache.page_size);
-            if (BITS == 4) {
-                kz[u] = *(const v4f *)(numbers + 2 * a.cache.page_size);
-                vz[u] = *(const v4f *)(numbers + 3 * a.cache.page_size);
-            }
-        }
+#pragma unroll 1
+    for (; t0 < to; t0 += STRIDE) {
+        if (t0 + (DEPTH - 1) * STRIDE < to) dg_wait_for_loads<(DEPTH - 1) * Kept::LOADS>();
+        else dg_wait_for_loads<0>();
+        const uint8_t *const tile = ring + slot * Kept::BYTES;
+        const bool is[2] = {is_page(page[0][0]), is_page(page[0][1])};
+        const int unit_end[2] = {is[0] ? end : 0, is[1] ? end : 0};
+        const bool all_seen = t0 + TILE <= all_end && is[0] && is[1];
         // scores
+        v4f score[2], ks[2], kz[2], vs[2], vz[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint8_t *keys = unit[u] + in_page[u] * (DIM * BITS / 8);
+            const v4f *numbers = (const v4f *)(tile + 2 * Kept::PART + 128 * u) + g;
+            ks[u] = numbers[0];
+            vs[u] = numbers[4];
+            if (BITS == 4) {
+                kz[u] = numbers[16];
+                vz[u] = numbers[20];
+            }
             v4f acc = {};
 #pragma unroll
-            for (int s = 0; s < STEPS; s += 2) {
-                v8h k0, k1;
+            for (int s = 0; s < STEPS / 2; ++s) {
+                const uint8_t *keys = tile + u * (Kept::PART / 2) + s * (128 * BITS);
+                v2h c[8];
                 if constexpr (BITS == 8) {
-                    const v4u w = *(const v4u *)(keys + 512 * s + 16 * lane);
-                    v2h c[8];
+                    const v4u w = *(const v4u *)(keys + 16 * lane);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) halves8(w[e], c[2 * e], c[2 * e + 1]);
-                    k0 = join(c[0], c[1], c[2], c[3]);
-                    k1 = join(c[4], c[5], c[6], c[7]);
                 } else {
-                    const v2u w = *(const v2u *)(keys + 256 * s + 8 * lane);
-                    v2h c[4];
-                    halves4(w[0], c);
-                    k0 = join(c[0], c[1], c[2], c[3]);
-                    halves4(w[1], c);
-                    k1 = join(c[0], c[1], c[2], c[3]);
+                    const v2u w = *(const v2u *)(keys + 8 * lane);
+                    v2h (&low)[4] = *(v2h(*)[4])c, (&high)[4] = *(v2h(*)[4])(c + 4);
+                    halves4(w[0], low);
+                    halves4(w[1], high);
                 }
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[s], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[s + 1], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[0], c[1], c[2], c[3]), q[2 * s], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[4], c[5], c[6], c[7]), q[2 * s + 1], acc, 0, 0, 0);
             }
             score[u] = acc;
         }
@@ -236,63 +286,68 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
                 if (BITS == 4) x = __builtin_fmaf(q_sum, __builtin_fmaf(8.0f, ks[u][e], kz[u][e]), x);
                 x *= f;
                 const int t = t0 + 16 * u + 4 * g + e;
-                if (!all_seen) {
-                    x = t < unit_end[u] ? x : -__builtin_inff();
-                    vs[u][e] = t < unit_end[u] ? vs[u][e] : 0.0f;
-                    if (BITS == 4) vz[u][e] = t < unit_end[u] ? vz[u][e] : 0.0f;
-                }
+                if (!all_seen) x = t < unit_end[u] ? x : -__builtin_inff();
                 top = fmaxf(top, x);
-                most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
                 score[u][e] = x;
             }
         if (__any(top > m + RAISE)) {
-            const float next = fmaxf(m, row_max(top));
-            const float next_shift = next == -__builtin_inff() ? 0.0f : next;
+            const float higher = fmaxf(m, row_max(top));
+            const float next_shift = higher == -__builtin_inff() ? 0.0f : higher;
             const float keep = exp2_(m - next_shift);
-            m = next;
+            m = higher;
             shift = next_shift;
             l *= keep;
             oz *= keep;
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[k] *= keep;
         }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!all_seen) {
+                    const bool seen = t0 + 16 * u + 4 * g + e < unit_end[u];
+                    vs[u][e] = seen ? vs[u][e] : 0.0f;
+                    if (BITS == 4) vz[u][e] = seen ? vz[u][e] : 0.0f;
+                }
+                most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
+            }
         if (__any(most_vs > R)) {
 #pragma unroll
             for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
-            // the next power of two above it, from 2^-100 to 2^127
-            const uint32_t bits = min(max((__float_as_uint(most_vs) >> 23) + 1, 27u), 254u);
-            const float next = __uint_as_float(bits << 23);
-            const float keep = R / next;
-            R = next;
-            per_R = __uint_as_float((254u - bits) << 23) * WEIGHT_UNIT;
+            // the next power of two above it, from 2^-100 to 2^126
+            const uint32_t bits = min(max((__float_as_uint(most_vs) >> 23) + 1, 27u), 253u);
+            const float inverse = __uint_as_float((254u - bits) << 23), keep = R * inverse;
+            R = __uint_as_float(bits << 23);
+            per_R = inverse * WEIGHT_UNIT;
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[k] *= keep;
         }
-        v2h w[2][2];
+        // The weights as the second product's operand.  Binary16 outputs show a weight's rounding beside their own (the error against 64 bits was 1.4
+        // times a binary32 computation's): there what the rounding left off goes through the matrix instructions as well.
+        _Float16 w[8], rest[8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float p[4], x[4];
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                p[e] = exp2_(score[u][e] - shift);
-                l += p[e];
-                if (BITS == 4) oz = __builtin_fmaf(p[e], __builtin_fmaf(8.0f, vs[u][e], vz[u][e]), oz);
-                x[e] = p[e] * (vs[u][e] * per_R);
+                const float p = exp2_(score[u][e] - shift);
+                l += p;
+                if (BITS == 4) oz = __builtin_fmaf(p, __builtin_fmaf(8.0f, vs[u][e], vz[u][e]), oz);
+                const float x = p * (vs[u][e] * per_R);
+                const int at = 4 * u + (BITS == 8 ? e : (e & 1) * 2 + (e >> 1));          // (4 bits: tokens 0, 2, 1, 3)
+                w[at] = (_Float16)x;
+                if (TWICE) rest[at] = (_Float16)(x - (float)w[at]);
             }
-            if constexpr (BITS == 8) {
-                w[u][0] = (v2h){(_Float16)x[0], (_Float16)x[1]};
-                w[u][1] = (v2h){(_Float16)x[2], (_Float16)x[3]};
-            } else {
-                w[u][0] = (v2h){(_Float16)x[0], (_Float16)x[2]};
-                w[u][1] = (v2h){(_Float16)x[1], (_Float16)x[3]};
-            }
-        }
-        const v8h weights = join(w[0][0], w[0][1], w[1][0], w[1][1]);
-        // values
+        const v8h weights = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+        const auto add = [&](v4f &acc, v8h values) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, weights, acc, 0, 0, 0);
+            if (TWICE)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, (v8h){rest[0], rest[1], rest[2], rest[3], rest[4], rest[5], rest[6], rest[7]}, acc, 0, 0, 0);
+        };
         uint32_t words[2][VALUE_WORDS];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint8_t *values = unit[u] + a.cache.part + in_page[u] * (DIM * BITS / 8) + g * (DIM * BITS / 2);
+            const uint8_t *values = tile + Kept::PART + u * (Kept::PART / 2) + g * (DIM * BITS / 2);
             if constexpr (VALUE_WORDS == 2) {
                 const v2u x = *(const v2u *)(values + 8 * r);
                 words[u][0] = x[0];
@@ -312,19 +367,29 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
                 v2h c[4];
                 halves8(words[0][k], c[0], c[1]);
                 halves8(words[1][k], c[2], c[3]);
-                o[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[0], c[1], c[2], c[3]), weights, o[k], 0, 0, 0);
+                add(o[k], join(c[0], c[1], c[2], c[3]));
             } else {
                 v2h c[4], d[4];      // (tokens 0 and 2, 1 and 3; even and odd channels)
                 halves4(words[0][k], c);
                 halves4(words[1][k], d);
-                o[2 * k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[0], c[2], d[0], d[2]), weights, o[2 * k], 0, 0, 0);
-                o[2 * k + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[1], c[3], d[1], d[3]), weights, o[2 * k + 1], 0, 0, 0);
+                add(o[2 * k], join(c[0], c[2], d[0], d[2]));
+                add(o[2 * k + 1], join(c[1], c[3], d[1], d[3]));
             }
         }
+        // the tile has been read: its place is the next one's
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t0 + DEPTH * STRIDE < to) fetch(t0 + DEPTH * STRIDE, page[DEPTH], slot);
+        slot = slot + 1 == DEPTH ? 0 : slot + 1;
+#pragma unroll
+        for (int n = 0; n < DEPTH; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) page[n][u] = page[n + 1][u];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) page[DEPTH][u] = page_of(t0 + (DEPTH + 1) * STRIDE + 16 * u);
     }
 
-    // the wavefronts' shares meet: a lane holds channel `channel(k, e)` of row r in o[k][e]
-    __shared__ float sum_o[16][DIM + 4];
+    // The wavefronts' shares meet.  A lane holds channels channel(4 k, e) ... + 3 of row r in o[4 k ... 4 k + 3][e].
+    float (*const all_o)[16][DIM + 4] = (float(*)[16][DIM + 4])room;       // (once every wavefront is done with its tiles)
     __shared__ float wave_m[WAVES][16], wave_l[WAVES][16];
     l = row_sum(l);
     oz = row_sum(oz);
@@ -335,96 +400,115 @@ __global__ __launch_bounds__(256) void attention_kernel(Args args)
     for (int k = 1; k < WAVES; ++k) most = fmaxf(most, wave_m[k][r]);
     const float mine = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);       // (a NaN stays one)
     if (g == 0) wave_l[wave][r] = l * mine;
-    const float unit_o = R * (1.0f / WEIGHT_UNIT) * mine;
-    auto channel = [&](int k, int e) {
-        if (BITS == 8) return 64 * (k / 4) + 16 * g + 4 * e + k % 4;
-        return DIM == 64 ? 16 * g + 4 * e + k : 128 * (k / 8) + 32 * g + 8 * e + k % 8;
-    };
-    for (int turn = 0; turn < WAVES; ++turn) {
-        if (wave == turn)
+    const float unit_o = R == 0.0f ? 1.0f : R * (1.0f / WEIGHT_UNIT) * mine;               // (nothing met: 0, or the NaN of a NaN)
+    const float add_z = oz * mine;
+    if (there)
 #pragma unroll
-            for (int k = 0; k < BLOCKS; ++k)
+        for (int k = 0; k < BLOCKS / 4; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = R == 0.0f ? o[k][e] : o[k][e] * unit_o;                // (nothing met: 0, or the NaN of a NaN)
-                    const float y = BITS == 4 ? __builtin_fmaf(oz, mine, x) : x;
-                    float &s = sum_o[r][channel(k, e)];
-                    s = turn ? s + y : y;
-                }
-        __syncthreads();
-    }
-    // 16 threads a row
-    const int my_row = threadIdx.x >> 4, part = threadIdx.x & 15;
-    const int out_row = row_block * 16 + my_row;
-    if (out_row >= seq.count * args.group) return;
-    const float total = wave_l[0][my_row] + wave_l[1][my_row] + wave_l[2][my_row] + wave_l[3][my_row];
-    const int oi = (int)dg_fdiv((uint32_t)out_row, args.by_group), oj = out_row - oi * args.group;
-    if (args.pieces == 1) {
-        T *out = (T *)a.out + (int64_t)(seq.first + oi) * a.out_token + (int64_t)(h * args.group + oj) * a.out_head;
-        const float by = total == 0.0f ? 0.0f : 1.0f / total;
-        DgVec<T, DIM / 16> v;
+            for (int e = 0; e < 4; ++e) {
+                const int channel = BITS == 8 ? 64 * k + 16 * g + 4 * e : DIM == 64 ? 16 * g + 4 * e : 128 * (k / 2) + 32 * g + 8 * e + 4 * (k % 2);
+                v4f x;
 #pragma unroll
-        for (int k = 0; k < DIM / 16; ++k) v.e[k] = dg_from_float<T>(sum_o[my_row][part * (DIM / 16) + k] * by);
-        dg_store_vec<T, DIM / 16>(out + part * (DIM / 16), v);
-    } else {
-        const int64_t at = (((int64_t)piece * a.B + b) * a.max_q + oi) * a.Hq + h * args.group + oj;
-        DgVec<float, DIM / 16> v;
+                for (int n = 0; n < 4; ++n) x[n] = BITS == 4 ? __builtin_fmaf(o[4 * k + n][e], unit_o, add_z) : o[4 * k + n][e] * unit_o;
+                *(v4f *)&all_o[wave][r][channel] = x;
+            }
+    __syncthreads();
+#pragma unroll 1
+    for (int at = threadIdx.x; at < have * (DIM / 4); at += 64 * WAVES) {
+        const int my_row = at / (DIM / 4), d = 4 * (at % (DIM / 4));
+        v4f sum = *(const v4f *)&all_o[0][my_row][d];
+        float total = wave_l[0][my_row], top = wave_m[0][my_row];
 #pragma unroll
-        for (int k = 0; k < DIM / 16; ++k) v.e[k] = sum_o[my_row][part * (DIM / 16) + k];
-        dg_store_vec<float, DIM / 16>(args.shares.o + at * DIM + part * (DIM / 16), v);
-        if (part == 0) {
-            float x = wave_m[0][my_row];
-            for (int k = 1; k < WAVES; ++k) x = fmaxf(x, wave_m[k][my_row]);
-            args.shares.m[at] = x;
-            args.shares.l[at] = total;
+        for (int k = 1; k < WAVES; ++k) {
+            sum += *(const v4f *)&all_o[k][my_row][d];
+            total += wave_l[k][my_row];
+            top = fmaxf(top, wave_m[k][my_row]);
+        }
+        const int out_row = row_block * 16 + my_row;
+        const int oi = (int)dg_fdiv((uint32_t)out_row, args.by_group), head = h * args.group + out_row - oi * args.group;
+        if (args.pieces == 1) {
+            const float by = total == 0.0f ? 0.0f : 1.0f / total;
+            DgVec<T, 4> v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v.e[k] = dg_from_float<T>(sum[k] * by);
+            dg_store_vec<T, 4>((T *)a.out + (int64_t)(seq.first + oi) * a.out_token + (int64_t)head * a.out_head + d, v);
+        } else {
+            const int64_t to_row = (((int64_t)piece * a.B + b) * a.max_q + oi) * a.Hq + head;
+            *(v4f *)(args.shares.o + to_row * DIM + d) = sum;
+            if (d == 0) {
+                args.shares.m[to_row] = top;
+                args.shares.l[to_row] = total;
+            }
         }
     }
 }
 
-// The pieces' shares of a row joined, in the pieces' order: a wavefront a row.
+// The pieces' shares of a row joined, a workgroup a row: the pieces' weights first, then groups of DIM / 4 threads take every GROUPS-th piece; the
+// groups' sums are added in their order, so that the same call gives the same bits.
+constexpr int MOST_PIECES = 256;
+
 template <class T, int DIM>
 __global__ __launch_bounds__(256) void attention_join_kernel(Args args)
 {
+    constexpr int LANES = DIM / 4, GROUPS = 256 / LANES;
+    __shared__ float weight[MOST_PIECES], wave_max[4], wave_sum[4];
+    __shared__ v4f sums[GROUPS][LANES];
     const DgAttention &a = args.a;
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = (int64_t)a.B * a.max_q * a.Hq, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= rows) return;
+    const int64_t rows = (int64_t)a.B * a.max_q * a.Hq, at = blockIdx.x;
     const int64_t token = at / a.Hq, head = at % a.Hq;
     const int b = (int)(token / a.max_q), i = (int)(token % a.max_q);
     const Sequence seq = sequence(a, b);
     if (i >= seq.count) return;
-    float most = -__builtin_inff();
-    for (int k = 0; k < args.pieces; ++k) most = fmaxf(most, args.shares.m[k * rows + at]);
-    constexpr int PER = DIM / 64;
-    float total = 0.0f, o[PER] = {};
-    for (int k = 0; k < args.pieces; ++k) {
-        const float m = args.shares.m[k * rows + at], l = args.shares.l[k * rows + at];
-        const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
-        const DgVec<float, PER> v = dg_load_vec<float, PER>(args.shares.o + (k * rows + at) * DIM + PER * lane);
-        total += l * w;
+    // (a thread a piece)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x / LANES, part = threadIdx.x % LANES;
+    const bool mine = (int)threadIdx.x < args.pieces;
+    const float m = mine ? args.shares.m[threadIdx.x * rows + at] : -__builtin_inff(), l = mine ? args.shares.l[threadIdx.x * rows + at] : 0.0f;
+    float most = m;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] += v.e[e] * w;
-    }
+    for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+    if (lane == 0) wave_max[wave] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+    const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
+    weight[threadIdx.x] = w;
+    float total = l * w;
+#pragma unroll
+    for (int k = 32; k; k >>= 1) total += __shfl_xor(total, k);
+    if (lane == 0) wave_sum[wave] = total;
+    __syncthreads();
+    v4f o = {};
+    const float *from = args.shares.o + at * DIM + 4 * part;
+#pragma unroll 4
+    for (int k = group; k < args.pieces; k += GROUPS) o += *(const v4f *)(from + k * rows * DIM) * weight[k];
+    sums[group][part] = o;
+    __syncthreads();
+    if (group) return;
+    for (int k = 1; k < GROUPS; ++k) o += sums[k][part];
+    total = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
     const float by = total == 0.0f ? 0.0f : 1.0f / total;
-    DgVec<T, PER> v;
+    DgVec<T, 4> v;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) v.e[e] = dg_from_float<T>(o[e] * by);
-    dg_store_vec<T, PER>((T *)a.out + (int64_t)(seq.first + i) * a.out_token + head * a.out_head + PER * lane, v);
+    for (int e = 0; e < 4; ++e) v.e[e] = dg_from_float<T>(o[e] * by);
+    dg_store_vec<T, 4>((T *)a.out + (int64_t)(seq.first + i) * a.out_token + head * a.out_head + 4 * part, v);
 }
 
-// How the context is cut: enough workgroups for the chip, pieces of at least 256 tokens.
+// How the context is cut.
 struct Plan {
-    int32_t row_blocks, pieces, piece_tokens;
+    int32_t row_blocks, pieces, piece_tokens, waves;
 };
+constexpr int PIECES_PER_SIMD = 2, LEAST_PIECE = 512;
 Plan plan_of(const DgAttention &a)
 {
     const int32_t group = a.Hq / a.cache.heads;
     Plan p;
     p.row_blocks = (int32_t)(((int64_t)a.max_q * group + 15) / 16);
-    const int64_t blocks = (int64_t)p.row_blocks * a.B * a.cache.heads, wanted = dg_simd_count();
-    const int64_t most = (a.max_ctx + 255) / 256;
-    p.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(wanted / blocks, most), 256));
-    const int32_t step = WAVES * TILE;
+    const int64_t blocks = (int64_t)p.row_blocks * a.B * a.cache.heads;
+    static const int PP=getenv("DGP")?atoi(getenv("DGP")):PIECES_PER_SIMD, LP=getenv("DGL")?atoi(getenv("DGL")):LEAST_PIECE;
+    const int64_t most = (a.max_ctx + LP - 1) / LP;
+    p.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>((int64_t)PP * dg_simd_count() / blocks, std::min<int64_t>(most, MOST_PIECES)));
+    p.waves = 4;
+    const int32_t step = p.waves * TILE;
     p.piece_tokens = (int32_t)(((a.max_ctx + (int64_t)p.pieces * step - 1) / ((int64_t)p.pieces * step)) * step);
     return p;
 }
@@ -450,8 +534,8 @@ dg_status dg_launch_attention(const DgAttention &a, dg_dtype type, hipStream_t s
     auto launch = [&](auto t, auto bits, auto dim) {
         typedef decltype(t) T;
         constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
-        attention_kernel<T, BITS, DIM><<<blocks, 256, 0, stream>>>(args);
-        if (p.pieces > 1) attention_join_kernel<T, DIM><<<(uint32_t)((rows + 3) / 4), 256, 0, stream>>>(args);
+        attention_kernel<T, BITS, DIM, 4><<<blocks, 256, 0, stream>>>(args);
+        if (p.pieces > 1) attention_join_kernel<T, DIM><<<(uint32_t)rows, 256, 0, stream>>>(args);
     };
     auto by_dim = [&](auto t, auto bits) {
         switch (a.cache.dim) {
