@@ -5,7 +5,7 @@
 // one row in the order in which the second product, O^T = V^T P^T, takes its operand, so that the weights never leave the lane.  Keys and
 // values lie in the cache as the two products' first operands: 16 contiguous bytes a lane, neighbouring lanes side by side.
 //
-// Numbers: codes become binary16 exactly (8 bits: code - 128; 4 bits: code - 8, the 8 s joining z).  A query row is scaled by a power of
+// Numbers: codes become binary16 exactly.  A query row is scaled by a power of
 // two to a largest magnitude in [2^13, 2^14), so that bfloat16's range fits binary16 and nothing above 2^-28 of the row's largest loses a
 // bit.  Scores, maxima, sums and outputs are binary32.  A weight is rounded once, to binary16, as p * (value scale / R) * 2^10, where R is
 // a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  The maximum is
@@ -29,23 +29,35 @@ constexpr float WEIGHT_UNIT = 1024.0f, RAISE = 4.0f;
 
 __device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
 
-// Four 8-bit codes in storage order -> code - 128 as binary16: a byte below 0x64 is 1024 + byte.
+// Codes become binary16 below the bits of a power of two, without their bias taken off: that is done on the matrix pipe, which has time to spare
+// where the vector pipe has none (32 packed additions a tile against 8 matrix instructions).  Scores start from minus the bias times the sum of the
+// query; outputs get minus the bias times the tile's weights by a product of its own, so that what cancels are sums over one tile, and what that rounds
+// off is 2^-24 of these.
+
+// Four 8-bit codes in storage order: 1024 + byte, in pairs of neighbours.
+constexpr float BIAS8 = 1024.0f + 128.0f;
 __device__ __forceinline__ void halves8(uint32_t w, v2h &a, v2h &b)
 {
-    const v2h bias = {(_Float16)1152.0f, (_Float16)1152.0f};
-    a = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00050004u)) - bias;
-    b = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00070006u)) - bias;
+    a = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00050004u));
+    b = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00070006u));
 }
-// Eight 4-bit codes, in nibbles 0 ... 7 -> code - 8 as binary16, in pairs of nibbles (0, 4), (1, 5), (2, 6), (3, 7): a nibble at bit 0 below
-// 0x6400 is 1024 + code, at bit 4 below 0x5400 64 + code.
+// Eight 4-bit codes, nibbles 0 ... 7, in pairs of nibbles (0, 4), (1, 5), (2, 6), (3, 7).  Values: 1024 + code in the even pairs, 64 + code in the odd
+// ones, which are other channels; they count as code - 8, the 8 s joining z.  Keys: 64 + code throughout.
+constexpr float BIAS4_EVEN = 1024.0f + 8.0f, BIAS4_ODD = 64.0f + 8.0f, BIAS4_KEYS = 64.0f;
 __device__ __forceinline__ void halves4(uint32_t w, v2h (&o)[4])
 {
-    const v2h b0 = {(_Float16)1032.0f, (_Float16)1032.0f}, b1 = {(_Float16)72.0f, (_Float16)72.0f};
     const uint32_t x = w >> 8;
-    o[0] = as_halves((w & 0x000F000Fu) | 0x64006400u) - b0;
-    o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u) - b1;
-    o[2] = as_halves((x & 0x000F000Fu) | 0x64006400u) - b0;
-    o[3] = as_halves((x & 0x00F000F0u) | 0x54005400u) - b1;
+    o[0] = as_halves((w & 0x000F000Fu) | 0x64006400u);
+    o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u);
+    o[2] = as_halves((x & 0x000F000Fu) | 0x64006400u);
+    o[3] = as_halves((x & 0x00F000F0u) | 0x54005400u);
+}
+__device__ __forceinline__ void halves4_keys(uint32_t w, v2h *o)
+{
+    o[0] = as_halves((w << 4 & 0x00F000F0u) | 0x54005400u);
+    o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u);
+    o[2] = as_halves((w >> 4 & 0x00F000F0u) | 0x54005400u);
+    o[3] = as_halves((w >> 8 & 0x00F000F0u) | 0x54005400u);
 }
 __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d)
 {
@@ -99,9 +111,10 @@ struct Sequence {
 // (b is the same in every lane of a wavefront)
 __device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
 {
-    const auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    typedef const __attribute__((address_space(4))) int32_t *Scalars;
+    b = __builtin_amdgcn_readfirstlane(b);
     Sequence s;
-    const int start = scalar(a.q_start[b]), stop = scalar(a.q_start[b + 1]), ctx = scalar(a.ctx_len[b]);
+    const int start = ((Scalars)a.q_start)[b], stop = ((Scalars)a.q_start)[b + 1], ctx = ((Scalars)a.ctx_len)[b];
     s.first = min(max(start, 0), a.T);
     s.count = min(max(stop, s.first), a.T) - s.first;
     s.ctx = (int32_t)min((int64_t)max(ctx, 0), (int64_t)a.table_width * a.cache.page_size);
@@ -143,10 +156,11 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
     const int i = (int)dg_fdiv((uint32_t)row, args.by_group), j = row - i * args.group;     // new token, head of the group
     const bool there = r < have;
     const int first_i = (int)dg_fdiv((uint32_t)row_block * 16, args.by_group), last_i = (int)dg_fdiv((uint32_t)(row_block * 16 + have - 1), args.by_group);
-    // tokens that the row sees: those before `end`; any row of the block: before `block_end`; every one of 16: before `all_end`
-    const int end = !there ? 0 : a.causal ? max(seq.past + i + 1, 0) : seq.ctx;
+    // tokens that the row sees: those before `end`; any row of the block: before `block_end`; every row: before `all_end` (rows that are not there
+    // are computed as the block's first)
     const int block_end = a.causal ? max(seq.past + last_i + 1, 0) : seq.ctx;
-    const int all_end = have < 16 ? 0 : a.causal ? max(seq.past + first_i + 1, 0) : seq.ctx;
+    const int all_end = a.causal ? max(seq.past + first_i + 1, 0) : seq.ctx;
+    const int end = a.causal && there ? max(seq.past + i + 1, 0) : all_end;
     const int from = piece * args.piece_tokens;
     const int to = piece == args.pieces - 1 ? block_end : min(block_end, from + args.piece_tokens);
 
@@ -208,7 +222,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
     float f, q_sum = 0.0f;
     {
         float x[STEPS][8], most = 0.0f;
-        const T *src = (const T *)a.q + (int64_t)(seq.first + (there ? i : 0)) * a.q_token + (int64_t)(h * args.group + (there ? j : 0)) * a.q_head;
+        const T *src = (const T *)a.q + (int64_t)(seq.first + (there ? i : first_i)) * a.q_token + (int64_t)(h * args.group + (there ? j : 0)) * a.q_head;
         bool finite = true;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
@@ -229,15 +243,16 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             q[s] = query_operand<BITS>(x[s], up);
-            if (BITS == 4)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q_sum += (float)q[s][e];
+            for (int e = 0; e < 8; ++e) q_sum += (float)q[s][e];
         }
-        if (BITS == 4) q_sum = row_sum(q_sum);
+        q_sum = row_sum(q_sum);
     }
+    const float from_bias = -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum, f_sum = f * q_sum;
 
     v4f o[BLOCKS] = {};
-    float m = -__builtin_inff(), shift = 0.0f, l = 0.0f, oz = 0.0f, R = 0.0f, per_R = 0.0f;
+    // sums are relative to 2^shift; a row's begin when it sees its first token, and `above` is what a score has to pass for the shift to be raised
+    float shift = 0.0f, above = -__builtin_inff(), l = 0.0f, oz = 0.0f, R = 0.0f, per_R = 0.0f;
 #pragma unroll 1
     for (; t0 < to; t0 += STRIDE) {
         if (t0 + (DEPTH - 1) * STRIDE < to) dg_wait_for_loads<(DEPTH - 1) * Kept::LOADS>();
@@ -257,7 +272,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
                 kz[u] = numbers[16];
                 vz[u] = numbers[20];
             }
-            v4f acc = {};
+            v4f acc = {from_bias, from_bias, from_bias, from_bias};
 #pragma unroll
             for (int s = 0; s < STEPS / 2; ++s) {
                 const uint8_t *keys = tile + u * (Kept::PART / 2) + s * (128 * BITS);
@@ -268,9 +283,8 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
                     for (int e = 0; e < 4; ++e) halves8(w[e], c[2 * e], c[2 * e + 1]);
                 } else {
                     const v2u w = *(const v2u *)(keys + 8 * lane);
-                    v2h (&low)[4] = *(v2h(*)[4])c, (&high)[4] = *(v2h(*)[4])(c + 4);
-                    halves4(w[0], low);
-                    halves4(w[1], high);
+                    halves4_keys(w[0], c);
+                    halves4_keys(w[1], c + 4);
                 }
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[0], c[1], c[2], c[3]), q[2 * s], acc, 0, 0, 0);
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(join(c[4], c[5], c[6], c[7]), q[2 * s + 1], acc, 0, 0, 0);
@@ -282,22 +296,24 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float x = score[u][e] * ks[u][e];
-                if (BITS == 4) x = __builtin_fmaf(q_sum, __builtin_fmaf(8.0f, ks[u][e], kz[u][e]), x);
-                x *= f;
-                const int t = t0 + 16 * u + 4 * g + e;
-                if (!all_seen) x = t < unit_end[u] ? x : -__builtin_inff();
+                // (relative to the maximum that the sums go by)
+                float x = BITS == 8 ? __builtin_fmaf(score[u][e], ks[u][e] * f, -shift)
+                                    : __builtin_fmaf(score[u][e] * f, ks[u][e], __builtin_fmaf(f_sum, kz[u][e], -shift));
+                if (!all_seen) x = t0 + 16 * u + 4 * g + e < unit_end[u] ? x : -__builtin_inff();
                 top = fmaxf(top, x);
                 score[u][e] = x;
             }
-        if (__any(top > m + RAISE)) {
-            const float higher = fmaxf(m, row_max(top));
-            const float next_shift = higher == -__builtin_inff() ? 0.0f : higher;
-            const float keep = exp2_(m - next_shift);
-            m = higher;
-            shift = next_shift;
+        if (__any(top > above)) {
+            top = row_max(top);
+            const bool begun = above == RAISE;
+            const float by = begun ? fmaxf(top, 0.0f) : top == -__builtin_inff() ? 0.0f : top;
+            const float keep = begun ? exp2_(-by) : 0.0f;                          // (nothing is summed before)
+            shift += by;
+            above = begun || top > -__builtin_inff() ? RAISE : above;
             l *= keep;
             oz *= keep;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) score[u] -= by;
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[k] *= keep;
         }
@@ -325,12 +341,12 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
         }
         // The weights as the second product's operand.  Binary16 outputs show a weight's rounding beside their own (the error against 64 bits was 1.4
         // times a binary32 computation's): there what the rounding left off goes through the matrix instructions as well.
-        _Float16 w[8], rest[8];
+        _Float16 w[8], rest[8] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp2_(score[u][e] - shift);
+                const float p = exp2_(score[u][e]);
                 l += p;
                 if (BITS == 4) oz = __builtin_fmaf(p, __builtin_fmaf(8.0f, vs[u][e], vz[u][e]), oz);
                 const float x = p * (vs[u][e] * per_R);
@@ -339,10 +355,16 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
                 if (TWICE) rest[at] = (_Float16)(x - (float)w[at]);
             }
         const v8h weights = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
-        const auto add = [&](v4f &acc, v8h values) {
+        const v8h rests = {rest[0], rest[1], rest[2], rest[3], rest[4], rest[5], rest[6], rest[7]};
+        const auto add = [&](v4f &acc, v8h values, float bias) {
+            const _Float16 x = (_Float16)-bias;
+            const v8h off = {x, x, x, x, x, x, x, x};
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, weights, acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, weights, acc, 0, 0, 0);
-            if (TWICE)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, (v8h){rest[0], rest[1], rest[2], rest[3], rest[4], rest[5], rest[6], rest[7]}, acc, 0, 0, 0);
+            if (TWICE) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, rests, acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, rests, acc, 0, 0, 0);
+            }
         };
         uint32_t words[2][VALUE_WORDS];
 #pragma unroll
@@ -367,13 +389,13 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
                 v2h c[4];
                 halves8(words[0][k], c[0], c[1]);
                 halves8(words[1][k], c[2], c[3]);
-                add(o[k], join(c[0], c[1], c[2], c[3]));
+                add(o[k], join(c[0], c[1], c[2], c[3]), BIAS8);
             } else {
                 v2h c[4], d[4];      // (tokens 0 and 2, 1 and 3; even and odd channels)
                 halves4(words[0][k], c);
                 halves4(words[1][k], d);
-                add(o[2 * k], join(c[0], c[2], d[0], d[2]));
-                add(o[2 * k + 1], join(c[1], c[3], d[1], d[3]));
+                add(o[2 * k], join(c[0], c[2], d[0], d[2]), BIAS4_EVEN);
+                add(o[2 * k + 1], join(c[1], c[3], d[1], d[3]), BIAS4_ODD);
             }
         }
         // the tile has been read: its place is the next one's
@@ -393,6 +415,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
     __shared__ float wave_m[WAVES][16], wave_l[WAVES][16];
     l = row_sum(l);
     oz = row_sum(oz);
+    const float m = above == RAISE ? shift : -__builtin_inff();
     if (g == 0) wave_m[wave][r] = m;
     __syncthreads();
     float most = wave_m[0][r];
