@@ -126,18 +126,18 @@ __device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
 constexpr int TILE = 32;      // tokens per step of a wavefront
 
 // A tile -- two units of 16 tokens -- as a wavefront keeps it in LDS: keys, values, and 64 numbers (unit 0's key and value scales, unit 1's), with 4
-// bits 64 more (z).  A wavefront has DEPTH tiles of its own on the way, by loads that write LDS: HBM answers after one or two microseconds, and
-// registers hold half a tile at most beside the sums (loads into registers, issued as soon as the tile before had left them: 131071 tokens of 8 bits
-// 63 us, 64 contexts of up to 8192 of 4 bits 162).
+// bits 64 more (z).  A wavefront has DEPTH tiles of its own on the way, by loads that write LDS, so that they take no registers: what hides HBM's one or
+// two microseconds is wavefronts, four to a SIMD at 128 registers and 40 KB a workgroup (64 contexts of up to 8192, 4 bits: two wavefronts with three
+// tiles each 131 us, four with two 100; 131071 tokens, 8 bits: two with two 74, four with one 64).
 template <int BITS, int DIM>
 struct Tile {
     static constexpr int PART = 4 * DIM * BITS, NUMBERS = BITS == 8 ? 256 : 512, BYTES = 2 * PART + NUMBERS;
     static constexpr int LOADS = 2 * PART / 1024 + NUMBERS / 256;
-    static constexpr int DEPTH = DIM == 256 ? 2 : BITS == 8 ? (DIM == 128 ? 2 : 3) : 3;
+    static constexpr int DEPTH = 4 * 2 * BYTES <= 40960 ? 2 : 1, WAVES_PER_SIMD = DIM == 256 ? 1 : 4;
 };
 
 template <class T, int BITS, int DIM, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attention_kernel(Args args)
+__global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void attention_kernel(Args args)
 {
     constexpr int STEPS = DIM / 32;                       // products of 32 channels
     constexpr int BLOCKS = DIM / 16;                      // accumulators of 16 channels
