@@ -11,35 +11,56 @@ struct WriteArgs {
     int64_t T;
 };
 
-// Four consecutive tokens of a head make a group: a wavefront quantises it, 16 lanes a token (DIM / 16 channels each), for the keys and then for the values.
-// Neighbouring lanes read neighbouring bytes.  A lane's keys are whole words of the cache.  A value's word in the cache is four tokens' bytes of one
-// channel: where the group's slots are four in a row from a multiple of four, as a chunk of a prompt has them, the wavefront turns its 4 x DIM bytes over
-// in LDS and stores words, side by side; a token by itself stores bytes.  (A lane a byte of two channels, one token a wavefront: 65536 tokens of 8 heads
-// written and read back 596 us.)
-// What a lane's PER channels of one token become: BYTES bytes, in 32-bit words, and the numbers.
-template <class T, int BITS, int PER>
-__device__ __forceinline__ void quantize_vector(const DgVec<T, PER> &x, uint32_t (&words)[(PER * BITS + 31) / 32], float &s, float &z)
+// A wavefront takes 64 / LANES consecutive tokens of a head, LANES lanes each: neighbouring lanes read neighbouring bytes.  A lane's keys are whole pieces
+// of the cache, or halves.  A value's word in the cache is four tokens' bytes of one channel: where four tokens' slots follow one another from a
+// multiple of four, the lanes of these four turn their 4 x DIM codes over by way of LDS and store words, side by side; other tokens store bytes.  So that a chunk
+// of a prompt, which begins anywhere in a page, is mostly such fours, a wavefront leaves its last tokens to the next one if they share a word with that
+// one's first (first_token).
+// Eight lanes a token where there are many; sixteen, for wavefronts with less to do one after another, where there are few.
+template <int BITS, int DIM, int LANES>
+struct Form {
+    static constexpr int TOKENS = 64 / LANES, FOUR = 4 * LANES;          // lanes of four tokens
+    static constexpr int PER = DIM / LANES;                              // channels of a lane
+    static constexpr int STEP = DIM * BITS / 8;                          // bytes of a token
+    static constexpr int BYTES = STEP / LANES, WORDS = (BYTES + 3) / 4;  // of a lane
+    static constexpr int PIECE = (PER < 16 ? PER : 16) * BITS / 8;       // of a lane's keys that lie side by side
+    static constexpr int MINE = STEP < FOUR ? 1 : STEP / FOUR;           // words of values that a lane stores, or reads, of four tokens
+};
+
+template <int CONTROL>
+__device__ __forceinline__ float other_lane(float v)
 {
-    float lo = __builtin_inff(), hi = -__builtin_inff();
-    bool finite = true;
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xF, 0xF, false));
+}
+// f over the lanes of a token, the same in each
+template <int LANES, class F>
+__device__ __forceinline__ float over_token(float v, F f)
+{
+    if (LANES == 16) v = f(v, other_lane<0x140>(v));        // row_mirror
+    v = f(v, other_lane<0xB1>(v));          // quad_perm 1, 0, 3, 2
+    v = f(v, other_lane<0x4E>(v));          // quad_perm 2, 3, 0, 1
+    return f(v, other_lane<0x141>(v));      // row_half_mirror
+}
+
+// A lane's channels of one token as codes, and the token's numbers.
+template <class T, int BITS, int DIM, int LANES>
+__device__ __forceinline__ void quantize_lane(const DgVec<T, DIM / LANES> &x, uint32_t (&words)[Form<BITS, DIM, LANES>::WORDS], float &s, float &z)
+{
+    constexpr int PER = DIM / LANES;
+    const auto most = [](float a, float b) { return fmaxf(a, b); };
+    float lo = __builtin_inff(), hi = BITS == 8 ? 0.0f : -__builtin_inff(), bad = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const float f = dg_to_float(x.e[i]);
-        lo = fminf(lo, f);
-        hi = fmaxf(hi, f);
-        finite = finite && fabsf(f) < __builtin_inff();
+        if (BITS == 8) hi = fmaxf(hi, fabsf(f));
+        else hi = fmaxf(hi, f), lo = fminf(lo, f);
+        bad = __builtin_fmaf(f, 0.0f, bad);                   // (a NaN once there was an infinity or a NaN)
     }
-    // (an infinity where a value was none: a NaN compares false)
-    lo = finite ? lo : -__builtin_inff();
-#pragma unroll
-    for (int i = 8; i; i >>= 1) {
-        lo = fminf(lo, __shfl_xor(lo, i));
-        hi = fmaxf(hi, __shfl_xor(hi, i));
-    }
-    const bool all = lo > -__builtin_inff();
-    z = lo;
+    bad = bad == 0.0f ? 0.0f : 1.0f;
+    hi = over_token<LANES>(hi, most);
+    bad = over_token<LANES>(bad, most);
     if constexpr (BITS == 8) {
-        s = all ? fmaxf(fabsf(lo), fabsf(hi)) / 127.0f : __builtin_nanf("");
+        s = bad == 0.0f ? hi / 127.0f : __builtin_nanf("");
         const DgDivisor by = dg_divisor(s);
 #pragma unroll
         for (int i = 0; i < PER; i += 4) {
@@ -48,72 +69,137 @@ __device__ __forceinline__ void quantize_vector(const DgVec<T, PER> &x, uint32_t
             for (int k = 0; k < 4; ++k) code[k] = dg_code8(dg_to_float(x.e[i + k]), by);
             words[i / 4] = (dg_bytes(code) & by.keep) ^ 0x80808080u;                 // (plus 128, byte by byte)
         }
+        z = 0.0f;
     } else {
-        s = all ? hi / 15.0f - lo / 15.0f : __builtin_nanf("");
+        lo = over_token<LANES>(lo, [](float a, float b) { return fminf(a, b); });
+        s = bad == 0.0f ? hi / 15.0f - lo / 15.0f : __builtin_nanf("");
+        z = lo;
         const DgDivisor by = dg_divisor(s);
-        words[0] = 0;
-        if constexpr (PER == 16) words[1] = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) words[i / 8] |= (uint32_t)(dg_code4(dg_to_float(x.e[i]), lo, by) & by.keep) << (4 * (i & 7));
+        for (int i = 0; i < PER; i += 8) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int k = 0; k < (PER < 8 ? PER : 8); ++k) w |= (uint32_t)dg_code4(dg_to_float(x.e[i + k]), lo, by) << (4 * k);
+            words[i / 8] = w & by.keep;
+        }
     }
 }
 
-template <class T, int BITS, int DIM>
+// Four rows of MINE bytes <-> MINE words of one byte of each row.
+template <int MINE>
+__device__ __forceinline__ void turn(const uint32_t *in, uint32_t *out)
+{
+    if constexpr (MINE >= 4) {
+#pragma unroll
+        for (int k = 0; k < MINE / 4; ++k) {
+            // (in: word k of rows 0 ... 3 at stride MINE / 4; out: four words)
+            const uint32_t a = in[k], b = in[k + MINE / 4], c = in[k + 2 * (MINE / 4)], d = in[k + 3 * (MINE / 4)];
+            const uint32_t ab0 = __builtin_amdgcn_perm(b, a, 0x05010400u), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+            const uint32_t cd0 = __builtin_amdgcn_perm(d, c, 0x05010400u), cd1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+            out[4 * k] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+            out[4 * k + 1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+            out[4 * k + 2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100u);
+            out[4 * k + 3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < MINE; ++c) {
+            out[c] = 0;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) out[c] |= (in[n] >> (8 * c) & 255u) << (8 * n);
+        }
+    }
+}
+
+// The first token of the wavefront whose tokens begin about token `base`: up to three before it, if these lie in one word of values with it.
+__device__ __forceinline__ int64_t first_token(const int32_t *slots, int64_t T, int64_t base)
+{
+    const auto scalar = (const __attribute__((address_space(4))) int32_t *)slots;
+    if (base >= T) return T;
+    const int32_t slot = scalar[base], in_word = slot & 3;
+    if (base < 3 || slot < 0) return base;
+    const bool a = scalar[base - 1] == slot - 1, b = scalar[base - 2] == slot - 2, c = scalar[base - 3] == slot - 3;
+    const bool together = in_word < 1 || (a && (in_word < 2 || (b && (in_word < 3 || c))));
+    return together ? base - in_word : base;
+}
+
+// Where a lane's token lies, and whether it is one of four in a row of four.
+struct Place {
+    bool given, there, whole;
+    uint32_t t, first_t;               // the token's, and the four's first one's, place in the page
+    int64_t block;                     // the first byte of the page's head
+};
+template <int LANES>
+__device__ __forceinline__ Place place_of(const DgCache &c, const int32_t *slots, int64_t token, int64_t end, int h, int lane)
+{
+    constexpr int FOUR = 4 * LANES;
+    Place p;
+    p.given = token < end;
+    const int32_t slot = p.given ? slots[token] : -1;
+    p.there = slot >= 0 && slot < c.pages * c.page_size;
+    const uint32_t place = p.there ? slot : 0, page = dg_fdiv(place, c.by_page);
+    p.t = place - page * c.page_size;
+    p.block = page * c.page_bytes() + (int64_t)h * c.head;
+    const int32_t first = FOUR == 64 || lane < 32 ? __builtin_amdgcn_readlane(slot, 0) : __builtin_amdgcn_readlane(slot, 32);
+    const uint64_t in_row = __ballot(p.there && slot == first + (lane / LANES) % 4 && (first & 3) == 0);
+    p.whole = FOUR == 64 ? in_row == ~0ull : (uint32_t)(lane < 32 ? in_row : in_row >> 32) == 0xFFFFFFFFu;
+    p.first_t = p.t - (lane / LANES) % 4;
+    return p;
+}
+
+template <class T, int BITS, int DIM, int LANES>
 __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a)
 {
-    constexpr int PER = DIM / 16, BYTES = PER * BITS / 8, WORDS = (BYTES + 3) / 4, STEP = DIM * BITS / 8;      // STEP: bytes of a token
-    __shared__ __align__(16) uint8_t turned[4][4 * STEP];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane & 15;
-    const int64_t at = (int64_t)blockIdx.x * 4 + wave;
-    if (at >= (a.T + 3) / 4 * a.c.heads) return;
-    const int64_t group = at / a.c.heads, token = 4 * group + (lane >> 4);
+    typedef Form<BITS, DIM, LANES> F;
+    __shared__ __align__(16) uint8_t turned[4][F::TOKENS * F::STEP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % LANES, mine = lane % F::FOUR * F::MINE;
+    const int64_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + wave);
+    if (at >= (a.T + F::TOKENS - 1) / F::TOKENS * a.c.heads) return;
+    const int64_t base = at / a.c.heads * F::TOKENS, first = first_token(a.slots, a.T, base), end = first_token(a.slots, a.T, base + F::TOKENS);
     const int h = (int)(at % a.c.heads);
-    const bool given = token < a.T;
-    const int32_t slot = given ? a.slots[token] : -1;
-    const bool there = slot >= 0 && slot < a.c.pages * a.c.page_size;
-    const int64_t from = given ? token : a.T - 1;                                      // (a lane without a token reads the last one)
-    const DgVec<T, PER> k = dg_load_vec<T, PER>((const T *)a.k + from * a.k_token + h * a.k_head + part * PER);
-    const DgVec<T, PER> v = dg_load_vec<T, PER>((const T *)a.v + from * a.v_token + h * a.v_head + part * PER);
-    const uint32_t place = there ? slot : 0, page = dg_fdiv(place, a.c.by_page), t = place - page * a.c.page_size;
-    uint8_t *const block = a.c.base + page * a.c.page_bytes() + (int64_t)h * a.c.head;
-    const int32_t first = __shfl(slot, 0);
-    const bool whole = __all(there && slot == first + (lane >> 4)) && (first & 3) == 0;
-    float *const numbers = (float *)(block + 2 * a.c.part) + t;
-    uint32_t words[WORDS];
+#pragma unroll 1
+    for (int64_t token = first + lane / LANES; token - lane / LANES < end; token += F::TOKENS) {     // (once, but where a run of slots ends)
+    const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
+    const int64_t from = p.given ? token : end - 1;                                    // (a lane without a token reads the last one)
+    const DgVec<T, F::PER> k = dg_load_vec<T, F::PER>((const T *)a.k + from * a.k_token + h * a.k_head + part * F::PER);
+    const DgVec<T, F::PER> v = dg_load_vec<T, F::PER>((const T *)a.v + from * a.v_token + h * a.v_head + part * F::PER);
+    uint8_t *const block = a.c.base + p.block;
+    float *const numbers = (float *)(block + 2 * a.c.part) + p.t;
+    uint32_t words[F::WORDS];
     float s, z;
 
-    quantize_vector<T, BITS, PER>(k, words, s, z);
-    if (there) {
-        __builtin_memcpy(block + dg_key_byte<BITS>(t, part * PER, DIM), words, BYTES);
+    quantize_lane<T, BITS, DIM, LANES>(k, words, s, z);
+    if (p.there) {
+#pragma unroll
+        for (int i = 0; i < F::BYTES / F::PIECE; ++i)
+            __builtin_memcpy(block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), (const uint8_t *)words + i * F::PIECE, F::PIECE);
         if (part == 0) {
             numbers[0] = s;
             if (BITS == 4) numbers[2 * a.c.page_size] = z;
         }
     }
-    quantize_vector<T, BITS, PER>(v, words, s, z);
+    quantize_lane<T, BITS, DIM, LANES>(v, words, s, z);
     uint8_t *const values = block + a.c.part;
-    if (there && part == 0) {
+    if (p.there && part == 0) {
         numbers[a.c.page_size] = s;
         if (BITS == 4) numbers[3 * a.c.page_size] = z;
     }
-    if (whole) {
-        // token n's bytes in LDS, row n; word c of the cache: byte c of the four rows
-        __builtin_memcpy(turned[wave] + (lane >> 4) * STEP + part * BYTES, words, BYTES);
+    if (p.whole) {
+        __builtin_memcpy(turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, words, F::BYTES);
         __builtin_amdgcn_wave_barrier();
-        constexpr int MINE = STEP < 64 ? 1 : STEP / 64;                                // words a lane stores
-        const int mine = min(lane, STEP / MINE - 1) * MINE;
-        uint8_t row[4][MINE];
+        constexpr int ROW = (F::MINE + 3) / 4;                                         // words of a row
+        uint32_t rows[4 * ROW] = {}, out[F::MINE];
+        if (mine < F::STEP) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) __builtin_memcpy(row[n], turned[wave] + n * STEP + mine, MINE);
-        uint32_t out[MINE];
+            for (int n = 0; n < 4; ++n) __builtin_memcpy(rows + n * ROW, turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, F::MINE);
+            turn<F::MINE>(rows, out);
+            __builtin_memcpy(values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, out, 4 * F::MINE);
+        }
+    } else if (p.there) {
 #pragma unroll
-        for (int c = 0; c < MINE; ++c) out[c] = row[0][c] | row[1][c] << 8 | row[2][c] << 16 | (uint32_t)row[3][c] << 24;
-        // (the first token's address: its lanes', the wavefront's first)
-        const uint32_t first_t = __shfl(t, 0);
-        if (STEP >= 64 || lane < STEP) __builtin_memcpy(values + (first_t >> 2) * (4 * STEP) + 4 * mine, out, 4 * MINE);
-    } else if (there) {
-#pragma unroll
-        for (int i = 0; i < BYTES; ++i) values[(t >> 2) * (4 * STEP) + (part * BYTES + i) * 4 + (t & 3)] = (uint8_t)(words[i / 4] >> (8 * (i & 3)));
+        for (int i = 0; i < F::BYTES; ++i) values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] = (uint8_t)(words[i / 4] >> (8 * (i & 3)));
+    }
+    __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -124,64 +210,83 @@ struct ReadArgs {
     int64_t T;
 };
 
-// The same groups the other way round.
-template <class T, int BITS, int DIM>
+// The same the other way round.
+template <class T, int BITS, int DIM, int LANES>
 __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
 {
-    constexpr int PER = DIM / 16, BYTES = PER * BITS / 8, WORDS = (BYTES + 3) / 4, STEP = DIM * BITS / 8;
-    __shared__ __align__(16) uint8_t turned[4][4 * STEP];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane & 15;
-    const int64_t at = (int64_t)blockIdx.x * 4 + wave;
-    if (at >= (a.T + 3) / 4 * a.c.heads) return;
-    const int64_t group = at / a.c.heads, token = 4 * group + (lane >> 4);
+    typedef Form<BITS, DIM, LANES> F;
+    __shared__ __align__(16) uint8_t turned[4][F::TOKENS * F::STEP];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane % LANES, mine = lane % F::FOUR * F::MINE;
+    const int64_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + wave);
+    if (at >= (a.T + F::TOKENS - 1) / F::TOKENS * a.c.heads) return;
+    const int64_t base = at / a.c.heads * F::TOKENS, first = first_token(a.slots, a.T, base), end = first_token(a.slots, a.T, base + F::TOKENS);
     const int h = (int)(at % a.c.heads);
-    const bool given = token < a.T;
-    const int32_t slot = given ? a.slots[token] : -1;
-    const bool there = slot >= 0 && slot < a.c.pages * a.c.page_size;
-    const uint32_t place = there ? slot : 0, page = dg_fdiv(place, a.c.by_page), t = place - page * a.c.page_size;
-    const uint8_t *const block = a.c.base + page * a.c.page_bytes() + (int64_t)h * a.c.head;
-    const int32_t first = __shfl(slot, 0);
-    const bool whole = __all(there && slot == first + (lane >> 4)) && (first & 3) == 0;
-    const float *const numbers = (const float *)(block + 2 * a.c.part) + t;
-    const auto put = [&](void *to, const uint32_t (&words)[WORDS], float s, float z) {
-        DgVec<T, PER> x;
+#pragma unroll 1
+    for (int64_t token = first + lane / LANES; token - lane / LANES < end; token += F::TOKENS) {
+    const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
+    const uint8_t *const block = a.c.base + p.block, *const values = block + a.c.part;
+    const float *const numbers = (const float *)(block + 2 * a.c.part) + p.t;
+    const auto put = [&](void *to, uint32_t (&words)[F::WORDS], float s, float z) {
+        DgVec<T, F::PER> x;
+        s = p.there ? s : 0.0f;
+        z = p.there ? z : 0.0f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint32_t code = words[i * BITS / 32] >> (i * BITS & 31) & (BITS == 8 ? 255 : 15);
-            const float y = BITS == 8 ? (float)((int)code - 128) * s : (float)(int)code * s + z;
-            x.e[i] = dg_from_float<T>(there ? y : 0.0f);
+        for (int i = 0; i < F::WORDS; ++i) words[i] = p.there ? words[i] : BITS == 8 ? 0x80808080u : 0u;
+#pragma unroll
+        for (int i = 0; i < F::PER; ++i) {
+            const float code = (float)(words[i * BITS / 32] >> (i * BITS & 31) & (BITS == 8 ? 255u : 15u));
+            x.e[i] = dg_from_float<T>(BITS == 8 ? (code - 128.0f) * s : code * s + z);
         }
-        if (given) dg_store_vec<T, PER>((T *)to + (token * a.c.heads + h) * DIM + part * PER, x);
+        if (p.given) dg_store_vec<T, F::PER>((T *)to + (token * a.c.heads + h) * DIM + part * F::PER, x);
     };
-    uint32_t words[WORDS] = {};
+    // everything is asked for before anything is waited for
+    uint32_t keys[F::WORDS] = {}, words[F::WORDS] = {}, in[F::MINE] = {};
+    float s[2] = {}, z[2] = {};
     if (a.k) {
-        __builtin_memcpy(words, block + dg_key_byte<BITS>(t, part * PER, DIM), BYTES);
-        put(a.k, words, numbers[0], BITS == 4 ? numbers[2 * a.c.page_size] : 0.0f);
+#pragma unroll
+        for (int i = 0; i < F::BYTES / F::PIECE; ++i)
+            __builtin_memcpy((uint8_t *)keys + i * F::PIECE, block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), F::PIECE);
+        s[0] = numbers[0];
+        if (BITS == 4) z[0] = numbers[2 * a.c.page_size];
     }
-    if (!a.v) return;
-    const uint8_t *const values = block + a.c.part;
-    if (whole) {
-        constexpr int MINE = STEP < 64 ? 1 : STEP / 64;
-        const int mine = min(lane, STEP / MINE - 1) * MINE;
-        uint32_t in[MINE];
-        const uint32_t first_t = __shfl(t, 0);
-        __builtin_memcpy(in, values + (first_t >> 2) * (4 * STEP) + 4 * mine, 4 * MINE);
+    if (a.v) {
+        s[1] = numbers[a.c.page_size];
+        if (BITS == 4) z[1] = numbers[3 * a.c.page_size];
+        if (p.whole) {
+            if (mine < F::STEP) __builtin_memcpy(in, values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, 4 * F::MINE);
+        } else {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            uint8_t row[MINE];
-#pragma unroll
-            for (int c = 0; c < MINE; ++c) row[c] = (uint8_t)(in[c] >> (8 * n));
-            __builtin_memcpy(turned[wave] + n * STEP + mine, row, MINE);
+            for (int i = 0; i < F::BYTES; ++i) words[i / 4] |= (uint32_t)values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] << (8 * (i & 3));
         }
-        __builtin_amdgcn_wave_barrier();
-        __builtin_memcpy(words, turned[wave] + (lane >> 4) * STEP + part * BYTES, BYTES);
-    } else {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) words[i] = 0;
-#pragma unroll
-        for (int i = 0; i < BYTES; ++i) words[i / 4] |= (uint32_t)values[(t >> 2) * (4 * STEP) + (part * BYTES + i) * 4 + (t & 3)] << (8 * (i & 3));
     }
-    put(a.v, words, numbers[a.c.page_size], BITS == 4 ? numbers[3 * a.c.page_size] : 0.0f);
+    if (a.k) put(a.k, keys, s[0], z[0]);
+    if (!a.v) continue;
+    if (p.whole) {
+        constexpr int ROW = (F::MINE + 3) / 4;
+        uint32_t rows[4 * ROW] = {};
+        if constexpr (F::MINE >= 4) {
+#pragma unroll
+            for (int i = 0; i < F::MINE / 4; ++i) {
+                uint32_t four[4];
+                turn<4>(in + 4 * i, four);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) rows[n * ROW + i] = four[n];
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int c = 0; c < F::MINE; ++c) rows[n] |= (in[c] >> (8 * n) & 255u) << (8 * c);
+        }
+        if (mine < F::STEP)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) __builtin_memcpy(turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, rows + n * ROW, F::MINE);
+        __builtin_amdgcn_wave_barrier();
+        __builtin_memcpy(words, turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, F::BYTES);
+    }
+    put(a.v, words, s[1], z[1]);
+    __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // f(element type, bits, channels), the last two as constants
@@ -204,13 +309,17 @@ void with_form(const DgCache &c, dg_dtype type, F f)
 
 }   // namespace
 
+// Whether there are enough tokens for eight lanes each (fewer: sixteen).
+static bool many(int64_t T, int32_t heads) { return T * heads >= 8192; }
+
 dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t T, const int64_t strides[4],
                                 const int32_t *slots, hipStream_t stream)
 {
     const WriteArgs a = {c, k, v, strides[0], strides[1], strides[2], strides[3], slots, T};
-    const uint32_t blocks = (uint32_t)(((T + 3) / 4 * c.heads + 3) / 4);
     with_form(c, type, [&](auto t, auto bits, auto dim) {
-        cache_write_kernel<decltype(t), decltype(bits)::value, decltype(dim)::value><<<blocks, 256, 0, stream>>>(a);
+        constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
+        if (many(T, c.heads)) cache_write_kernel<decltype(t), BITS, DIM, 8><<<(uint32_t)(((T + 7) / 8 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+        else cache_write_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
     });
     return dg_check_launch("dg_cache_write");
 }
@@ -218,9 +327,10 @@ dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, 
 dg_status dg_launch_cache_read(const DgCache &c, const int32_t *slots, int64_t T, void *k, void *v, dg_dtype type, hipStream_t stream)
 {
     const ReadArgs a = {c, k, v, slots, T};
-    const uint32_t blocks = (uint32_t)(((T + 3) / 4 * c.heads + 3) / 4);
     with_form(c, type, [&](auto t, auto bits, auto dim) {
-        cache_read_kernel<decltype(t), decltype(bits)::value, decltype(dim)::value><<<blocks, 256, 0, stream>>>(a);
+        constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
+        if (many(T, c.heads)) cache_read_kernel<decltype(t), BITS, DIM, 8><<<(uint32_t)(((T + 7) / 8 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+        else cache_read_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
     });
     return dg_check_launch("dg_cache_read");
 }

@@ -215,6 +215,31 @@ def test_cache_write_and_read(T, H, D, page, bits, dtype):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("T,H,D,page,dtype", [(1031, 8, 64, 16, "f16"), (2077, 4, 128, 48, "bf16"), (517, 16, 256, 32, "f32"), (150, 3, 128, 16, "bf16")])
+def test_cache_of_runs_of_slots(T, H, D, page, dtype, bits):
+    """Many tokens: runs of following slots of all lengths and beginnings, some slots that are none, in between."""
+    rng = np.random.default_rng(T + bits)
+    pages = T // 3 + 60
+    free, slots = list(rng.permutation(pages)), []
+    while len(slots) < T:
+        at, n = int(rng.integers(0, page)), int(rng.choice([1, 2, 3, 5, 9, 30, page]))
+        mine = int(free.pop()) * page
+        slots += [mine + t for t in range(at, min(page, at + n))]
+        if rng.random() < 0.1:
+            slots += [-1] * int(rng.integers(1, 6))
+    slots = np.array(slots[:T], np.int32)
+    k, v = _kv(T, H, D, T, dtype)
+    want = Cache(pages, page, H, D, bits, fill=0x5A)
+    want.write(slots, k.float().numpy(), v.float().numpy())
+    desc = dg.cache_desc(pages, page, H, D, bits)
+    cache = torch.full((dg.dg_cache_bytes(desc),), 0x5A, dtype=torch.uint8, device="cuda")
+    dg.dg_cache_write(desc, cache, k.cuda(), v.cuda(), on_gpu(slots))
+    assert same(cache.cpu().numpy(), want.bytes)
+    for x, y in zip(dg.dg_cache_read(desc, cache, on_gpu(slots), dtype=TYPES[dtype]), want.read(slots)):
+        assert same(as_f32(x), rounded(y, dtype))
+
+
+@pytest.mark.parametrize("bits", [8, 4])
 def test_cache_skips_slots_that_are_none(bits):
     desc, ref = dg.cache_desc(2, 16, 2, 64, bits), Cache(2, 16, 2, 64, bits)
     k, v = _kv(8, 2, 64, 3, "bf16")
