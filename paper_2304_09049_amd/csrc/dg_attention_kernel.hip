@@ -12,116 +12,10 @@
 // raised only when a score passes it by 2^4, so that p <= 16 and the weights stay below 2^15.
 #include <algorithm>
 #include <cstdlib>
-#include <type_traits>
 
-#include "dg_decoder.h"
-#include "dg_lds_dma.h"
+#include "dg_attention.h"
 
 namespace {
-
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-
-constexpr float WEIGHT_UNIT = 1024.0f, RAISE = 4.0f;
-
-__device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
-
-// Codes become binary16 below the bits of a power of two, without their bias taken off: that is done on the matrix pipe, which has time to spare
-// where the vector pipe has none (32 packed additions a tile against 8 matrix instructions).  Scores start from minus the bias times the sum of the
-// query; outputs get minus the bias times the tile's weights by a product of its own, so that what cancels are sums over one tile, and what that rounds
-// off is 2^-24 of these.
-
-// Four 8-bit codes in storage order: 1024 + byte, in pairs of neighbours.
-constexpr float BIAS8 = 1024.0f + 128.0f;
-__device__ __forceinline__ void halves8(uint32_t w, v2h &a, v2h &b)
-{
-    a = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00050004u));
-    b = as_halves(__builtin_amdgcn_perm(w, 0x64646464u, 0x00070006u));
-}
-// Eight 4-bit codes, nibbles 0 ... 7, in pairs of nibbles (0, 4), (1, 5), (2, 6), (3, 7).  Values: 1024 + code in the even pairs, 64 + code in the odd
-// ones, which are other channels; they count as code - 8, the 8 s joining z.  Keys: 64 + code throughout.
-constexpr float BIAS4_EVEN = 1024.0f + 8.0f, BIAS4_ODD = 64.0f + 8.0f, BIAS4_KEYS = 64.0f;
-__device__ __forceinline__ void halves4(uint32_t w, v2h (&o)[4])
-{
-    const uint32_t x = w >> 8;
-    o[0] = as_halves((w & 0x000F000Fu) | 0x64006400u);
-    o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u);
-    o[2] = as_halves((x & 0x000F000Fu) | 0x64006400u);
-    o[3] = as_halves((x & 0x00F000F0u) | 0x54005400u);
-}
-__device__ __forceinline__ void halves4_keys(uint32_t w, v2h *o)
-{
-    o[0] = as_halves((w << 4 & 0x00F000F0u) | 0x54005400u);
-    o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u);
-    o[2] = as_halves((w >> 4 & 0x00F000F0u) | 0x54005400u);
-    o[3] = as_halves((w >> 8 & 0x00F000F0u) | 0x54005400u);
-}
-__device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d)
-{
-    return (v8h){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-// Eight neighbouring channels of a query row as the product's operand: pairs of neighbours for 8-bit keys, of the first and the last four
-// for 4-bit ones (as halves4 gives them).
-template <int BITS>
-__device__ __forceinline__ v8h query_operand(const float (&x)[8], float up)
-{
-    v8h q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        q[2 * i] = (_Float16)(x[BITS == 8 ? 2 * i : i] * up);
-        q[2 * i + 1] = (_Float16)(x[BITS == 8 ? 2 * i + 1 : i + 4] * up);
-    }
-    return q;
-}
-
-// max / sum over the four lanes that hold a row (l, l ^ 16, l ^ 32, l ^ 48)
-__device__ __forceinline__ float row_max(float v)
-{
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float row_sum(float v)
-{
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
-}
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// A row's share of the work (one workgroup's piece of the context): sums relative to 2^m.
-struct Shares {
-    float *o;         // [piece][sequence][its new token][query head][dim]
-    float *m, *l;     // the same without the last
-};
-
-struct Args {
-    DgAttention a;
-    int32_t group, row_blocks, pieces, piece_tokens;
-    DgFastDiv by_group;
-    Shares shares;
-};
-
-// What a sequence's new tokens are, with everything that lies in device memory held to what the buffers have.
-struct Sequence {
-    int32_t first, count, ctx, past;      // past: the context before its new tokens (negative if these are more than the context)
-};
-// (b is the same in every lane of a wavefront)
-__device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
-{
-    typedef const __attribute__((address_space(4))) int32_t *Scalars;
-    b = __builtin_amdgcn_readfirstlane(b);
-    Sequence s;
-    const int start = ((Scalars)a.q_start)[b], stop = ((Scalars)a.q_start)[b + 1], ctx = ((Scalars)a.ctx_len)[b];
-    s.first = min(max(start, 0), a.T);
-    s.count = min(max(stop, s.first), a.T) - s.first;
-    s.ctx = (int32_t)min((int64_t)max(ctx, 0), (int64_t)a.table_width * a.cache.page_size);
-    s.past = s.ctx - s.count;
-    s.count = min(s.count, a.max_q);
-    return s;
-}
 
 constexpr int TILE = 32;      // tokens per step of a wavefront
 
@@ -219,35 +113,9 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
 
     // the row's query
     v8h q[STEPS];
-    float f, q_sum = 0.0f;
-    {
-        float x[STEPS][8], most = 0.0f;
-        const T *src = (const T *)a.q + (int64_t)(seq.first + (there ? i : first_i)) * a.q_token + (int64_t)(h * args.group + (there ? j : 0)) * a.q_head;
-        bool finite = true;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const DgVec<T, 8> v = dg_load_vec<T, 8>(src + 64 * (s / 2) + 16 * g + 8 * (s & 1));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[s][e] = dg_to_float(v.e[e]);
-                most = fmaxf(most, fabsf(x[s][e]));
-                finite = finite && fabsf(x[s][e]) < __builtin_inff();
-            }
-        }
-        most = row_max(finite ? most : __builtin_inff());
-        // up = 2^(13 - floor(log2 most)), at most 2^126
-        const uint32_t biased = __float_as_uint(most) >> 23;
-        const uint32_t up_bits = min(267u - min(biased, 254u), 253u);
-        const float up = __uint_as_float(up_bits << 23), down = __uint_as_float((254u - up_bits) << 23);
-        f = most < __builtin_inff() ? a.scale * 1.4426950408889634f * down : __builtin_nanf("");
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            q[s] = query_operand<BITS>(x[s], up);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q_sum += (float)q[s][e];
-        }
-        q_sum = row_sum(q_sum);
-    }
+    float f, q_sum;
+    load_query<T, BITS, DIM>((const T *)a.q + (int64_t)(seq.first + (there ? i : first_i)) * a.q_token + (int64_t)(h * args.group + (there ? j : 0)) * a.q_head,
+                             g, a.scale, q, f, q_sum);
     const float from_bias = -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum, f_sum = f * q_sum;
 
     v4f o[BLOCKS] = {};
@@ -331,8 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
         if (__any(most_vs > R)) {
 #pragma unroll
             for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
-            // the next power of two above it, from 2^-100 to 2^126
-            const uint32_t bits = min(max((__float_as_uint(most_vs) >> 23) + 1, 27u), 253u);
+            const uint32_t bits = above_scale(most_vs);
             const float inverse = __uint_as_float((254u - bits) << 23), keep = R * inverse;
             R = __uint_as_float(bits << 23);
             per_R = inverse * WEIGHT_UNIT;
@@ -516,22 +383,23 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args args)
     dg_store_vec<T, 4>((T *)a.out + (int64_t)(seq.first + i) * a.out_token + head * a.out_head + 4 * part, v);
 }
 
-// How the context is cut.
+// How the rows and the context are cut.
 struct Plan {
-    int32_t row_blocks, pieces, piece_tokens, waves;
+    bool chunk;
+    int32_t row_blocks, pieces, piece_tokens;
 };
 constexpr int PIECES_PER_SIMD = 2, LEAST_PIECE = 512;
 Plan plan_of(const DgAttention &a)
 {
-    const int32_t group = a.Hq / a.cache.heads;
+    const int64_t rows = (int64_t)a.max_q * (a.Hq / a.cache.heads);
     Plan p;
-    p.row_blocks = (int32_t)(((int64_t)a.max_q * group + 15) / 16);
+    p.chunk = rows > 16;
+    const int32_t block = p.chunk ? CHUNK_ROWS : 16, step = p.chunk ? CHUNK_STEP : TILE * 4;
+    p.row_blocks = (int32_t)((rows + block - 1) / block);
     const int64_t blocks = (int64_t)p.row_blocks * a.B * a.cache.heads;
-    static const int PP=getenv("DGP")?atoi(getenv("DGP")):PIECES_PER_SIMD, LP=getenv("DGL")?atoi(getenv("DGL")):LEAST_PIECE;
-    const int64_t most = (a.max_ctx + LP - 1) / LP;
-    p.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>((int64_t)PP * dg_simd_count() / blocks, std::min<int64_t>(most, MOST_PIECES)));
-    p.waves = 4;
-    const int32_t step = p.waves * TILE;
+    const int64_t most = std::min<int64_t>((a.max_ctx + LEAST_PIECE - 1) / LEAST_PIECE, MOST_PIECES);
+    const int64_t wanted = p.chunk ? dg_simd_count() / 2 : (int64_t)PIECES_PER_SIMD * dg_simd_count();
+    p.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(wanted / blocks, most));
     p.piece_tokens = (int32_t)(((a.max_ctx + (int64_t)p.pieces * step - 1) / ((int64_t)p.pieces * step)) * step);
     return p;
 }
@@ -553,25 +421,13 @@ dg_status dg_launch_attention(const DgAttention &a, dg_dtype type, hipStream_t s
     args.shares.o = (float *)a.work;
     args.shares.m = args.shares.o + (int64_t)p.pieces * rows * a.cache.dim;
     args.shares.l = args.shares.m + (int64_t)p.pieces * rows;
-    const uint32_t blocks = (uint32_t)((int64_t)p.row_blocks * a.B * a.cache.heads * p.pieces);
-    auto launch = [&](auto t, auto bits, auto dim) {
+    if (p.chunk) dg_launch_attention_chunk(args, type, stream);
+    with_form(a, type, [&](auto t, auto bits, auto dim) {
         typedef decltype(t) T;
         constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
-        attention_kernel<T, BITS, DIM, 4><<<blocks, 256, 0, stream>>>(args);
+        const uint32_t blocks = (uint32_t)((int64_t)p.row_blocks * a.B * a.cache.heads * p.pieces);
+        if (!p.chunk) attention_kernel<T, BITS, DIM, 4><<<blocks, 256, 0, stream>>>(args);
         if (p.pieces > 1) attention_join_kernel<T, DIM><<<(uint32_t)rows, 256, 0, stream>>>(args);
-    };
-    auto by_dim = [&](auto t, auto bits) {
-        switch (a.cache.dim) {
-        case 64: launch(t, bits, std::integral_constant<int, 64>{}); break;
-        case 128: launch(t, bits, std::integral_constant<int, 128>{}); break;
-        default: launch(t, bits, std::integral_constant<int, 256>{}); break;
-        }
-    };
-    auto by_bits = [&](auto t) {
-        if (a.cache.bits == 8) by_dim(t, std::integral_constant<int, 8>{});
-        else by_dim(t, std::integral_constant<int, 4>{});
-    };
-    if (type == DG_F16) by_bits((_Float16){});
-    else by_bits((__bf16){});
+    });
     return dg_check_launch("dg_paged_attention");
 }
