@@ -97,17 +97,18 @@ __device__ __forceinline__ float row_sum(float v)
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
 }
+// In a block that few tiles come to: keeps it a branch of its own, where the compiler would select value by value in every tile.
+__device__ __forceinline__ void branch() { asm volatile(""); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A lane's channels of a query row as STEPS operands; `f` takes a score to the base-2 logit; the sum of the operands' numbers over the row.
-template <class T, int BITS, int DIM>
-__device__ __forceinline__ void load_query(const T *row, int g, float scale, v8h (&q)[DIM / 32], float &f, float &q_sum)
+// A lane's channels of a query row, and the row's largest magnitude (an infinity if it holds an infinity or a NaN).
+template <class T, int DIM>
+__device__ __forceinline__ float load_query(const T *row, int g, float (&x)[DIM / 32][8])
 {
-    constexpr int STEPS = DIM / 32;
-    float x[STEPS][8], most = 0.0f;
+    float most = 0.0f;
     bool finite = true;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
+    for (int s = 0; s < DIM / 32; ++s) {
         const DgVec<T, 8> v = dg_load_vec<T, 8>(row + 64 * (s / 2) + 16 * g + 8 * (s & 1));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -116,20 +117,24 @@ __device__ __forceinline__ void load_query(const T *row, int g, float scale, v8h
             finite = finite && fabsf(x[s][e]) < __builtin_inff();
         }
     }
-    most = row_max(finite ? most : __builtin_inff());
-    // up = 2^(13 - floor(log2 most)), at most 2^126
-    const uint32_t biased = __float_as_uint(most) >> 23;
-    const uint32_t up_bits = min(267u - min(biased, 254u), 253u);
+    return row_max(finite ? most : __builtin_inff());
+}
+// The same as operands, times a power of two that takes `most` (finite) into [2^13, 2^14), at most 2^126; `f` takes a score to the base-2 logit.  The
+// sum of the operands' numbers over the row.
+template <int BITS, int DIM>
+__device__ __forceinline__ float query_operands(const float (&x)[DIM / 32][8], float most, float scale, v8h (&q)[DIM / 32], float &f)
+{
+    const uint32_t up_bits = min(267u - min(__float_as_uint(most) >> 23, 254u), 253u);
     const float up = __uint_as_float(up_bits << 23), down = __uint_as_float((254u - up_bits) << 23);
-    f = most < __builtin_inff() ? scale * 1.4426950408889634f * down : __builtin_nanf("");
-    q_sum = 0.0f;
+    f = scale * 1.4426950408889634f * down;
+    float sum = 0.0f;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
+    for (int s = 0; s < DIM / 32; ++s) {
         q[s] = query_operand<BITS>(x[s], up);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q_sum += (float)q[s][e];
+        for (int e = 0; e < 8; ++e) sum += (float)q[s][e];
     }
-    q_sum = row_sum(q_sum);
+    return row_sum(sum);
 }
 
 // The power of two above a value scale, from 2^-100 to 2^126, by its exponent's bits.

@@ -8,6 +8,17 @@ namespace {
 
 constexpr int WAVES = 4, BLOCKS_Q = CHUNK_ROWS / (16 * WAVES);
 
+// What a lane's eight weights of a tile may add up to before the shift is raised: p <= 16, so that weights stay below 2^14.  A row that has seen nothing
+// raises it whatever they are.
+constexpr float MOST_SUM = 16.0f, NOT_BEGUN = -1.0f;
+
+__device__ __forceinline__ uint32_t two_halves(float a, float b)       // rounded to nearest even
+{
+    uint32_t w;
+    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(a), "v"(b));
+    return w;
+}
+
 // A stage in LDS: four units, each keys, values and 64 numbers (key scale, value scale and, 4 bits, key z and value z of 16 tokens).
 template <int BITS, int DIM>
 struct Stage {
@@ -81,22 +92,32 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
         page = page_of(ahead + 16 * wave);
     }
 
+    // The wavefront's rows are scaled by one power of two, the one for its largest query: a score's factor is then the token's alone.  (A row whose
+    // queries are 2^-10 of another's keeps 18 bits of them, for logits that are as much smaller.)
     v8h q[BLOCKS_Q][STEPS];
-    float f[BLOCKS_Q], f_sum[BLOCKS_Q], from_bias[BLOCKS_Q], shift[BLOCKS_Q], above[BLOCKS_Q], l[BLOCKS_Q], oz[BLOCKS_Q];
+    float f, q_sum[BLOCKS_Q], from_bias[BLOCKS_Q], shift[BLOCKS_Q], above[BLOCKS_Q], l[BLOCKS_Q], oz[BLOCKS_Q];
     int end[BLOCKS_Q];
+    {
+        float x[BLOCKS_Q][STEPS][8], most[BLOCKS_Q], largest = 0.0f;
 #pragma unroll
-    for (int n = 0; n < BLOCKS_Q; ++n) {
-        const int at = 16 * n + r, row = wave_row + at;
-        const bool there = at < mine;
-        const int i = there ? (int)dg_fdiv((uint32_t)row, args.by_group) : 0, j = there ? row - i * args.group : 0;
-        float q_sum;
-        load_query<T, BITS, DIM>((const T *)a.q + (int64_t)(seq.first + i) * a.q_token + (int64_t)(h * args.group + j) * a.q_head, g, a.scale, q[n], f[n], q_sum);
-        f_sum[n] = f[n] * q_sum;
-        from_bias[n] = -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum;
-        end[n] = there && a.causal ? max(seq.past + i + 1, 0) : all_end;
-        shift[n] = 0.0f;
-        above[n] = -__builtin_inff();
-        l[n] = oz[n] = 0.0f;
+        for (int n = 0; n < BLOCKS_Q; ++n) {
+            const int at = 16 * n + r, row = wave_row + at;
+            const bool there = at < mine;
+            const int i = there ? (int)dg_fdiv((uint32_t)row, args.by_group) : 0, j = there ? row - i * args.group : 0;
+            most[n] = load_query<T, DIM>((const T *)a.q + (int64_t)(seq.first + i) * a.q_token + (int64_t)(h * args.group + j) * a.q_head, g, x[n]);
+            largest = fmaxf(largest, there && most[n] < __builtin_inff() ? most[n] : 0.0f);
+            end[n] = there && a.causal ? max(seq.past + i + 1, 0) : all_end;
+            shift[n] = 0.0f;
+            above[n] = NOT_BEGUN;
+            l[n] = oz[n] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 8; k; k >>= 1) largest = fmaxf(largest, __shfl_xor(largest, k));
+#pragma unroll
+        for (int n = 0; n < BLOCKS_Q; ++n) {
+            q_sum[n] = query_operands<BITS, DIM>(x[n], largest, a.scale, q[n], f);
+            from_bias[n] = most[n] < __builtin_inff() ? -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum[n] : __builtin_nanf("");
+        }
     }
     v4f o[BLOCKS_Q][BLOCKS] = {};
     float R = 0.0f, per_R = 0.0f;
@@ -154,52 +175,81 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
                     for (int n = 0; n < BLOCKS_Q; ++n) score[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * s + 1], score[n][u], 0, 0, 0);
                 }
             }
-            float top[BLOCKS_Q];
-            bool raise = false;
+            // Logits, and their exponentials relative to 2^shift.  That these have grown too large is seen from their sum, which is needed anyway.
+            float p[BLOCKS_Q][2][4], sum[BLOCKS_Q];
 #pragma unroll
-            for (int n = 0; n < BLOCKS_Q; ++n) {
-                top[n] = -__builtin_inff();
+            for (int u = 0; u < 2; ++u) {
+                ks[u] *= f;
+                if (BITS == 4) kz[u] *= f;
+            }
+#pragma unroll
+            for (int n = 0; n < BLOCKS_Q; ++n)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        score[n][u][e] = __builtin_fmaf(score[n][u][e], ks[u][e], BITS == 8 ? -shift[n] : __builtin_fmaf(q_sum[n], kz[u][e], -shift[n]));
+            if (!all_seen) {
+                branch();
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float x = BITS == 8 ? __builtin_fmaf(score[n][u][e], ks[u][e] * f[n], -shift[n])
-                                            : __builtin_fmaf(score[n][u][e] * f[n], ks[u][e], __builtin_fmaf(f_sum[n], kz[u][e], -shift[n]));
-                        if (!all_seen) x = t1 + 16 * u + 4 * g + e < end[n] && (u ? is1 : is0) ? x : -__builtin_inff();
-                        top[n] = fmaxf(top[n], x);
-                        score[n][u][e] = x;
+                        const int t = (u ? is1 : is0) ? t1 + 16 * u + 4 * g + e : INT32_MAX;
+#pragma unroll
+                        for (int n = 0; n < BLOCKS_Q; ++n) score[n][u][e] = t < end[n] ? score[n][u][e] : -__builtin_inff();
+                        // (a row that does not see a token that others see: its weight is 0 times this, which may be a NaN; see below)
+                        vs[u][e] = t < wave_end ? vs[u][e] : 0.0f;
+                        if (BITS == 4) vz[u][e] = t < wave_end ? vz[u][e] : 0.0f;
                     }
-                raise = raise || top[n] > above[n];
             }
+#pragma unroll
+            for (int n = 0; n < BLOCKS_Q; ++n)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[n][u][e] = exp2_(score[n][u][e]);
+                        sum[n] = u + e == 0 ? p[n][0][0] : sum[n] + p[n][u][e];
+                    }
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < BLOCKS_Q; ++n) raise = raise || sum[n] > above[n];
             if (__any(raise)) {
 #pragma unroll
                 for (int n = 0; n < BLOCKS_Q; ++n) {
-                    const float high = row_max(top[n]);
-                    const bool begun = above[n] == RAISE;
+                    float high = -__builtin_inff();
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) high = fmaxf(high, score[n][u][e]);
+                    high = row_max(high);
+                    const bool begun = above[n] == MOST_SUM;
                     const float by = begun ? fmaxf(high, 0.0f) : high == -__builtin_inff() ? 0.0f : high;
                     const float keep = begun ? exp2_(-by) : 0.0f;                          // (nothing is summed before)
                     shift[n] += by;
-                    above[n] = begun || high > -__builtin_inff() ? RAISE : above[n];
+                    above[n] = begun || high > -__builtin_inff() ? MOST_SUM : NOT_BEGUN;
                     l[n] *= keep;
                     oz[n] *= keep;
+                    sum[n] = 0.0f;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) score[n][u] -= by;
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            p[n][u][e] = exp2_(score[n][u][e] - by);
+                            sum[n] += p[n][u][e];
+                        }
 #pragma unroll
                     for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
                 }
             }
+#pragma unroll
+            for (int n = 0; n < BLOCKS_Q; ++n) l[n] += sum[n];
             float most_vs = 0.0f;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (!all_seen) {
-                        const bool seen = t1 + 16 * u + 4 * g + e < wave_end && (u ? is1 : is0);
-                        vs[u][e] = seen ? vs[u][e] : 0.0f;
-                        if (BITS == 4) vz[u][e] = seen ? vz[u][e] : 0.0f;
-                    }
-                    most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
-                }
+                for (int e = 0; e < 4; ++e) most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
             if (__any(most_vs > R)) {
 #pragma unroll
                 for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
@@ -213,6 +263,7 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
                     for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
             }
             v8h weights[BLOCKS_Q], rests[TWICE ? BLOCKS_Q : 1];
+            float x[BLOCKS_Q][8], xz[BITS == 4 ? BLOCKS_Q : 1][8];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -221,19 +272,42 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
                     const int at = 4 * u + (BITS == 8 ? e : (e & 1) * 2 + (e >> 1));          // (4 bits: tokens 0, 2, 1, 3)
 #pragma unroll
                     for (int n = 0; n < BLOCKS_Q; ++n) {
-                        const float p = exp2_(score[n][u][e]);
-                        l[n] += p;
-                        float x = p * by, xz = p * z;
-                        if (!all_seen) {                  // (what others of the rows see may be a NaN)
-                            const bool seen = t1 + 16 * u + 4 * g + e < end[n];
-                            x = seen ? x : 0.0f;
-                            xz = seen ? xz : 0.0f;
-                        }
-                        if (BITS == 4) oz[n] += xz;
-                        weights[n][at] = (_Float16)x;
-                        if (TWICE) rests[n][at] = (_Float16)(x - (float)weights[n][at]);
+                        x[n][at] = p[n][u][e] * by;
+                        if (BITS == 4) xz[n][at] = p[n][u][e] * z;
                     }
                 }
+            if (!all_seen) {
+                branch();
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int n = 0; n < BLOCKS_Q; ++n) {
+                            const int at = 4 * u + (BITS == 8 ? e : (e & 1) * 2 + (e >> 1));
+                            const bool seen = t1 + 16 * u + 4 * g + e < end[n];
+                            x[n][at] = seen ? x[n][at] : 0.0f;
+                            if (BITS == 4) xz[n][at] = seen ? xz[n][at] : 0.0f;
+                        }
+            }
+            if (BITS == 4)
+#pragma unroll
+                for (int n = 0; n < BLOCKS_Q; ++n)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) oz[n] += xz[n][k];
+#pragma unroll
+            for (int n = 0; n < BLOCKS_Q; ++n) {
+                v4u w, rest = {};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = two_halves(x[n][2 * k], x[n][2 * k + 1]);
+                weights[n] = __builtin_bit_cast(v8h, w);
+                if (TWICE) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        rest[k] = two_halves(x[n][2 * k] - (float)weights[n][2 * k], x[n][2 * k + 1] - (float)weights[n][2 * k + 1]);
+                    rests[n] = __builtin_bit_cast(v8h, rest);
+                }
+            }
             uint32_t words[2][VALUE_WORDS];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -312,7 +386,7 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
                 else *(v4f *)(args.shares.o + share * DIM + channel) = x;
             }
         if (!alone && g == 0) {
-            args.shares.m[share] = above[n] == RAISE ? shift[n] : -__builtin_inff();
+            args.shares.m[share] = above[n] == MOST_SUM ? shift[n] : -__builtin_inff();
             args.shares.l[share] = total;
         }
     }

@@ -113,9 +113,11 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
 
     // the row's query
     v8h q[STEPS];
-    float f, q_sum;
-    load_query<T, BITS, DIM>((const T *)a.q + (int64_t)(seq.first + (there ? i : first_i)) * a.q_token + (int64_t)(h * args.group + (there ? j : 0)) * a.q_head,
-                             g, a.scale, q, f, q_sum);
+    float f, x[STEPS][8];
+    const float most_q = load_query<T, DIM>((const T *)a.q + (int64_t)(seq.first + (there ? i : first_i)) * a.q_token +
+                                                (int64_t)(h * args.group + (there ? j : 0)) * a.q_head, g, x);
+    const float q_sum = query_operands<BITS, DIM>(x, most_q, a.scale, q, f);
+    if (!(most_q < __builtin_inff())) f = __builtin_nanf("");
     const float from_bias = -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum, f_sum = f * q_sum;
 
     v4f o[BLOCKS] = {};
@@ -167,9 +169,26 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
                 // (relative to the maximum that the sums go by)
                 float x = BITS == 8 ? __builtin_fmaf(score[u][e], ks[u][e] * f, -shift)
                                     : __builtin_fmaf(score[u][e] * f, ks[u][e], __builtin_fmaf(f_sum, kz[u][e], -shift));
-                if (!all_seen) x = t0 + 16 * u + 4 * g + e < unit_end[u] ? x : -__builtin_inff();
-                top = fmaxf(top, x);
                 score[u][e] = x;
+            }
+        if (!all_seen) {
+            branch();
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool seen = t0 + 16 * u + 4 * g + e < unit_end[u];
+                    score[u][e] = seen ? score[u][e] : -__builtin_inff();
+                    vs[u][e] = seen ? vs[u][e] : 0.0f;
+                    if (BITS == 4) vz[u][e] = seen ? vz[u][e] : 0.0f;
+                }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                top = fmaxf(top, score[u][e]);
+                most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
             }
         if (__any(top > above)) {
             top = row_max(top);
@@ -185,17 +204,6 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[k] *= keep;
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (!all_seen) {
-                    const bool seen = t0 + 16 * u + 4 * g + e < unit_end[u];
-                    vs[u][e] = seen ? vs[u][e] : 0.0f;
-                    if (BITS == 4) vz[u][e] = seen ? vz[u][e] : 0.0f;
-                }
-                most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
-            }
         if (__any(most_vs > R)) {
 #pragma unroll
             for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
