@@ -11,7 +11,6 @@
 // a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  The maximum is
 // raised only when a score passes it by 2^4, so that p <= 16 and the weights stay below 2^15.
 #include <algorithm>
-#include <cstdlib>
 
 #include "dg_attention.h"
 
@@ -27,7 +26,7 @@ template <int BITS, int DIM>
 struct Tile {
     static constexpr int PART = 4 * DIM * BITS, NUMBERS = BITS == 8 ? 256 : 512, BYTES = 2 * PART + NUMBERS;
     static constexpr int LOADS = 2 * PART / 1024 + NUMBERS / 256;
-    static constexpr int DEPTH = 4 * 2 * BYTES <= 40960 ? 2 : 1, WAVES_PER_SIMD = DIM == 256 ? 1 : 4;
+    static constexpr int DEPTH = 4 * 2 * BYTES <= 40960 ? 2 : 1, WAVES_PER_SIMD = DIM == 256 ? 1 : DIM == 128 && BITS == 4 ? 3 : 4;
 };
 
 template <class T, int BITS, int DIM, int WAVES>
@@ -40,9 +39,14 @@ __global__ __launch_bounds__(64 * WAVES, (Tile<BITS, DIM>::WAVES_PER_SIMD)) void
     const DgAttention &a = args.a;
     // (a matrix instruction runs whatever the lanes' mask: what it stands under has to be a scalar branch)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int piece = blockIdx.x % args.pieces, rows = blockIdx.x / args.pieces;
-    const int row_block = rows % args.row_blocks, bh = rows / args.row_blocks;
-    const int h = bh % a.cache.heads, b = bh / a.cache.heads;
+    // Heads innermost and pieces outermost: neighbouring workgroups go to different dies (eight), and a context's last pieces, which shorter ones do not
+    // have, are not to be all of one die (64 contexts of up to 8192 in 4 pieces, pieces innermost: 104 us for 81).
+    int rest = blockIdx.x;
+    const int h = rest % a.cache.heads;
+    rest /= a.cache.heads;
+    const int b = rest % a.B;
+    rest /= a.B;
+    const int row_block = rest % args.row_blocks, piece = rest / args.row_blocks;
     const Sequence seq = sequence(a, b);
     const int have = min(seq.count * args.group - row_block * 16, 16);                      // rows of the block that are there
     if (have <= 0) return;
@@ -396,19 +400,21 @@ struct Plan {
     bool chunk;
     int32_t row_blocks, pieces, piece_tokens;
 };
-constexpr int PIECES_PER_SIMD = 2, LEAST_PIECE = 512;
+// One workgroup a SIMD (more: 64 contexts of up to 8192, 4 bits, 92 us with one or two, 107 with eight), pieces of 512 tokens at least; where that leaves
+// compute units without a workgroup, pieces of 256 (one context of 1000 9.7 us for 11.3, of 4096 10.9 for 12.7; four of 8192 23.0 for 19.4).
 Plan plan_of(const DgAttention &a)
 {
-    const int64_t rows = (int64_t)a.max_q * (a.Hq / a.cache.heads);
+    const int64_t rows = (int64_t)a.max_q * (a.Hq / a.cache.heads), simds = dg_simd_count(), units = simds / 4;
     Plan p;
     p.chunk = rows > 16;
     const int32_t block = p.chunk ? CHUNK_ROWS : 16, step = p.chunk ? CHUNK_STEP : TILE * 4;
     p.row_blocks = (int32_t)((rows + block - 1) / block);
     const int64_t blocks = (int64_t)p.row_blocks * a.B * a.cache.heads;
-    const int64_t most = std::min<int64_t>((a.max_ctx + LEAST_PIECE - 1) / LEAST_PIECE, MOST_PIECES);
-    const int64_t wanted = p.chunk ? dg_simd_count() / 2 : (int64_t)PIECES_PER_SIMD * dg_simd_count();
-    p.pieces = (int32_t)std::max<int64_t>(1, std::min<int64_t>(wanted / blocks, most));
-    p.piece_tokens = (int32_t)(((a.max_ctx + (int64_t)p.pieces * step - 1) / ((int64_t)p.pieces * step)) * step);
+    const auto cut = [&](int64_t most, int64_t least) { return std::max<int64_t>(1, std::min({most / blocks, (a.max_ctx + least - 1) / least, (int64_t)MOST_PIECES})); };
+    int64_t pieces = cut(p.chunk ? 2 * units : simds, 512);
+    if (blocks * pieces < units) pieces = cut(units, 256);
+    p.pieces = (int32_t)pieces;
+    p.piece_tokens = (int32_t)((a.max_ctx + pieces * step - 1) / (pieces * step) * step);
     return p;
 }
 
