@@ -19,7 +19,7 @@ struct DgAttentionArgs {
     DgAttentionShares shares;
 };
 
-// The kernel for chunks (dg_attention_chunk_kernel.hip), CHUNK_ROWS rows a workgroup; `args` with its cut of the context.
+// The kernel for many rows (dg_attention_chunk_kernel.hip), CHUNK_ROWS rows a workgroup; `args` with its cut of the context.
 constexpr int CHUNK_ROWS = 128, CHUNK_STEP = 64;
 void dg_launch_attention_chunk(const DgAttentionArgs &args, dg_dtype type, hipStream_t stream);
 
@@ -33,7 +33,10 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-constexpr float WEIGHT_UNIT = 1024.0f, RAISE = 4.0f;
+constexpr float WEIGHT_UNIT = 1024.0f;
+// What a lane's eight weights of a tile may add up to before the shift is raised: p <= 16, so that weights stay below 2^14.  A row that has seen nothing
+// raises it whatever they are.
+constexpr float MOST_SUM = 16.0f, NOT_BEGUN = -1.0f;
 
 __device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
 
@@ -66,6 +69,12 @@ __device__ __forceinline__ void halves4_keys(uint32_t w, v2h *o)
     o[1] = as_halves((w & 0x00F000F0u) | 0x54005400u);
     o[2] = as_halves((w >> 4 & 0x00F000F0u) | 0x54005400u);
     o[3] = as_halves((w >> 8 & 0x00F000F0u) | 0x54005400u);
+}
+__device__ __forceinline__ uint32_t two_halves(float a, float b)       // rounded to nearest even
+{
+    uint32_t w;
+    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(a), "v"(b));
+    return w;
 }
 __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d)
 {
@@ -158,6 +167,331 @@ __device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
     s.count = min(s.count, a.max_q);
     return s;
 }
+
+// ---- a unit in LDS --------------------------------------------------------------------------------------------------------
+
+// 16 tokens: keys, values, and 64 numbers (key scale, value scale and, with 4 bits, key z and value z, of 16 tokens each).
+template <int BITS, int DIM>
+struct Unit {
+    static constexpr int PART = 2 * DIM * BITS, BYTES = 2 * PART + 256;
+    static constexpr int LOADS = (2 * PART + 1023) / 1024 + 1;
+};
+
+// The wavefront's loads of the unit from token t of a sequence, to LDS byte `lds`.  `heads`: the head's place in page 0.  A page that is none of the
+// cache's (false is returned): the first page is read instead, and its tokens are to count as unseen.
+template <int BITS, int DIM>
+__device__ __forceinline__ bool fetch_unit(const DgCache &c, const uint8_t *heads, int t, int page, uint32_t lds, int lane)
+{
+    constexpr int PART = Unit<BITS, DIM>::PART;
+    const bool is = (uint32_t)page < (uint32_t)c.pages;
+    const uint32_t in_page = is ? (uint32_t)t - dg_fdiv((uint32_t)t, c.by_page) * c.page_size : 0;
+    const uint8_t *const block = heads + (is ? (int64_t)page : 0) * c.page_bytes(), *const keys = block + in_page * (DIM * BITS / 8);
+    if constexpr (PART >= 1024) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int n = 0; n < PART / 1024; ++n) dg_load16_to_lds(keys + which * c.part, 1024 * n + 16 * lane, lds + which * PART + 1024 * n);
+    } else {
+        dg_load16_to_lds(keys, (lane < 32 ? 0 : c.part) + 16 * (lane & 31), lds);
+    }
+    const int number = BITS == 8 ? lane >> 4 & 1 : lane >> 4;
+    dg_load4_to_lds(block + 2 * c.part, 4 * (int)(in_page + number * c.page_size + (lane & 15)), lds + 2 * PART);
+    return is;
+}
+
+// ---- a wavefront's rows: N blocks of 16, a lane's row r = lane % 16 of each, its channels and tokens by g = lane / 16 --------------------------------
+
+template <class T, int BITS, int DIM, int N>
+struct Rows {
+    static constexpr int STEPS = DIM / 32;                    // products of 32 channels
+    static constexpr int BLOCKS = DIM / 16;                   // accumulators of 16 channels
+    static constexpr int WORDS = DIM * BITS / 128;            // words of 4 tokens' values that a lane takes of a unit
+    // Binary16 outputs show a weight's rounding beside their own (the error against 64 bits was 1.4 times a binary32 computation's): there what the rounding
+    // left off goes through the matrix instructions as well.
+    static constexpr bool TWICE = std::is_same<T, _Float16>::value;
+
+    v8h q[N][STEPS];
+    v4f o[N][BLOCKS];                                         // sums of weight * code, times 2^10 / R
+    float f, q_sum[N], from_bias[N];
+    float shift[N], above[N], l[N], oz[N];                    // sums are relative to 2^shift; of weights, and of weight * z
+    float R, per_R;                                           // the power of two that value scales are taken by, and 2^10 over it
+    int end[N];                                               // a row sees the tokens before this
+    int all_end, any_end;                                     // tokens that every row sees, and that any sees
+
+    // Rows first ... first + have - 1 of a sequence's cached head h (rows that are not there are computed as its first one).  The wavefront's rows are scaled
+    // by one power of two, the one for its largest query: a score's factor is then the token's alone.  (A row whose queries are 2^-10 of another's keeps
+    // 18 bits of them, for logits that are as much smaller.)
+    __device__ __forceinline__ void begin(const Args &args, const Sequence &seq, int h, int first, int have, int r, int g)
+    {
+        const DgAttention &a = args.a;
+        const int first_i = (int)dg_fdiv((uint32_t)first, args.by_group), last_i = (int)dg_fdiv((uint32_t)(first + max(have, 1) - 1), args.by_group);
+        all_end = a.causal ? max(seq.past + first_i + 1, 0) : seq.ctx;
+        any_end = have <= 0 ? 0 : a.causal ? max(seq.past + last_i + 1, 0) : seq.ctx;
+        float x[N][STEPS][8], most[N], largest = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int at = 16 * n + r;
+            const bool there = at < have;
+            const int i = there ? (int)dg_fdiv((uint32_t)(first + at), args.by_group) : 0, j = there ? first + at - i * args.group : 0;
+            most[n] = load_query<T, DIM>((const T *)a.q + (int64_t)(seq.first + i) * a.q_token + (int64_t)(h * args.group + j) * a.q_head, g, x[n]);
+            largest = fmaxf(largest, there && most[n] < __builtin_inff() ? most[n] : 0.0f);
+            end[n] = there && a.causal ? max(seq.past + i + 1, 0) : all_end;
+            shift[n] = 0.0f;
+            above[n] = NOT_BEGUN;
+            l[n] = oz[n] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < BLOCKS; ++k) o[n][k] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+        for (int k = 8; k; k >>= 1) largest = fmaxf(largest, __shfl_xor(largest, k));
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            q_sum[n] = query_operands<BITS, DIM>(x[n], largest, a.scale, q[n], f);
+            from_bias[n] = most[n] < __builtin_inff() ? -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum[n] : __builtin_nanf("");
+        }
+        R = per_R = 0.0f;
+    }
+
+    // The 32 tokens from t0 on, two units one after another in LDS; is0, is1: whether their pages are the cache's.
+    __device__ __forceinline__ void step(const uint8_t *pair, int t0, bool is0, bool is1, int lane)
+    {
+        typedef Unit<BITS, DIM> U;
+        const int r = lane & 15, g = lane >> 4;
+        const bool all_seen = t0 + 32 <= all_end && is0 && is1;
+        v4f score[N][2], ks[2], vs[2], kz[2], vz[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint8_t *const unit = pair + u * U::BYTES;
+            const v4f *const numbers = (const v4f *)(unit + 2 * U::PART) + g;
+            ks[u] = numbers[0];
+            vs[u] = numbers[4];
+            if (BITS == 4) {
+                kz[u] = numbers[8];
+                vz[u] = numbers[12];
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) score[n][u] = (v4f){from_bias[n], from_bias[n], from_bias[n], from_bias[n]};
+#pragma unroll
+            for (int s = 0; s < STEPS / 2; ++s) {
+                v2h c[8];
+                if constexpr (BITS == 8) {
+                    const v4u w = *(const v4u *)(unit + 1024 * s + 16 * lane);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) halves8(w[e], c[2 * e], c[2 * e + 1]);
+                } else {
+                    const v2u w = *(const v2u *)(unit + 512 * s + 8 * lane);
+                    halves4_keys(w[0], c);
+                    halves4_keys(w[1], c + 4);
+                }
+                const v8h k0 = join(c[0], c[1], c[2], c[3]), k1 = join(c[4], c[5], c[6], c[7]);
+#pragma unroll
+                for (int n = 0; n < N; ++n) score[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][2 * s], score[n][u], 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < N; ++n) score[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * s + 1], score[n][u], 0, 0, 0);
+            }
+        }
+        // Logits, and their exponentials relative to 2^shift.  That these have grown too large is seen from their sum, which is needed anyway.
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            ks[u] *= f;
+            if (BITS == 4) kz[u] *= f;
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    score[n][u][e] = __builtin_fmaf(score[n][u][e], ks[u][e], BITS == 8 ? -shift[n] : __builtin_fmaf(q_sum[n], kz[u][e], -shift[n]));
+        if (!all_seen) {
+            branch();
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int t = (u ? is1 : is0) ? t0 + 16 * u + 4 * g + e : INT32_MAX;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) score[n][u][e] = t < end[n] ? score[n][u][e] : -__builtin_inff();
+                    vs[u][e] = t < any_end ? vs[u][e] : 0.0f;
+                    if (BITS == 4) vz[u][e] = t < any_end ? vz[u][e] : 0.0f;
+                }
+        }
+        float p[N][2][4], sum[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[n][u][e] = exp2_(score[n][u][e]);
+                    sum[n] = u + e == 0 ? p[n][0][0] : sum[n] + p[n][u][e];
+                }
+        bool raise = false;
+#pragma unroll
+        for (int n = 0; n < N; ++n) raise = raise || sum[n] > above[n];
+        if (__any(raise)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float high = -__builtin_inff();
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) high = fmaxf(high, score[n][u][e]);
+                high = row_max(high);
+                const bool begun = above[n] == MOST_SUM;
+                const float by = begun ? fmaxf(high, 0.0f) : high == -__builtin_inff() ? 0.0f : high;
+                const float keep = begun ? exp2_(-by) : 0.0f;                          // (nothing is summed before)
+                shift[n] += by;
+                above[n] = begun || high > -__builtin_inff() ? MOST_SUM : NOT_BEGUN;
+                l[n] *= keep;
+                oz[n] *= keep;
+                sum[n] = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[n][u][e] = exp2_(score[n][u][e] - by);
+                        sum[n] += p[n][u][e];
+                    }
+#pragma unroll
+                for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) l[n] += sum[n];
+        float most_vs = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
+        if (__any(most_vs > R)) {
+#pragma unroll
+            for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
+            const uint32_t bits = above_scale(most_vs);
+            const float inverse = __uint_as_float((254u - bits) << 23), keep = R * inverse;
+            R = __uint_as_float(bits << 23);
+            per_R = inverse * WEIGHT_UNIT;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
+        }
+        // The weights as the second product's operand.
+        float x[N][8], xz[BITS == 4 ? N : 1][8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float by = vs[u][e] * per_R, z = BITS == 4 ? __builtin_fmaf(8.0f, vs[u][e], vz[u][e]) : 0.0f;
+                const int at = place(u, e);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    x[n][at] = p[n][u][e] * by;
+                    if (BITS == 4) xz[n][at] = p[n][u][e] * z;
+                }
+            }
+        if (!all_seen) {
+            // (what only others of the rows see may be a NaN, and 0 times that one too)
+            branch();
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        const bool seen = t0 + 16 * u + 4 * g + e < end[n];
+                        const int at = place(u, e);
+                        x[n][at] = seen ? x[n][at] : 0.0f;
+                        if (BITS == 4) xz[n][at] = seen ? xz[n][at] : 0.0f;
+                    }
+        }
+        if (BITS == 4)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) oz[n] += xz[n][k];
+        v8h weights[N], rests[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            v4u w, rest = {};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = two_halves(x[n][2 * k], x[n][2 * k + 1]);
+            weights[n] = __builtin_bit_cast(v8h, w);
+            if (TWICE)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rest[k] = two_halves(x[n][2 * k] - (float)weights[n][2 * k], x[n][2 * k + 1] - (float)weights[n][2 * k + 1]);
+            rests[n] = __builtin_bit_cast(v8h, rest);
+        }
+        uint32_t words[2][WORDS];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint8_t *const values = pair + u * U::BYTES + U::PART + g * (DIM * BITS / 2);
+            if constexpr (WORDS == 2) {
+                const v2u w = *(const v2u *)(values + 8 * r);
+                words[u][0] = w[0];
+                words[u][1] = w[1];
+            } else {
+#pragma unroll
+                for (int k = 0; k < WORDS / 4; ++k) {
+                    const v4u w = *(const v4u *)(values + 256 * k + 16 * r);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) words[u][4 * k + e] = w[e];
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            v2h c[4], d[4];
+            if constexpr (BITS == 8) {
+                halves8(words[0][k], c[0], c[1]);
+                halves8(words[1][k], c[2], c[3]);
+                add(k, join(c[0], c[1], c[2], c[3]), BIAS8, weights, rests);
+            } else {
+                halves4(words[0][k], c);          // (tokens 0 and 2, 1 and 3; even and odd channels)
+                halves4(words[1][k], d);
+                add(2 * k, join(c[0], c[2], d[0], d[2]), BIAS4_EVEN, weights, rests);
+                add(2 * k + 1, join(c[1], c[3], d[1], d[3]), BIAS4_ODD, weights, rests);
+            }
+        }
+    }
+
+    // Where unit u's token 4 g + e stands in a lane's operand (4 bits: tokens 0, 2, 1, 3, as halves4 has them).
+    static constexpr __device__ int place(int u, int e) { return 4 * u + (BITS == 8 ? e : (e & 1) * 2 + (e >> 1)); }
+
+    // o[.][k] += values * weights.  The values' bias comes off in a product of its own for one block of rows, where the matrix pipe has time to spare (what is
+    // rounded off is 2^-24 of one tile's sums), and before the products for two, which share it.
+    __device__ __forceinline__ void add(int k, v8h values, float bias, const v8h (&weights)[N], const v8h (&rests)[N])
+    {
+        const _Float16 b = (_Float16)-bias;
+        const v8h off = {b, b, b, b, b, b, b, b};
+        if (N > 1) values += off;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (N == 1) o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, weights[n], o[n][k], 0, 0, 0);
+            o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, weights[n], o[n][k], 0, 0, 0);
+            if (TWICE) {
+                if (N == 1) o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, rests[n], o[n][k], 0, 0, 0);
+                o[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values, rests[n], o[n][k], 0, 0, 0);
+            }
+        }
+    }
+
+    __device__ __forceinline__ float most(int n) const { return above[n] == MOST_SUM ? shift[n] : -__builtin_inff(); }
+
+    // Channels channel(k, e, g) ... + 3 of the lane's row of block n, times `by`; z: `by` times the row's sum of weight * z.
+    static constexpr __device__ int channel(int k, int e, int g)
+    {
+        return BITS == 8 ? 64 * k + 16 * g + 4 * e : DIM == 64 ? 16 * g + 4 * e : 128 * (k / 2) + 32 * g + 8 * e + 4 * (k % 2);
+    }
+    __device__ __forceinline__ v4f channels(int n, int k, int e, float by, float z) const
+    {
+        const float unit = R == 0.0f ? 1.0f : R * (1.0f / WEIGHT_UNIT) * by;               // (nothing met: 0, or the NaN of a NaN)
+        v4f x;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = BITS == 4 ? __builtin_fmaf(o[n][4 * k + c][e], unit, z) : o[n][4 * k + c][e] * unit;
+        return x;
+    }
+};
 
 // f(element type, bits, channels), the last two as constants
 template <class F>

@@ -28,10 +28,10 @@ __device__ __forceinline__ void dg_load16_to_lds(const uint8_t *address, uint32_
                  :: "v"(address), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
 // 4 bytes per lane: lane l's land at LDS byte `lds` + 4 l.
-__device__ __forceinline__ void dg_load4_to_lds(const uint8_t *address, uint32_t lds)
+__device__ __forceinline__ void dg_load4_to_lds(const uint8_t *base, int32_t offset, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
-                 :: "v"(address), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+                 :: "v"(offset), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
 // 16 bytes per lane from a buffer: `offset` bytes into it.  The hardware compares the lane's offset with the buffer's size: a load from outside
 // reads as zeros and touches no memory.  There is no scalar offset (soffset is 0): it is not part of what is compared -- it comes off the

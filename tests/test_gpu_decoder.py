@@ -376,6 +376,15 @@ def test_attention(layout, bits, dtype):
         batch.check(batch.run(causal=causal), causal=causal)
 
 
+@pytest.mark.parametrize("rows", ["16", "32", "128"])
+@pytest.mark.parametrize("layout", [1, 3, 4, 7, 8, 9, 10, 11, 13])
+def test_attention_by_any_number_of_rows(layout, rows, monkeypatch):
+    monkeypatch.setenv("DG_ATTENTION_ROWS", rows)
+    for bits, dtype in ((8, "bf16"), (4, "f16")):
+        batch = Batch(*LAYOUTS[layout], bits, dtype, seed=50 + layout)
+        batch.check(batch.run())
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 def test_attention_whatever_max_ctx_says(bits):
     batch = Batch([1, 2], [3000, 900], 4, 2, 64, 16, bits, "f16")
@@ -397,10 +406,12 @@ def test_attention_of_strided_tensors_and_rows_of_no_sequence(new, ctx, bits):
     assert (got[new:] == 9).all() and (out[:, :, 0] == 9).all() and (out[:, :, 65:] == 9).all()
 
 
+@pytest.mark.parametrize("rows", ["16", "32", "128"])
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("new", [1, 3, 80])
-def test_attention_does_not_see_what_is_masked(new, bits):
+def test_attention_does_not_see_what_is_masked(new, bits, rows, monkeypatch):
     """NaN and infinite keys and values that a causal mask hides, or whose page is none, change nothing; seen, they show."""
+    monkeypatch.setenv("DG_ATTENTION_ROWS", rows)
     def poison(b, k, v):
         if new > 1:
             k[-1], v[-1] = float("nan"), float("inf")                # the last token: only the last row sees it
@@ -419,8 +430,10 @@ def test_attention_does_not_see_what_is_masked(new, bits):
     clean.check(hidden, causal=False)
 
 
+@pytest.mark.parametrize("rows", ["16", "32", "128"])
 @pytest.mark.parametrize("bits", [8, 4])
-def test_attention_queries_that_are_not_finite(bits):
+def test_attention_queries_that_are_not_finite(bits, rows, monkeypatch):
+    monkeypatch.setenv("DG_ATTENTION_ROWS", rows)
     batch = Batch([20], [200], 2, 1, 64, 16, bits, "bf16")
     batch.q[3, 1, 5], batch.q[7, 0, 63], batch.q[9, 1] = float("inf"), float("nan"), 0
     got = batch.run()
@@ -432,11 +445,13 @@ def test_attention_queries_that_are_not_finite(bits):
     assert (np.abs(as_f32(got) - want) <= off)[keep].all()
 
 
+@pytest.mark.parametrize("rows", ["16", "32", "128"])
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("new,ctx", [(1, 900), (60, 900)])
 @pytest.mark.parametrize("what", ["large", "small", "outlier", "far", "zero"])
-def test_attention_of_extreme_values(what, new, ctx, bits):
+def test_attention_of_extreme_values(what, new, ctx, bits, rows, monkeypatch):
     """bfloat16's range: keys, values and queries that binary16 does not hold, one value far beyond the others', scores far apart."""
+    monkeypatch.setenv("DG_ATTENTION_ROWS", rows)
     def change(b, k, v):
         if what == "large":
             k *= 1e-25
