@@ -167,7 +167,7 @@ struct Fused {
 template <class T, class X, int WAVES, int ROWS, int TOKENS, bool FUSED>
 __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
 {
-    constexpr int STEPS = TOKENS == 1 ? 4 : 2;
+    constexpr int STEPS = TOKENS == 1 && ROWS == 1 ? 3 : 2;
     __shared__ v4i sums[WAVES][ROWS][TOKENS][64];
     extern __shared__ int8_t quantized[];
     __shared__ float part[WAVES];
@@ -257,9 +257,9 @@ void launch_few(const DgGemmI8 &p, hipStream_t stream)
 {
     const Fused<float> none = {nullptr, 0};
     const int units = dg_simd_count() / 4;
-    // 32 channels a workgroup share the tokens' loads; with too few channels for that, 16, and where that leaves half of the compute units
-    // without a workgroup, twice the wavefronts
-    if (p.M >= 32 * units) gemm_i8_few_kernel<T, float, 8, 2, TOKENS, false><<<(p.M + 31) / 32, 512, 0, stream>>>(p, none);
+    // 32 channels a workgroup share the tokens' loads (16 x 8192 x 8192 18.4 us for 19.7); with too few channels for that, or tokens that cost
+    // little to load, 16 (one token 14.6 for 16.6), and where that leaves half of the compute units without a workgroup, twice the wavefronts
+    if (p.N > 4 && p.M >= 32 * units) gemm_i8_few_kernel<T, float, 8, 2, TOKENS, false><<<(p.M + 31) / 32, 512, 0, stream>>>(p, none);
     else if (p.M > 8 * units || p.K <= 2048) gemm_i8_few_kernel<T, float, 8, 1, TOKENS, false><<<(p.M + 15) / 16, 512, 0, stream>>>(p, none);
     else gemm_i8_few_kernel<T, float, 16, 1, TOKENS, false><<<(p.M + 15) / 16, 1024, 0, stream>>>(p, none);
 }
