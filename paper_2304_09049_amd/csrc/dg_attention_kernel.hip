@@ -222,7 +222,6 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(Args args)
     for (int k = 32; k; k >>= 1) total += __shfl_xor(total, k);
     float o[PER] = {};
     const float *from = args.shares.o + at * DIM + PER * lane;
-#pragma unroll 4
     for (int k = 0; k < args.pieces; ++k) {
         const DgVec<float, PER> x = dg_load_vec<float, PER>(from + k * rows * DIM);
         const float by = __shfl(w, k);

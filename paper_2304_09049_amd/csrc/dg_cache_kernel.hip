@@ -159,47 +159,47 @@ __global__ __launch_bounds__(256) void cache_write_kernel(WriteArgs a)
     const int h = (int)(at % a.c.heads);
 #pragma unroll 1
     for (int64_t token = first + lane / LANES; token - lane / LANES < end; token += F::TOKENS) {     // (once, but where a run of slots ends)
-    const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
-    const int64_t from = p.given ? token : end - 1;                                    // (a lane without a token reads the last one)
-    const DgVec<T, F::PER> k = dg_load_vec<T, F::PER>((const T *)a.k + from * a.k_token + h * a.k_head + part * F::PER);
-    const DgVec<T, F::PER> v = dg_load_vec<T, F::PER>((const T *)a.v + from * a.v_token + h * a.v_head + part * F::PER);
-    uint8_t *const block = a.c.base + p.block;
-    float *const numbers = (float *)(block + 2 * a.c.part) + p.t;
-    uint32_t words[F::WORDS];
-    float s, z;
+        const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
+        const int64_t from = p.given ? token : end - 1;                                    // (a lane without a token reads the last one)
+        const DgVec<T, F::PER> k = dg_load_vec<T, F::PER>((const T *)a.k + from * a.k_token + h * a.k_head + part * F::PER);
+        const DgVec<T, F::PER> v = dg_load_vec<T, F::PER>((const T *)a.v + from * a.v_token + h * a.v_head + part * F::PER);
+        uint8_t *const block = a.c.base + p.block;
+        float *const numbers = (float *)(block + 2 * a.c.part) + p.t;
+        uint32_t words[F::WORDS];
+        float s, z;
 
-    quantize_lane<T, BITS, DIM, LANES>(k, words, s, z);
-    if (p.there) {
+        quantize_lane<T, BITS, DIM, LANES>(k, words, s, z);
+        if (p.there) {
 #pragma unroll
-        for (int i = 0; i < F::BYTES / F::PIECE; ++i)
-            __builtin_memcpy(block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), (const uint8_t *)words + i * F::PIECE, F::PIECE);
-        if (part == 0) {
-            numbers[0] = s;
-            if (BITS == 4) numbers[2 * a.c.page_size] = z;
+            for (int i = 0; i < F::BYTES / F::PIECE; ++i)
+                __builtin_memcpy(block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), (const uint8_t *)words + i * F::PIECE, F::PIECE);
+            if (part == 0) {
+                numbers[0] = s;
+                if (BITS == 4) numbers[2 * a.c.page_size] = z;
+            }
         }
-    }
-    quantize_lane<T, BITS, DIM, LANES>(v, words, s, z);
-    uint8_t *const values = block + a.c.part;
-    if (p.there && part == 0) {
-        numbers[a.c.page_size] = s;
-        if (BITS == 4) numbers[3 * a.c.page_size] = z;
-    }
-    if (p.whole) {
-        __builtin_memcpy(turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, words, F::BYTES);
+        quantize_lane<T, BITS, DIM, LANES>(v, words, s, z);
+        uint8_t *const values = block + a.c.part;
+        if (p.there && part == 0) {
+            numbers[a.c.page_size] = s;
+            if (BITS == 4) numbers[3 * a.c.page_size] = z;
+        }
+        if (p.whole) {
+            __builtin_memcpy(turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, words, F::BYTES);
+            __builtin_amdgcn_wave_barrier();
+            constexpr int ROW = (F::MINE + 3) / 4;                                         // words of a row
+            uint32_t rows[4 * ROW] = {}, out[F::MINE];
+            if (mine < F::STEP) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) __builtin_memcpy(rows + n * ROW, turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, F::MINE);
+                turn<F::MINE>(rows, out);
+                __builtin_memcpy(values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, out, 4 * F::MINE);
+            }
+        } else if (p.there) {
+#pragma unroll
+            for (int i = 0; i < F::BYTES; ++i) values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] = (uint8_t)(words[i / 4] >> (8 * (i & 3)));
+        }
         __builtin_amdgcn_wave_barrier();
-        constexpr int ROW = (F::MINE + 3) / 4;                                         // words of a row
-        uint32_t rows[4 * ROW] = {}, out[F::MINE];
-        if (mine < F::STEP) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) __builtin_memcpy(rows + n * ROW, turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, F::MINE);
-            turn<F::MINE>(rows, out);
-            __builtin_memcpy(values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, out, 4 * F::MINE);
-        }
-    } else if (p.there) {
-#pragma unroll
-        for (int i = 0; i < F::BYTES; ++i) values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] = (uint8_t)(words[i / 4] >> (8 * (i & 3)));
-    }
-    __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -223,69 +223,69 @@ __global__ __launch_bounds__(256) void cache_read_kernel(ReadArgs a)
     const int h = (int)(at % a.c.heads);
 #pragma unroll 1
     for (int64_t token = first + lane / LANES; token - lane / LANES < end; token += F::TOKENS) {
-    const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
-    const uint8_t *const block = a.c.base + p.block, *const values = block + a.c.part;
-    const float *const numbers = (const float *)(block + 2 * a.c.part) + p.t;
-    const auto put = [&](void *to, uint32_t (&words)[F::WORDS], float s, float z) {
-        DgVec<T, F::PER> x;
-        s = p.there ? s : 0.0f;
-        z = p.there ? z : 0.0f;
+        const Place p = place_of<LANES>(a.c, a.slots, token, end, h, lane);
+        const uint8_t *const block = a.c.base + p.block, *const values = block + a.c.part;
+        const float *const numbers = (const float *)(block + 2 * a.c.part) + p.t;
+        const auto put = [&](void *to, uint32_t (&words)[F::WORDS], float s, float z) {
+            DgVec<T, F::PER> x;
+            s = p.there ? s : 0.0f;
+            z = p.there ? z : 0.0f;
 #pragma unroll
-        for (int i = 0; i < F::WORDS; ++i) words[i] = p.there ? words[i] : BITS == 8 ? 0x80808080u : 0u;
+            for (int i = 0; i < F::WORDS; ++i) words[i] = p.there ? words[i] : BITS == 8 ? 0x80808080u : 0u;
 #pragma unroll
-        for (int i = 0; i < F::PER; ++i) {
-            const float code = (float)(words[i * BITS / 32] >> (i * BITS & 31) & (BITS == 8 ? 255u : 15u));
-            x.e[i] = dg_from_float<T>(BITS == 8 ? (code - 128.0f) * s : code * s + z);
-        }
-        if (p.given) dg_store_vec<T, F::PER>((T *)to + (token * a.c.heads + h) * DIM + part * F::PER, x);
-    };
-    // everything is asked for before anything is waited for
-    uint32_t keys[F::WORDS] = {}, words[F::WORDS] = {}, in[F::MINE] = {};
-    float s[2] = {}, z[2] = {};
-    if (a.k) {
-#pragma unroll
-        for (int i = 0; i < F::BYTES / F::PIECE; ++i)
-            __builtin_memcpy((uint8_t *)keys + i * F::PIECE, block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), F::PIECE);
-        s[0] = numbers[0];
-        if (BITS == 4) z[0] = numbers[2 * a.c.page_size];
-    }
-    if (a.v) {
-        s[1] = numbers[a.c.page_size];
-        if (BITS == 4) z[1] = numbers[3 * a.c.page_size];
-        if (p.whole) {
-            if (mine < F::STEP) __builtin_memcpy(in, values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, 4 * F::MINE);
-        } else {
-#pragma unroll
-            for (int i = 0; i < F::BYTES; ++i) words[i / 4] |= (uint32_t)values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] << (8 * (i & 3));
-        }
-    }
-    if (a.k) put(a.k, keys, s[0], z[0]);
-    if (!a.v) continue;
-    if (p.whole) {
-        constexpr int ROW = (F::MINE + 3) / 4;
-        uint32_t rows[4 * ROW] = {};
-        if constexpr (F::MINE >= 4) {
-#pragma unroll
-            for (int i = 0; i < F::MINE / 4; ++i) {
-                uint32_t four[4];
-                turn<4>(in + 4 * i, four);
-#pragma unroll
-                for (int n = 0; n < 4; ++n) rows[n * ROW + i] = four[n];
+            for (int i = 0; i < F::PER; ++i) {
+                const float code = (float)(words[i * BITS / 32] >> (i * BITS & 31) & (BITS == 8 ? 255u : 15u));
+                x.e[i] = dg_from_float<T>(BITS == 8 ? (code - 128.0f) * s : code * s + z);
             }
-        } else {
+            if (p.given) dg_store_vec<T, F::PER>((T *)to + (token * a.c.heads + h) * DIM + part * F::PER, x);
+        };
+        // everything is asked for before anything is waited for
+        uint32_t keys[F::WORDS] = {}, words[F::WORDS] = {}, in[F::MINE] = {};
+        float s[2] = {}, z[2] = {};
+        if (a.k) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-                for (int c = 0; c < F::MINE; ++c) rows[n] |= (in[c] >> (8 * n) & 255u) << (8 * c);
+            for (int i = 0; i < F::BYTES / F::PIECE; ++i)
+                __builtin_memcpy((uint8_t *)keys + i * F::PIECE, block + dg_key_byte<BITS>(p.t, part * F::PER + 16 * i, DIM), F::PIECE);
+            s[0] = numbers[0];
+            if (BITS == 4) z[0] = numbers[2 * a.c.page_size];
         }
-        if (mine < F::STEP)
+        if (a.v) {
+            s[1] = numbers[a.c.page_size];
+            if (BITS == 4) z[1] = numbers[3 * a.c.page_size];
+            if (p.whole) {
+                if (mine < F::STEP) __builtin_memcpy(in, values + (p.first_t >> 2) * (4 * F::STEP) + 4 * mine, 4 * F::MINE);
+            } else {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) __builtin_memcpy(turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, rows + n * ROW, F::MINE);
+                for (int i = 0; i < F::BYTES; ++i) words[i / 4] |= (uint32_t)values[(p.t >> 2) * (4 * F::STEP) + (part * F::BYTES + i) * 4 + (p.t & 3)] << (8 * (i & 3));
+            }
+        }
+        if (a.k) put(a.k, keys, s[0], z[0]);
+        if (!a.v) continue;
+        if (p.whole) {
+            constexpr int ROW = (F::MINE + 3) / 4;
+            uint32_t rows[4 * ROW] = {};
+            if constexpr (F::MINE >= 4) {
+#pragma unroll
+                for (int i = 0; i < F::MINE / 4; ++i) {
+                    uint32_t four[4];
+                    turn<4>(in + 4 * i, four);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) rows[n * ROW + i] = four[n];
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int c = 0; c < F::MINE; ++c) rows[n] |= (in[c] >> (8 * n) & 255u) << (8 * c);
+            }
+            if (mine < F::STEP)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) __builtin_memcpy(turned[wave] + (lane / F::FOUR * 4 + n) * F::STEP + mine, rows + n * ROW, F::MINE);
+            __builtin_amdgcn_wave_barrier();
+            __builtin_memcpy(words, turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, F::BYTES);
+        }
+        put(a.v, words, s[1], z[1]);
         __builtin_amdgcn_wave_barrier();
-        __builtin_memcpy(words, turned[wave] + (lane / LANES) * F::STEP + part * F::BYTES, F::BYTES);
-    }
-    put(a.v, words, s[1], z[1]);
-    __builtin_amdgcn_wave_barrier();
     }
 }
 

@@ -593,3 +593,34 @@ def test_the_same_call_gives_the_same_bits():
     first = batch.run()
     for _ in range(3):
         assert torch.equal(first, batch.run())
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_a_layer_in_chunks_and_in_one_go(bits):
+    """The example layer: a prompt in ragged chunks and decoded tokens leaves the cache as the whole prompt at once does, bit for bit, and its outputs
+    are those up to the attention's rounding (a bfloat16 output's, 2^-8, and what the projection's 8 bits and rounding add to that)."""
+    from paper_2304_09049_amd.decoder_layer import DecoderLayer, PagedSequences
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    hidden, heads, kv_heads, dim = 256, 4, 2, 64
+    weights = [torch.randn(n, m, device="cuda", generator=gen) * m ** -0.5 for n, m in ((8 * dim, hidden), (hidden, heads * dim), (hidden, hidden))]
+    layer = DecoderLayer(*weights, heads, kv_heads, dim)
+    x = torch.randn(2, 60, hidden, device="cuda", generator=gen).bfloat16()
+    desc = dg.cache_desc(16, 16, kv_heads, dim, bits)
+    together, apart = PagedSequences(desc, 2, x.device), PagedSequences(desc, 2, x.device)
+    first = layer.attend(x.reshape(120, hidden), together, [60, 60]).view(2, 60, hidden)
+    at, seen = [0, 0], [[], []]
+    for new in ([17, 1], [1, 40], [1, 1], [40, 17], [1, 1]):
+        tokens = torch.cat([x[b, at[b]:at[b] + n] for b, n in enumerate(new)])
+        y = layer.attend(tokens, apart, new)
+        for b, part in enumerate(y.split(new)):
+            seen[b].append(part)
+            at[b] += new[b]
+    assert at == [60, 60]
+    slots = [torch.tensor([s.pages[b][t // 16] * 16 + t % 16 for b in range(2) for t in range(60)], dtype=torch.int32, device="cuda") for s in (together, apart)]
+    for p, q in zip(*(dg.dg_cache_read(desc, s.cache, at) for s, at in zip((together, apart), slots))):
+        assert torch.equal(p, q)
+    for b in range(2):
+        got, want = torch.cat(seen[b]).float(), first[b].float()
+        assert ((got - want).norm() / want.norm()).item() < 4 * 2.0 ** -8
+    y = layer.step(x[:, 0], together, [1, 1])
+    assert y.shape == (2, hidden) and y.dtype == x.dtype and y.isfinite().all()
