@@ -152,7 +152,9 @@ __device__ __forceinline__ void store4(const DgGemmI8 &p, int32_t m, int32_t n, 
 // ---- few tokens ---------------------------------------------------------------------------------------------------------
 //
 // A workgroup computes 16 ROWS channels x 16 TOKENS tokens; its wavefronts share K in pieces of 128 positions, a cache line of a row, and
-// their sums meet in LDS.  The weights are read once, straight into the matrix instructions' operands, STEPS pieces in flight a wavefront.
+// their sums meet in LDS.  The weights are read once, straight into the matrix instructions' operands, a piece on its way while the one before is
+// multiplied.  That reading bounds it (16 x 8192 x 8192 17.2 us, 3.9 TB/s with the launch; one token 13.7, 4.9 TB/s): two or three pieces asked for at once
+// and then multiplied 18.3, pieces two or three at a time in this way 17.6 and 17.8.
 // FUSED: a single token is quantised here too, by every workgroup for itself, into LDS, while the first weights are on their way (4096 x 4096
 // 6.5 us for 8.1 as two launches; four tokens 11.3 for 8.5).
 
@@ -167,7 +169,6 @@ struct Fused {
 template <class T, class X, int WAVES, int ROWS, int TOKENS, bool FUSED>
 __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fused<X> f)
 {
-    constexpr int STEPS = TOKENS == 1 && ROWS == 1 ? 3 : 2;
     __shared__ v4i sums[WAVES][ROWS][TOKENS][64];
     extern __shared__ int8_t quantized[];
     __shared__ float part[WAVES];
@@ -182,17 +183,32 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fus
     for (int t = 0; t < TOKENS; ++t) a[t] = FUSED ? quantized : p.A + (int64_t)min(16 * t + r, last) * p.stride_a;
     // a piece: two instructions of 64 positions, 16 a lane
     const int32_t pieces = p.K / 128;
-    v4i wk[STEPS][ROWS][2], ak[STEPS][TOKENS][2];
-    const auto fetch_weights = [&](int32_t piece) {
+    v4i wk[2][ROWS][2], ak[2][TOKENS][2], acc[ROWS][TOKENS] = {};
+    const auto fetch_tokens = [&](int to, int32_t piece) {
 #pragma unroll
-        for (int u = 0; u < STEPS; ++u)
-            if (piece + WAVES * u < pieces)
+        for (int t = 0; t < TOKENS; ++t)
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) __builtin_memcpy(&wk[u][i][h], w[i] + 128 * (piece + WAVES * u) + 64 * h + 16 * g, 16);
+            for (int h = 0; h < 2; ++h) __builtin_memcpy(&ak[to][t][h], a[t] + 128 * piece + 64 * h + 16 * g, 16);
     };
-    fetch_weights(wave);
+    const auto fetch = [&](int to, int32_t piece) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) __builtin_memcpy(&wk[to][i][h], w[i] + 128 * piece + 64 * h + 16 * g, 16);
+        if (!FUSED) fetch_tokens(to, piece);
+    };
+    const auto multiply = [&](int from, int32_t piece) {
+        __builtin_amdgcn_sched_barrier(0);                  // (or the compiler moves the next piece's loads behind these products)
+        if (FUSED) fetch_tokens(from, piece);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t)
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[from][i][h], ak[from][t][h], acc[i][t], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (wave < pieces) fetch(0, wave);
     if constexpr (FUSED) {
         constexpr int COUNT = 16 / sizeof(X), STEP = 64 * WAVES * COUNT;
         float most = 0.0f;
@@ -204,26 +220,20 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fus
             store_codes(quantized, at, f.pitch, elements<X, COUNT>(f.x, at, p.K), by);
         __syncthreads();
     }
-    v4i acc[ROWS][TOKENS] = {};
-    for (int32_t piece = wave; piece < pieces; piece += WAVES * STEPS) {
-        if (piece != wave) fetch_weights(piece);
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u)
-            if (piece + WAVES * u < pieces)
-#pragma unroll
-                for (int t = 0; t < TOKENS; ++t)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) __builtin_memcpy(&ak[u][t][h], a[t] + 128 * (piece + WAVES * u) + 64 * h + 16 * g, 16);
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u)
-            if (piece + WAVES * u < pieces)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int t = 0; t < TOKENS; ++t)
-#pragma unroll
-                        for (int i = 0; i < ROWS; ++i)
-                            acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wk[u][i][h], ak[u][t][h], acc[i][t], 0, 0, 0);
+    int32_t at = wave;
+#pragma unroll 1
+    for (; at + 2 * WAVES < pieces; at += 2 * WAVES) {
+        fetch(1, at + WAVES);
+        multiply(0, at);
+        fetch(0, at + 2 * WAVES);
+        multiply(1, at + WAVES);
+    }
+    if (at + WAVES < pieces) {
+        fetch(1, at + WAVES);
+        multiply(0, at);
+        multiply(1, at + WAVES);
+    } else if (at < pieces) {
+        multiply(0, at);
     }
     if (128 * pieces < p.K && pieces % WAVES == wave)               // the rest of the row
 #pragma unroll 1
@@ -252,15 +262,19 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_i8_few_kernel(DgGemmI8 p, Fus
     }
 }
 
+// Whether 16 channels a workgroup are one workgroup a compute unit at most: then twice the wavefronts (one token x 4096 x 4096 5.2 us for 5.5, quantised here
+// as well 6.9 for 7.3; but not where each would have one piece at most: 2048 x 2048 3.1 for 3.0).
+bool few_channels(const DgGemmI8 &p, int units) { return p.M <= 16 * units && p.K > 2048; }
+
 template <class T, int TOKENS>
 void launch_few(const DgGemmI8 &p, hipStream_t stream)
 {
     const Fused<float> none = {nullptr, 0};
     const int units = dg_simd_count() / 4;
-    // 32 channels a workgroup share the tokens' loads (16 x 8192 x 8192 18.4 us for 19.7); with too few channels for that, or tokens that cost
-    // little to load, 16 (one token 14.6 for 16.6), and where that leaves half of the compute units without a workgroup, twice the wavefronts
+    // 32 channels a workgroup share the tokens' loads (16 x 8192 x 8192 17.2 us for 19.9); with too few channels for that, or tokens that cost
+    // little to load, 16 (one token 13.7 for 15.4, four 15.1 for 16.5)
     if (p.N > 4 && p.M >= 32 * units) gemm_i8_few_kernel<T, float, 8, 2, TOKENS, false><<<(p.M + 31) / 32, 512, 0, stream>>>(p, none);
-    else if (p.M > 8 * units || p.K <= 2048) gemm_i8_few_kernel<T, float, 8, 1, TOKENS, false><<<(p.M + 15) / 16, 512, 0, stream>>>(p, none);
+    else if (!few_channels(p, units)) gemm_i8_few_kernel<T, float, 8, 1, TOKENS, false><<<(p.M + 15) / 16, 512, 0, stream>>>(p, none);
     else gemm_i8_few_kernel<T, float, 16, 1, TOKENS, false><<<(p.M + 15) / 16, 1024, 0, stream>>>(p, none);
 }
 
@@ -545,7 +559,9 @@ dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x
     dg_with_type(type, [&](auto t) {
         dg_with_type(x_type, [&](auto s) {
             const Fused<decltype(s)> f = {(const decltype(s) *)x, (p.K + 127) / 128 * 128};
-            gemm_i8_few_kernel<decltype(t), decltype(s), 8, 1, 1, true><<<(p.M + 15) / 16, 512, (uint32_t)f.pitch, stream>>>(p, f);
+            const uint32_t blocks = (p.M + 15) / 16, room = f.pitch;
+            if (few_channels(p, dg_simd_count() / 4)) gemm_i8_few_kernel<decltype(t), decltype(s), 16, 1, 1, true><<<blocks, 1024, room, stream>>>(p, f);
+            else gemm_i8_few_kernel<decltype(t), decltype(s), 8, 1, 1, true><<<blocks, 512, room, stream>>>(p, f);
             return 0;
         });
         return 0;
