@@ -15,7 +15,7 @@ struct DgAttentionShares {
 struct DgAttentionArgs {
     DgAttention a;
     int32_t group, row_blocks, pieces, piece_tokens;
-    DgFastDiv by_group;
+    DgFastDiv by_group, by_heads, by_sequences, by_blocks, by_pieces, by_Hq, by_max_q;       // (divisions by numbers as they come are 100 to 200 instructions each)
     DgAttentionShares shares;
 };
 
@@ -148,6 +148,14 @@ __device__ __forceinline__ float query_operands(const float (&x)[DIM / 32][8], f
 
 // The power of two above a value scale, from 2^-100 to 2^126, by its exponent's bits.
 __device__ __forceinline__ uint32_t above_scale(float most) { return min(max((__float_as_uint(most) >> 23) + 1, 27u), 253u); }
+
+// at / by, and at becomes the rest.
+__device__ __forceinline__ uint32_t taken(uint32_t &at, const DgFastDiv &by)
+{
+    const uint32_t n = dg_fdiv(at, by);
+    at -= n * by.d;
+    return n;
+}
 
 // What a sequence's new tokens are, with everything that lies in device memory held to what the buffers have.
 struct Sequence {

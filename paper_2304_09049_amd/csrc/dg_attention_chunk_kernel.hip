@@ -20,12 +20,8 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chun
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     // heads innermost: a head's workgroups follow each other at a distance of `heads`, so with eight of them each die has its own; the last rows, which see
     // most, first
-    int rest = blockIdx.x;
-    const int h = rest % a.cache.heads;
-    rest /= a.cache.heads;
-    const int piece = rest % args.pieces;
-    rest /= args.pieces;
-    const int row_block = args.row_blocks - 1 - rest % args.row_blocks, b = rest / args.row_blocks;
+    uint32_t in_heads = blockIdx.x, in_pieces = taken(in_heads, args.by_heads), in_blocks = taken(in_pieces, args.by_pieces);
+    const int b = taken(in_blocks, args.by_blocks), row_block = args.row_blocks - 1 - (int)in_blocks, piece = in_pieces, h = in_heads;
     const Sequence seq = sequence(a, b);
     const int first_row = row_block * CHUNK_ROWS, have = min(seq.count * args.group - first_row, CHUNK_ROWS);
     if (have <= 0) return;

@@ -43,12 +43,8 @@ __global__ __launch_bounds__(64 * WAVES, (Kept<BITS, DIM, N>::WAVES_PER_SIMD)) v
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     // Heads innermost and pieces outermost: neighbouring workgroups go to different dies (eight), and a context's last pieces, which shorter ones do not
     // have, are not to be all of one die (64 contexts of up to 8192 in 4 pieces, pieces innermost: 104 us for 92).
-    int rest = blockIdx.x;
-    const int h = rest % a.cache.heads;
-    rest /= a.cache.heads;
-    const int b = rest % a.B;
-    rest /= a.B;
-    const int row_block = rest % args.row_blocks, piece = rest / args.row_blocks;
+    uint32_t in_heads = blockIdx.x, in_sequences = taken(in_heads, args.by_heads), in_blocks = taken(in_sequences, args.by_sequences);
+    const int piece = taken(in_blocks, args.by_blocks), h = in_heads, b = in_sequences, row_block = in_blocks;
     const Sequence seq = sequence(a, b);
     const int have = min(seq.count * args.group - row_block * ROWS, ROWS);                  // rows of the block that are there
     if (have <= 0) return;
@@ -161,8 +157,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args args)
     __shared__ v4f sums[GROUPS][LANES];
     const DgAttention &a = args.a;
     const int64_t rows = (int64_t)a.B * a.max_q * a.Hq, at = blockIdx.x;
-    const int64_t token = at / a.Hq, head = at % a.Hq;
-    const int b = (int)(token / a.max_q), i = (int)(token % a.max_q);
+    uint32_t in_token = (uint32_t)at, in_sequence = taken(in_token, args.by_Hq);
+    const int b = taken(in_sequence, args.by_max_q), i = in_sequence, head = in_token;
     const Sequence seq = sequence(a, b);
     if (i >= seq.count) return;
     // (a thread a piece)
@@ -207,8 +203,8 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(Args args)
     const int64_t rows = (int64_t)a.B * a.max_q * a.Hq, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= rows) return;
     const int lane = threadIdx.x & 63;
-    const int64_t token = at / a.Hq, head = at % a.Hq;
-    const int b = (int)(token / a.max_q), i = (int)(token % a.max_q);
+    uint32_t in_token = (uint32_t)at, in_sequence = taken(in_token, args.by_Hq);
+    const int b = taken(in_sequence, args.by_max_q), i = in_sequence, head = in_token;
     const Sequence seq = sequence(a, b);
     if (i >= seq.count) return;
     const bool mine = lane < args.pieces;
@@ -283,7 +279,8 @@ int64_t dg_attention_work_bytes(const DgAttention &a)
 dg_status dg_launch_attention(const DgAttention &a, dg_dtype type, hipStream_t stream)
 {
     const Plan p = plan_of(a);
-    Args args = {a, a.Hq / a.cache.heads, p.row_blocks, p.pieces, p.piece_tokens, dg_make_div((uint32_t)(a.Hq / a.cache.heads)), {}};
+    Args args = {a, a.Hq / a.cache.heads, p.row_blocks, p.pieces, p.piece_tokens, dg_make_div((uint32_t)(a.Hq / a.cache.heads)), dg_make_div(a.cache.heads), dg_make_div(a.B),
+                 dg_make_div(p.row_blocks), dg_make_div(p.pieces), dg_make_div(a.Hq), dg_make_div(a.max_q), {}};
     const int64_t rows = (int64_t)a.B * a.max_q * a.Hq;
     args.shares.o = (float *)a.work;
     args.shares.m = args.shares.o + (int64_t)p.pieces * rows * a.cache.dim;
