@@ -72,9 +72,8 @@ __device__ __forceinline__ void halves4_keys(uint32_t w, v2h *o)
 }
 __device__ __forceinline__ uint32_t two_halves(float a, float b)       // rounded to nearest even
 {
-    uint32_t w;
-    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(a), "v"(b));
-    return w;
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){a, b}, v2h));
 }
 __device__ __forceinline__ v8h join(v2h a, v2h b, v2h c, v2h d)
 {
