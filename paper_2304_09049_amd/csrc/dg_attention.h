@@ -95,16 +95,8 @@ __device__ __forceinline__ v8h query_operand(const float (&x)[8], float up)
 }
 
 // max / sum over the four lanes that hold a row (l, l ^ 16, l ^ 32, l ^ 48)
-__device__ __forceinline__ float row_max(float v)
-{
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float row_sum(float v)
-{
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
-}
+__device__ __forceinline__ float row_max(float v) { return dg_over_rows(v, DgMax()); }
+__device__ __forceinline__ float row_sum(float v) { return dg_over_rows(v, DgAdd()); }
 // In a block that few tiles come to: keeps it a branch of its own, where the compiler would select value by value in every tile.
 __device__ __forceinline__ void branch() { asm volatile(""); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -249,8 +241,7 @@ struct Rows {
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[n][k] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
         }
-#pragma unroll
-        for (int k = 8; k; k >>= 1) largest = fmaxf(largest, __shfl_xor(largest, k));
+        largest = dg_over_lanes<16>(largest, DgMax());
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             q_sum[n] = query_operands<BITS, DIM>(x[n], largest, a.scale, q[n], f);
@@ -372,8 +363,7 @@ struct Rows {
 #pragma unroll
             for (int e = 0; e < 4; ++e) most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
         if (__any(most_vs > R)) {
-#pragma unroll
-            for (int k = 32; k; k >>= 1) most_vs = fmaxf(most_vs, __shfl_xor(most_vs, k));
+            most_vs = row_max(most_vs);                                                // (a lane's tokens are those of its row of lanes)
             const uint32_t bits = above_scale(most_vs);
             const float inverse = __uint_as_float((254u - bits) << 23), keep = R * inverse;
             R = __uint_as_float(bits << 23);

@@ -165,17 +165,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args args)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x / LANES, part = threadIdx.x % LANES;
     const bool mine = (int)threadIdx.x < args.pieces;
     const float m = mine ? args.shares.m[threadIdx.x * rows + at] : -__builtin_inff(), l = mine ? args.shares.l[threadIdx.x * rows + at] : 0.0f;
-    float most = m;
-#pragma unroll
-    for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+    float most = dg_over_wave(m, DgMax());
     if (lane == 0) wave_max[wave] = most;
     __syncthreads();
     most = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
     const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
     weight[threadIdx.x] = w;
-    float total = l * w;
-#pragma unroll
-    for (int k = 32; k; k >>= 1) total += __shfl_xor(total, k);
+    float total = dg_over_wave(l * w, DgAdd());
     if (lane == 0) wave_sum[wave] = total;
     __syncthreads();
     v4f o = {};
@@ -209,18 +205,14 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(Args args)
     if (i >= seq.count) return;
     const bool mine = lane < args.pieces;
     const float m = mine ? args.shares.m[lane * rows + at] : -__builtin_inff(), l = mine ? args.shares.l[lane * rows + at] : 0.0f;
-    float most = m;
-#pragma unroll
-    for (int k = 32; k; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+    const float most = dg_over_wave(m, DgMax());
     const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
-    float total = l * w;
-#pragma unroll
-    for (int k = 32; k; k >>= 1) total += __shfl_xor(total, k);
+    float total = dg_over_wave(l * w, DgAdd());
     float o[PER] = {};
     const float *from = args.shares.o + at * DIM + PER * lane;
     for (int k = 0; k < args.pieces; ++k) {
         const DgVec<float, PER> x = dg_load_vec<float, PER>(from + k * rows * DIM);
-        const float by = __shfl(w, k);
+        const float by = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
 #pragma unroll
         for (int e = 0; e < PER; ++e) o[e] += x.e[e] * by;
     }
@@ -245,8 +237,9 @@ struct Plan {
 //     1000 on 1000, 16/16 x 64          20    34    36        512 x 4 on 4096 (ragged), 32/8 x 128     131   130   151
 //     2048 x 2 on 2048, 32/8 x 128     255   241   171        2048 on 32768, 32/8 x 128   1850  1470  1400
 // Pieces: one workgroup a SIMD (half as many of 32 rows; more: 64 contexts of up to 8192, 4 bits, 92 us with one or two a SIMD, 107 with eight), pieces of 512
-// tokens at least; where that leaves compute units without a workgroup, pieces of 256 (one context of 1000 9.7 us for 11.3, of 4096 10.9 for 12.7; but
-// four of 8192 23.0 for 19.4).
+// tokens at least; where that leaves compute units without a workgroup, pieces of 128, a tile a wavefront (one context of 1000 8.1 us, 8.9 by pieces of
+// 256; of 4000 8.8, 9.9; but four of 8192 by pieces of 256 23.0 for 19.4), or one piece, which needs no joining, of up to four tiles a wavefront (two with
+// 256 channels, whose tiles take twice as long): 250 tokens 6.1 for 8.0, 500 7.8 for 8.1, 600 8.6 for 8.1.
 Plan plan_of(const DgAttention &a)
 {
     const int64_t rows = (int64_t)a.max_q * (a.Hq / a.cache.heads), simds = dg_simd_count(), units = simds / 4;
@@ -261,7 +254,7 @@ Plan plan_of(const DgAttention &a)
     const int64_t blocks = blocks_of(p.rows);
     const auto cut = [&](int64_t most, int64_t least) { return std::max<int64_t>(1, std::min({most / blocks, (a.max_ctx + least - 1) / least, (int64_t)MOST_PIECES})); };
     int64_t pieces = cut(p.rows == 16 ? simds : simds / 2, 512);
-    if (blocks * pieces < units) pieces = cut(units, 256);
+    if (blocks * pieces < units) pieces = a.max_ctx <= (a.cache.dim == 256 ? 256 : 512) ? 1 : cut(units, 128);
     p.pieces = (int32_t)pieces;
     p.piece_tokens = (int32_t)((a.max_ctx + pieces * step - 1) / (pieces * step) * step);
     return p;

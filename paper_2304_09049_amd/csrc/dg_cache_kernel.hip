@@ -27,27 +27,11 @@ struct Form {
     static constexpr int MINE = STEP < FOUR ? 1 : STEP / FOUR;           // words of values that a lane stores, or reads, of four tokens
 };
 
-template <int CONTROL>
-__device__ __forceinline__ float other_lane(float v)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xF, 0xF, false));
-}
-// f over the lanes of a token, the same in each
-template <int LANES, class F>
-__device__ __forceinline__ float over_token(float v, F f)
-{
-    if (LANES == 16) v = f(v, other_lane<0x140>(v));        // row_mirror
-    v = f(v, other_lane<0xB1>(v));          // quad_perm 1, 0, 3, 2
-    v = f(v, other_lane<0x4E>(v));          // quad_perm 2, 3, 0, 1
-    return f(v, other_lane<0x141>(v));      // row_half_mirror
-}
-
 // A lane's channels of one token as codes, and the token's numbers.
 template <class T, int BITS, int DIM, int LANES>
 __device__ __forceinline__ void quantize_lane(const DgVec<T, DIM / LANES> &x, uint32_t (&words)[Form<BITS, DIM, LANES>::WORDS], float &s, float &z)
 {
     constexpr int PER = DIM / LANES;
-    const auto most = [](float a, float b) { return fmaxf(a, b); };
     float lo = __builtin_inff(), hi = BITS == 8 ? 0.0f : -__builtin_inff(), bad = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -57,8 +41,8 @@ __device__ __forceinline__ void quantize_lane(const DgVec<T, DIM / LANES> &x, ui
         bad = __builtin_fmaf(f, 0.0f, bad);                   // (a NaN once there was an infinity or a NaN)
     }
     bad = bad == 0.0f ? 0.0f : 1.0f;
-    hi = over_token<LANES>(hi, most);
-    bad = over_token<LANES>(bad, most);
+    hi = dg_over_lanes<LANES>(hi, DgMax());
+    bad = dg_over_lanes<LANES>(bad, DgMax());
     if constexpr (BITS == 8) {
         s = bad == 0.0f ? hi / 127.0f : __builtin_nanf("");
         const DgDivisor by = dg_divisor(s);
@@ -71,7 +55,7 @@ __device__ __forceinline__ void quantize_lane(const DgVec<T, DIM / LANES> &x, ui
         }
         z = 0.0f;
     } else {
-        lo = over_token<LANES>(lo, [](float a, float b) { return fminf(a, b); });
+        lo = dg_over_lanes<LANES>(lo, DgMin());
         s = bad == 0.0f ? hi / 15.0f - lo / 15.0f : __builtin_nanf("");
         z = lo;
         const DgDivisor by = dg_divisor(s);

@@ -40,6 +40,43 @@ auto dg_with_type(dg_dtype type, F f)
 }
 inline int64_t dg_type_size(dg_dtype type) { return type == DG_F32 ? 4 : 2; }
 
+// ---- one number out of a wavefront's, by register moves (a shuffle by way of LDS is some 130 cycles, and six of them make a kernel of 2 us 0.3 longer) ----
+
+template <int CONTROL>
+__device__ __forceinline__ float dg_other_lane(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xF, 0xF, false));
+}
+// f over neighbouring lanes, the same in each: 8 or 16 of them, the four that are 16 apart, all 64.
+template <int LANES, class F>
+__device__ __forceinline__ float dg_over_lanes(float v, F f)
+{
+    static_assert(LANES == 8 || LANES == 16, "within a row of lanes");
+    if (LANES == 16) v = f(v, dg_other_lane<0x140>(v));        // row_mirror
+    v = f(v, dg_other_lane<0xB1>(v));          // quad_perm 1, 0, 3, 2
+    v = f(v, dg_other_lane<0x4E>(v));          // quad_perm 2, 3, 0, 1
+    return f(v, dg_other_lane<0x141>(v));      // row_half_mirror
+}
+template <class F>
+__device__ __forceinline__ float dg_over_rows(float v, F f)
+{
+    const auto near = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(near[0]), __uint_as_float(near[1]));
+    const auto far = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(far[0]), __uint_as_float(far[1]));
+}
+template <class F>
+__device__ __forceinline__ float dg_over_wave(float v, F f) { return dg_over_rows(dg_over_lanes<16>(v, f), f); }
+struct DgMax {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct DgMin {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
+};
+struct DgAdd {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+
 // ---- quantisers (binary32, operation by operation) -----------------------------------------------------------------------
 
 // Division by one s for many x, correctly rounded and without a branch: x times the rounded reciprocal, then twice the remainder, which a fused

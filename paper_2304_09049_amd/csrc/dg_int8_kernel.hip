@@ -17,9 +17,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 template <int WAVES>
 __device__ __forceinline__ float workgroup_most(float most, bool finite, float *part)
 {
-    most = finite ? most : __builtin_inff();
-#pragma unroll
-    for (int i = 32; i; i >>= 1) most = fmaxf(most, __shfl_xor(most, i));
+    most = dg_over_wave(finite ? most : __builtin_inff(), DgMax());
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
     __syncthreads();
     most = part[0];
