@@ -10,6 +10,9 @@
  * K = reduction length (KH*KW*Cin for a convolution).  Wc[m][k], Ac[n][k] are codes in {0..3};
  * lw[4], la[4] are the level tables; LUT[4*w + a] = lw[w] * la[a].
  *
+ * The last part is what a quantised decoder layer needs around such products: 8-bit integer products with run-time scales, a
+ * paged cache of keys and values in 8 or 4 bits, attention over it.
+ *
  * Conventions common to every call
  *   - Every function returns a dg_status, never throws, never aborts, never synchronises the
  *     device.  Arguments are validated on the host BEFORE anything is launched; on error nothing

@@ -1,15 +1,19 @@
 // Attention of new tokens over the paged cache.
 //
 // A row is one query head of one new token; the rows of a sequence that read the same cached head -- (token, head of the group), the
-// token outermost -- are taken 16 at a time.  Scores come out transposed, S^T = K Q^T (tokens x rows): a lane then holds four tokens of
+// token outermost -- are taken 16 at a time (two such blocks a wavefront where there are many).  Scores come out transposed, S^T = K Q^T (tokens x rows): a lane then holds four tokens of
 // one row in the order in which the second product, O^T = V^T P^T, takes its operand, so that the weights never leave the lane.  Keys and
 // values lie in the cache as the two products' first operands: 16 contiguous bytes a lane, neighbouring lanes side by side.
 //
 // Numbers: codes become binary16 exactly.  A query row is scaled by a power of
 // two to a largest magnitude in [2^13, 2^14), so that bfloat16's range fits binary16 and nothing above 2^-28 of the row's largest loses a
-// bit.  Scores, maxima, sums and outputs are binary32.  A weight is rounded once, to binary16, as p * (value scale / R) * 2^10, where R is
-// a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  The maximum is
-// raised only when a score passes it by 2^4, so that p <= 16 and the weights stay below 2^15.
+// bit.  Scores, shifts, sums and outputs are binary32.  A weight is rounded once, to binary16, as p * (value scale / R) * 2^10, where R is
+// a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  p = 2^(logit - shift); the shift is
+// the first tile's maximum, and is raised only when eight of a lane's weights add up to more than 16: any p is then at most 16, and weights stay below 2^15.
+//
+// What bounds it: for single tokens the cache's bytes, read once (one context of 131071 tokens, 32 heads on 8 of 128 channels, 8 bits: 59 us, 4.7 TB/s; 64 contexts of
+// up to 8192, 4 bits: 82 us, 3.7 TB/s: there the vector unit is as busy, 16 columns of a product for the 4 rows that there are), or, for short contexts, two launches
+// and one tile's chain of latencies (one context of 1000: 8.1 us; of 250, one launch, 6.1); for many rows the vector unit (chunk kernel).
 #include <algorithm>
 #include <cstring>
 
