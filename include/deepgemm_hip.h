@@ -455,7 +455,8 @@ dg_status dg_cache_read(const dg_cache_desc *desc, const void *cache_dev, size_t
  * to the table's width, and a page number that is none of the cache's hides its tokens, as does nothing else.  max_q: no sequence has more new tokens
  * (later ones get no output).  max_ctx: about the longest context; how the work is cut goes by it, results are right whatever it is.
  * Codes enter the matrix instructions exactly; scores, softmax and sums are binary32; weights are rounded once, to binary16 with a scale of
- * their own.  Rows of no sequence are not written.  work_dev: dg_paged_attention_work_bytes(...) bytes, 16-byte aligned (0 bytes: may be NULL).
+ * their own (to two binary16 numbers for binary16 outputs).
+ * Rows of no sequence are not written.  work_dev: dg_paged_attention_work_bytes(...) bytes, 16-byte aligned (0 bytes: may be NULL).
  * Errors: DG_ERR_NULL; DG_ERR_SHAPE (Hq no multiple of heads, negative sizes); DG_ERR_RANGE (rows beyond 32 bits); DG_ERR_UNSUPPORTED;
  * DG_ERR_BUFFER.
  */
