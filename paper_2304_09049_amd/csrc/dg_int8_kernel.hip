@@ -495,19 +495,20 @@ void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
     else gemm_i8_tile_kernel<T, WM, WN, TM, TN, KS, 2, false><<<tiles, 64 * WM * WN * KS, 0, stream>>>(a);
 }
 
-enum class Form { Few, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
+enum class Form { Few, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
 constexpr int FEW_TOKENS = 32;
 
-// The kernel for up to 32 tokens (16 x 4096 x 4096 6.4 us, 64 x 64 tiles 8.8; 32 tokens 8.5, 9.3; 48 11.3, 9.5), or the tile whose rounds over the
-// compute units, one workgroup each, cost least.  A round's cost by tile, us for K = 4096 and 8192: 64 x 64 10, 24; 128 x 64 15, 34; 128 x 128 23, 46;
-// 256 x 128 39, 72; 256 x 256 54, 104.  Of 20 products from 64 x 4096 x 4096 to 8192 x 8192 x 8192 this takes the fastest tile on all.
+// The kernel for up to 32 tokens (16 x 4096 x 4096 6.4 us, 64 x 64 tiles 8.8; 32 tokens 8.1, 32 x 64 tiles 8.2), or the tile (channels x tokens) whose
+// rounds over the compute units, one workgroup each, cost least.  A round's cost by tile, us for K = 4096 and 8192: 32 x 64 8, 18; 64 x 64 10, 24; 128 x 64 15, 34;
+// 128 x 128 23, 46; 256 x 128 39, 72; 256 x 256 54, 104.  Of 60 products, 33 to 2048 tokens, this is within 3 % of the fastest tile on 58, 6 % on two (64 x 2048 x 8192
+// 11.7 us by 32 x 64, 15.0 by 64 x 64; 128 x 8192 x 8192 33.8, 24.1).
 Form form_of(const DgGemmI8 &p)
 {
     static const struct {
         Form form;
         int32_t m, n, cost;
         const char *name;
-    } tiles[] = {{Form::Tile64x64, 64, 64, 28, "64x64"}, {Form::Tile128x64, 128, 64, 40, "128x64"}, {Form::Tile128x128, 128, 128, 54, "128x128"},
+    } tiles[] = {{Form::Tile32x64, 32, 64, 22, "32x64"}, {Form::Tile64x64, 64, 64, 28, "64x64"}, {Form::Tile128x64, 128, 64, 40, "128x64"}, {Form::Tile128x128, 128, 128, 54, "128x128"},
                  {Form::Tile256x128, 256, 128, 85, "256x128"}, {Form::Tile256x256, 256, 256, 124, "256x256"}};
     const char *forced = dg_override("DG_GEMM_I8_TILE");
     const int64_t units = dg_simd_count() / 4;
@@ -580,6 +581,7 @@ dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream
             if (p.N <= 16) launch_few<T, 1>(p, stream);
             else launch_few<T, 2>(p, stream);
             break;
+        case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
         case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
         case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
         case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;

@@ -104,7 +104,7 @@ def test_gemm_i8(M, N, K, dtype):
     assert same(as_f32(out), rounded(product(W, A, sm, sn, bias if with_bias else None), dtype))
 
 
-@pytest.mark.parametrize("tile", ["64x64", "128x64", "128x128", "256x128", "256x256"])
+@pytest.mark.parametrize("tile", ["32x64", "64x64", "128x64", "128x128", "256x128", "256x256"])
 @pytest.mark.parametrize("M,N,K", [(300, 200, 1040), (257, 130, 128), (64, 300, 16), (1030, 515, 272), (129, 1, 2000), (520, 260, 999)])
 def test_gemm_i8_in_every_tile(M, N, K, tile, monkeypatch):
     monkeypatch.setenv("DG_GEMM_I8_TILE", tile)
