@@ -323,18 +323,24 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_i8_tile_kernel(TileArg
     const int8_t *rows_w = p.W + (int64_t)m0 * p.stride_w, *rows_a = p.A + (int64_t)n0 * p.stride_a;
     const int32_t have_w = min(p.M - m0, BM), have_a = min(p.N - n0, BN);
     uint32_t offset[LOADS];
-    bool there[LOADS];
+    const auto row_of = [&](int i) { return (wave + WAVES * (i < LOADS_M ? i : i - LOADS_M)) * 8 + (lane >> 3); };
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int row = (wave + WAVES * (i < LOADS_M ? i : i - LOADS_M)) * 8 + (lane >> 3);
-        there[i] = row < (i < LOADS_M ? have_w : have_a);
         const uint32_t stride = (uint32_t)(i < LOADS_M ? p.stride_w : p.stride_a);
-        offset[i] = there[i] ? row * stride + 16 * piece : DIRECT ? 0xF0000000u : 0u;
+        offset[i] = row_of(i) < (i < LOADS_M ? have_w : have_a) ? row_of(i) * stride + 16 * piece : 0xF0000000u;
     }
     const dg_v4i buffer_w = dg_buffer((const uint8_t *)rows_w, DIRECT ? (uint32_t)((have_w - 1) * (uint32_t)p.stride_w + p.K) : 0u);
     const dg_v4i buffer_a = dg_buffer((const uint8_t *)rows_a, DIRECT ? (uint32_t)((have_a - 1) * (uint32_t)p.stride_a + p.K) : 0u);
     const uint32_t lds = dg_lds_address(room) + share * (STAGES * STAGE) + 1024 * wave;
-    v4i held[DIRECT ? 1 : LOADS];
+    // Through registers, two stages on their way where a stage is few of them (300 x 4000 x 5001 37.8 us, one 39.5).  What bounds this form is the loads themselves,
+    // which the hardware serves at a fraction of its rate where they do not begin on 16 bytes (300 x 4000 x 4992 16.5).
+    constexpr int AHEAD = LOADS <= 6 ? 2 : 1;
+    v4i held[DIRECT ? 1 : AHEAD][LOADS];
+    const auto address = [&](int i, int32_t k) {
+        int row = min(row_of(i), (i < LOADS_M ? have_w : have_a) - 1);                       // (what a row past the end gives is not stored)
+        if (AHEAD == 1) asm volatile("" : "+v"(row));                                        // (its address is not worth two registers)
+        return (i < LOADS_M ? rows_w : rows_a) + row * (i < LOADS_M ? p.stride_w : p.stride_a) + k;
+    };
 
     auto fetch = [&](int32_t k, int to) {
         if constexpr (DIRECT) {
@@ -344,13 +350,12 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_i8_tile_kernel(TileArg
                 const uint32_t at = past ? 0xF0000000u : offset[i] + k;
                 dg_load16_to_lds(i < LOADS_M ? buffer_w : buffer_a, at, lds + to * STAGE + i * (1024 * WAVES));
             }
+        } else if (k + 128 <= p.K) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&held[to][i], address(i, k) + 16 * piece, 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int8_t *row = (i < LOADS_M ? rows_w : rows_a) + (int64_t)((wave + WAVES * (i < LOADS_M ? i : i - LOADS_M)) * 8 + (lane >> 3)) *
-                                                                          (i < LOADS_M ? p.stride_w : p.stride_a);
-                held[i] = there[i] ? codes16(row, k + 16 * piece, p.K) : (v4i){0, 0, 0, 0};
-            }
+            for (int i = 0; i < LOADS; ++i) held[to][i] = codes16(address(i, 0), k + 16 * piece, p.K);
         }
     };
     const int r = lane & 31, g = lane >> 5, wm = wave % WM, wn = wave / WM;
@@ -395,19 +400,26 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_i8_tile_kernel(TileArg
         }
         dg_wait_for_loads<0>();
     } else {
-        const auto put = [&](int to) {
+        const auto put = [&](int from, int to) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) *(v4i *)(stages[to] + 1024 * (wave + WAVES * i) + 16 * lane) = held[i];
+            for (int i = 0; i < LOADS; ++i) *(v4i *)(stages[to] + 1024 * (wave + WAVES * i) + 16 * lane) = held[from][i];
             __syncthreads();
         };
-        fetch(128 * share, 0);
-        put(0);
-        for (int32_t k = 0, now = 0; k < p.K; k += 128 * KS, now ^= 1) {
-            const bool more = k + 128 * KS < p.K;
-            if (more) fetch(k + 128 * (KS + share), now ^ 1);
-            read(now, 0);
-            multiply(now);
-            if (more) put(now ^ 1);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(128 * (KS * i + share), i);
+        put(0, 0);
+        for (int32_t k = 0, now = 0; k < p.K;) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (i && k >= p.K) break;
+                const bool more = k + 128 * KS < p.K;
+                if (k + 128 * KS * AHEAD < p.K) fetch(k + 128 * (KS * AHEAD + share), i);
+                read(now, 0);
+                multiply(now);
+                if (more) put((i + 1) % AHEAD, now ^ 1);
+                k += 128 * KS;
+                now ^= 1;
+            }
         }
     }
     // The results go by way of LDS, a wavefront's 32 tokens at a time: rows of channels leave side by side, and a loop does it (written out
