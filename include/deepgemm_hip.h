@@ -424,7 +424,8 @@ dg_status dg_linear_i8(const int8_t *W_dev, int64_t stride_w, const void *x_dev,
  *     key    byte (t/16) * 2*b*dim + (d/16) * 32*b + (t%16) * 2*b + (d%16)*b/8
  *     value  byte (t/4) * b*dim/2 + (d*b/8) * 4 + t%4
  * and of a 4-bit byte the even channel has the low half.  (Both are the matrix instructions' operands as they lie.)
- * A slot is page * page_size + token; pages * page_size < 2^31.
+ * A slot is page * page_size + token; pages * page_size < 2^31; a page's bytes for one head are below 2^31,
+ * a cache's below 2^63 (else DG_ERR_RANGE).
  */
 typedef struct {
     int32_t pages, page_size, heads, dim, bits;
@@ -434,7 +435,7 @@ size_t dg_cache_bytes(const dg_cache_desc *desc);
 /*
  * Quantise T tokens' keys and values ([T][heads][dim] of `type`, token and head strides apart, channels contiguous) into slots_dev[T].  A
  * negative slot, or one past the cache, is skipped; the other slots must differ from one another.  Nothing else in the cache changes.
- * Errors: DG_ERR_NULL; DG_ERR_SHAPE; DG_ERR_RANGE (slots beyond 32 bits); DG_ERR_UNSUPPORTED (bits, dim, type); DG_ERR_BUFFER
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE; DG_ERR_RANGE (slots, pages or caches too large); DG_ERR_UNSUPPORTED (bits, dim, type); DG_ERR_BUFFER
  * (cache_bytes, alignment).
  */
 dg_status dg_cache_write(const dg_cache_desc *desc, void *cache_dev, size_t cache_bytes, const void *k_dev, const void *v_dev, dg_dtype type,

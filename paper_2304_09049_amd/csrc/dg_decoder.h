@@ -125,7 +125,8 @@ __device__ __forceinline__ float dg_scale8(float most) { return most < __builtin
 // ---- the cache ---------------------------------------------------------------------------------------------------------
 
 // A cache as the kernels take it.  A page holds `heads` blocks of `head` bytes: keys' codes (`part` bytes), values' codes (`part`),
-// then `page_size` binary32 numbers each of key scale, value scale and, 4 bits, key z and value z.
+// then `page_size` binary32 numbers each of key scale, value scale and, 4 bits, key z and value z.  `head` is below 2^31 (the API layer has seen to it),
+// so places within a head are 32-bit numbers; a token's bytes are whole, so that no product here is larger than what it stands for.
 struct DgCache {
     uint8_t *base;
     int32_t pages, page_size, heads, dim, bits;
@@ -143,7 +144,7 @@ inline DgCache dg_cache_of(const dg_cache_desc *d, void *base)
     c.heads = d->heads;
     c.dim = d->dim;
     c.bits = d->bits;
-    c.part = d->page_size * d->dim * d->bits / 8;
+    c.part = d->page_size * (d->dim * d->bits / 8);
     c.head = 2 * c.part + d->page_size * (d->bits == 8 ? 8 : 16);
     c.by_page = dg_make_div((uint32_t)d->page_size);
     return c;

@@ -45,8 +45,11 @@ dg_status check_cache(const char *what, const dg_cache_desc *d, const void *cach
     if (d->pages <= 0 || d->heads <= 0 || d->page_size <= 0 || d->page_size % 16 != 0)
         return dg_fail(DG_ERR_SHAPE, "%s: %d pages of %d tokens (a multiple of 16), %d heads", what, (int)d->pages, (int)d->page_size,
                        (int)d->heads);
-    if ((int64_t)d->pages * d->page_size > MOST_ROWS || (int64_t)d->page_size * (2 * d->dim + 16) > MOST_ROWS)
-        return dg_fail(DG_ERR_RANGE, "%s: %d pages of %d tokens: slots are 32-bit numbers", what, (int)d->pages, (int)d->page_size);
+    const int64_t head = d->page_size * (int64_t)(2 * d->dim * d->bits / 8 + (d->bits == 8 ? 8 : 16));       // a page's bytes for one head
+    if ((int64_t)d->pages * d->page_size > MOST_ROWS || head > MOST_ROWS)
+        return dg_fail(DG_ERR_RANGE, "%s: %d pages of %d tokens: slots, and a page's bytes for one head, are 32-bit numbers", what, (int)d->pages, (int)d->page_size);
+    if (head * d->heads > INT64_MAX / d->pages)
+        return dg_fail(DG_ERR_RANGE, "%s: %d pages of %d tokens, %d heads: the bytes are no 64-bit number", what, (int)d->pages, (int)d->page_size, (int)d->heads);
     if ((uintptr_t)cache % 16 != 0) return dg_fail(DG_ERR_BUFFER, "%s: the cache must be 16-byte aligned", what);
     return DG_OK;
 }
