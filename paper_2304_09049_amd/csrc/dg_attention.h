@@ -119,7 +119,7 @@ __device__ __forceinline__ float load_query(const T *row, int g, float (&x)[DIM 
     }
     return row_max(finite ? most : __builtin_inff());
 }
-// The same as operands, times a power of two that takes `most` (finite) into [2^13, 2^14), at most 2^126; `f` takes a score to the base-2 logit.  The
+// The same as operands, times a power of two that takes `most` into [2^13, 2^14), at most 2^126; `f` takes a score to the base-2 logit.  The
 // sum of the operands' numbers over the row.
 template <int BITS, int DIM>
 __device__ __forceinline__ float query_operands(const float (&x)[DIM / 32][8], float most, float scale, v8h (&q)[DIM / 32], float &f)
@@ -211,29 +211,27 @@ struct Rows {
 
     v8h q[N][STEPS];
     v4f o[N][BLOCKS];                                         // sums of weight * code, times 2^10 / R
-    float f, q_sum[N], from_bias[N];
+    float f[N], q_sum[N], from_bias[N];                       // a score's way to the base-2 logit; sums of the operands' numbers
     float shift[N], above[N], l[N], oz[N];                    // sums are relative to 2^shift; of weights, and of weight * z
     float R, per_R;                                           // the power of two that value scales are taken by, and 2^10 over it
     int end[N];                                               // a row sees the tokens before this
     int all_end, any_end;                                     // tokens that every row sees, and that any sees
 
-    // Rows first ... first + have - 1 of a sequence's cached head h (rows that are not there are computed as its first one).  The wavefront's rows are scaled
-    // by one power of two, the one for its largest query: a score's factor is then the token's alone.  (A row whose queries are 2^-10 of another's keeps
-    // 18 bits of them, for logits that are as much smaller.)
+    // Rows first ... first + have - 1 of a sequence's cached head h (rows that are not there are computed as its first one).  Each row is scaled by a power of
+    // two of its own: a softmax is relative to its row, so what a row gives must not go by how large others are.
     __device__ __forceinline__ void begin(const Args &args, const Sequence &seq, int h, int first, int have, int r, int g)
     {
         const DgAttention &a = args.a;
         const int first_i = (int)dg_fdiv((uint32_t)first, args.by_group), last_i = (int)dg_fdiv((uint32_t)(first + max(have, 1) - 1), args.by_group);
         all_end = a.causal ? max(seq.past + first_i + 1, 0) : seq.ctx;
         any_end = have <= 0 ? 0 : a.causal ? max(seq.past + last_i + 1, 0) : seq.ctx;
-        float x[N][STEPS][8], most[N], largest = 0.0f;
+        float x[N][STEPS][8], most[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int at = 16 * n + r;
             const bool there = at < have;
             const int i = there ? (int)dg_fdiv((uint32_t)(first + at), args.by_group) : 0, j = there ? first + at - i * args.group : 0;
             most[n] = load_query<T, DIM>((const T *)a.q + (int64_t)(seq.first + i) * a.q_token + (int64_t)(h * args.group + j) * a.q_head, g, x[n]);
-            largest = fmaxf(largest, there && most[n] < __builtin_inff() ? most[n] : 0.0f);
             end[n] = there && a.causal ? max(seq.past + i + 1, 0) : all_end;
             shift[n] = 0.0f;
             above[n] = NOT_BEGUN;
@@ -241,10 +239,9 @@ struct Rows {
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) o[n][k] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
         }
-        largest = dg_over_lanes<16>(largest, DgMax());
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            q_sum[n] = query_operands<BITS, DIM>(x[n], largest, a.scale, q[n], f);
+            q_sum[n] = query_operands<BITS, DIM>(x[n], most[n], a.scale, q[n], f[n]);
             from_bias[n] = most[n] < __builtin_inff() ? -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum[n] : __builtin_nanf("");
         }
         R = per_R = 0.0f;
@@ -290,17 +287,13 @@ struct Rows {
         }
         // Logits, and their exponentials relative to 2^shift.  That these have grown too large is seen from their sum, which is needed anyway.
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            ks[u] *= f;
-            if (BITS == 4) kz[u] *= f;
-        }
-#pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    score[n][u][e] = __builtin_fmaf(score[n][u][e], ks[u][e], BITS == 8 ? -shift[n] : __builtin_fmaf(q_sum[n], kz[u][e], -shift[n]));
+                    score[n][u][e] = __builtin_fmaf(score[n][u][e], ks[u][e] * f[n],
+                                                    BITS == 8 ? -shift[n] : __builtin_fmaf(q_sum[n], kz[u][e] * f[n], -shift[n]));
         if (!all_seen) {
             branch();
 #pragma unroll
