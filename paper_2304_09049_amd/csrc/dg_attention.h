@@ -33,10 +33,15 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-constexpr float WEIGHT_UNIT = 1024.0f;
-// What a lane's eight weights of a tile may add up to before the shift is raised: p <= 16, so that weights stay below 2^14.  A row that has seen nothing
-// raises it whatever they are.
-constexpr float MOST_SUM = 16.0f, NOT_BEGUN = -1.0f;
+// A token's weight, the second product's operand, is its power 2^(logit - shift) times its value scale.  A row's shift is its own, by what the row sees and how
+// much of the output that is: the first tile's largest weight becomes 2^FIRST_WEIGHT, and the shift is raised, to that again, when a weight passes MOST_WEIGHT.
+// Binary16 then holds weights down to 2^-18 of the largest in full, and counts them down to 2^-28.  (Begun at 2^10 the shift is raised often: 300 x 12 queries on
+// 3000 tokens in 4 bits took 57 us, 2048 on 32768 1550, where 2^4 took 48 and 1490; 2^0 is as 2^4.)
+// Where value scales are so small that the powers would leave binary32, the shift goes by these: 2^FIRST_POWER, and a lane's sum at most MOST_SUM (four lanes,
+// four wavefronts and 256 pieces of it are a number).  A row that has seen nothing raises it whatever they are.
+constexpr float FIRST_WEIGHT = 4.0f, MOST_WEIGHT = 0x1p14f, FIRST_POWER = 104.0f, MOST_SUM = 0x1p110f, NOT_BEGUN = -1.0f;
+// 4 bits: what a lane adds up of power * z stays in binary32, the shift counting 2^-6 of it as a weight (values that are all alike have no scale).
+constexpr float MOST_Z = 0x1p100f;
 
 __device__ __forceinline__ v2h as_halves(uint32_t w) { return __builtin_bit_cast(v2h, w); }
 
@@ -137,8 +142,12 @@ __device__ __forceinline__ float query_operands(const float (&x)[DIM / 32][8], f
     return row_sum(sum);
 }
 
-// The power of two above a value scale, from 2^-100 to 2^126, by its exponent's bits.
-__device__ __forceinline__ uint32_t above_scale(float most) { return min(max((__float_as_uint(most) >> 23) + 1, 27u), 253u); }
+// Half of the factor that takes sums relative to 2^m to 2^top.  Squared, it is for outputs; for the sum of weights it is multiplied twice, because that one counts
+// where the factor is below binary32: 2^m goes by the values' sizes too.
+__device__ __forceinline__ float half_factor(float m, float l, float top)
+{
+    return m == -__builtin_inff() && l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(0.5f * (m - top));       // (a NaN stays one)
+}
 
 // at / by, and at becomes the rest.
 __device__ __forceinline__ uint32_t taken(uint32_t &at, const DgFastDiv &by)
@@ -210,10 +219,9 @@ struct Rows {
     static constexpr bool TWICE = std::is_same<T, _Float16>::value;
 
     v8h q[N][STEPS];
-    v4f o[N][BLOCKS];                                         // sums of weight * code, times 2^10 / R
-    float f[N], q_sum[N], from_bias[N];                       // a score's way to the base-2 logit; sums of the operands' numbers
-    float shift[N], above[N], l[N], oz[N];                    // sums are relative to 2^shift; of weights, and of weight * z
-    float R, per_R;                                           // the power of two that value scales are taken by, and 2^10 over it
+    v4f o[N][BLOCKS];                                         // sums of weight * code
+    float f[N], per_z[N], from_bias[N];                       // what takes a score, and what takes a key's z, to the base-2 logit; where scores start
+    float shift[N], above[N], l[N], oz[N];                    // sums are relative to 2^shift: of powers 2^(logit - shift), and of powers * z
     int end[N];                                               // a row sees the tokens before this
     int all_end, any_end;                                     // tokens that every row sees, and that any sees
 
@@ -241,10 +249,10 @@ struct Rows {
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            q_sum[n] = query_operands<BITS, DIM>(x[n], most[n], a.scale, q[n], f[n]);
-            from_bias[n] = most[n] < __builtin_inff() ? -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * q_sum[n] : __builtin_nanf("");
+            const float sum = query_operands<BITS, DIM>(x[n], most[n], a.scale, q[n], f[n]);
+            from_bias[n] = most[n] < __builtin_inff() ? -(BITS == 8 ? BIAS8 : BIAS4_KEYS) * sum : __builtin_nanf("");
+            per_z[n] = __builtin_amdgcn_fmed3f(sum * f[n], -__FLT_MAX__, __FLT_MAX__);         // (finite: a z of 0 adds nothing)
         }
-        R = per_R = 0.0f;
     }
 
     // The 32 tokens from t0 on, two units one after another in LDS; is0, is1: whether their pages are the cache's.
@@ -285,7 +293,7 @@ struct Rows {
                 for (int n = 0; n < N; ++n) score[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][2 * s + 1], score[n][u], 0, 0, 0);
             }
         }
-        // Logits, and their exponentials relative to 2^shift.  That these have grown too large is seen from their sum, which is needed anyway.
+        // Logits relative to the shift.
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -293,113 +301,106 @@ struct Rows {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     score[n][u][e] = __builtin_fmaf(score[n][u][e], ks[u][e] * f[n],
-                                                    BITS == 8 ? -shift[n] : __builtin_fmaf(q_sum[n], kz[u][e] * f[n], -shift[n]));
+                                                    BITS == 8 ? -shift[n] : __builtin_fmaf(per_z[n], kz[u][e], -shift[n]));
+        // A token's powers, the weights, and what to the outputs comes from z (a code counts as code - 8).
+        float p[N][2][4], x[N][8], xz[N][2][4], y[2][4], sum[N], z[N];
+        if (BITS == 4)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[u][e] = __builtin_fmaf(8.0f, vs[u][e], vz[u][e]);
+        const auto weigh = [&](int n, float by) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[n][u][e] = exp2_(score[n][u][e] - by);
+                    x[n][place(u, e)] = p[n][u][e] * vs[u][e];
+                    if (BITS == 4) xz[n][u][e] = p[n][u][e] * y[u][e];
+                }
+        };
+        // What a row does not see is selected away, whatever it is.
+        const auto hide = [&](int n) {
+            int first = t0 + 4 * g;
+            asm volatile("" : "+v"(first));                                            // (or the places are worked out for every tile)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool seen = ((u ? is1 : is0) ? first + 16 * u + e : INT32_MAX) < end[n];
+                    score[n][u][e] = seen ? score[n][u][e] : -__builtin_inff();
+                    p[n][u][e] = seen ? p[n][u][e] : 0.0f;
+                    x[n][place(u, e)] = seen ? x[n][place(u, e)] : 0.0f;
+                    if (BITS == 4) xz[n][u][e] = seen ? xz[n][u][e] : 0.0f;
+                }
+        };
+        const auto add_up = [&](int n) {
+            sum[n] = p[n][0][0];
+            z[n] = BITS == 4 ? xz[n][0][0] : 0.0f;
+#pragma unroll
+            for (int k = 1; k < 8; ++k) {
+                sum[n] += p[n][k / 4][k % 4];
+                if (BITS == 4) z[n] += xz[n][k / 4][k % 4];
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < N; ++n) weigh(n, 0.0f);
         if (!all_seen) {
             branch();
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int t = (u ? is1 : is0) ? t0 + 16 * u + 4 * g + e : INT32_MAX;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) score[n][u][e] = t < end[n] ? score[n][u][e] : -__builtin_inff();
-                    vs[u][e] = t < any_end ? vs[u][e] : 0.0f;
-                    if (BITS == 4) vz[u][e] = t < any_end ? vz[u][e] : 0.0f;
-                }
+            for (int n = 0; n < N; ++n) hide(n);
         }
-        float p[N][2][4], sum[N];
+        bool raise[N], any_raise = false;
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) {
+            add_up(n);
+            float most = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[n][k]));
+            raise[n] = (most > MOST_WEIGHT) | (l[n] + sum[n] > above[n]);                        // (| : || would be branches of its own)
+            if (BITS == 4) raise[n] |= !(fabsf(oz[n] + z[n]) <= MOST_Z);
+            any_raise |= raise[n];
+        }
+        if (__any(any_raise)) {
+            float size[2][4];                                                          // log2 of what a weight is its power times
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[n][u][e] = exp2_(score[n][u][e]);
-                    sum[n] = u + e == 0 ? p[n][0][0] : sum[n] + p[n][u][e];
-                }
-        bool raise = false;
-#pragma unroll
-        for (int n = 0; n < N; ++n) raise = raise || sum[n] > above[n];
-        if (__any(raise)) {
+                for (int e = 0; e < 4; ++e) size[u][e] = __builtin_amdgcn_logf(BITS == 8 ? fabsf(vs[u][e]) : fmaxf(fabsf(vs[u][e]), fabsf(y[u][e]) * 0x1p-6f));
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                float high = -__builtin_inff();
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) high = fmaxf(high, score[n][u][e]);
-                high = row_max(high);
-                const bool begun = above[n] == MOST_SUM;
-                const float by = begun ? fmaxf(high, 0.0f) : high == -__builtin_inff() ? 0.0f : high;
-                const float keep = begun ? exp2_(-by) : 0.0f;                          // (nothing is summed before)
-                shift[n] += by;
-                above[n] = begun || high > -__builtin_inff() ? MOST_SUM : NOT_BEGUN;
-                l[n] *= keep;
-                oz[n] *= keep;
-                sum[n] = 0.0f;
+                // (only the rows that ask for it: a row's bits do not go by its neighbours)
+                const bool mine = row_max(raise[n] ? 1.0f : 0.0f) > 0.0f, full = row_max(l[n] + sum[n]) > MOST_SUM;
+                float high = -__builtin_inff(), power = -__builtin_inff();
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        p[n][u][e] = exp2_(score[n][u][e] - by);
-                        sum[n] += p[n][u][e];
+                        power = fmaxf(power, score[n][u][e]);
+                        high = fmaxf(high, score[n][u][e] + size[u][e]);
                     }
+                power = row_max(power);
+                high = fmaxf(row_max(high) - FIRST_WEIGHT, power - FIRST_POWER);
+                const bool begun = above[n] == MOST_SUM, nothing = high == -__builtin_inff();
+                const float by = !mine || nothing ? 0.0f : begun ? fmaxf(high, full ? 8.0f : 0.0f) : high;
+                const float half = begun ? exp2_(-0.5f * by) : 0.0f, keep = half * half;          // (nothing is summed before)
+                shift[n] += by;
+                above[n] = begun || (mine && !nothing) ? MOST_SUM : NOT_BEGUN;
+                l[n] = l[n] * half * half;
+                oz[n] *= keep;
+                weigh(n, by);
+                if (!all_seen) hide(n);
+                add_up(n);
 #pragma unroll
                 for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
             }
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) l[n] += sum[n];
-        float most_vs = 0.0f;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) most_vs = fmaxf(most_vs, fabsf(vs[u][e]));
-        if (__any(most_vs > R)) {
-            most_vs = row_max(most_vs);                                                // (a lane's tokens are those of its row of lanes)
-            const uint32_t bits = above_scale(most_vs);
-            const float inverse = __uint_as_float((254u - bits) << 23), keep = R * inverse;
-            R = __uint_as_float(bits << 23);
-            per_R = inverse * WEIGHT_UNIT;
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int k = 0; k < BLOCKS; ++k) o[n][k] *= keep;
+        for (int n = 0; n < N; ++n) {
+            l[n] += sum[n];
+            oz[n] += z[n];
         }
         // The weights as the second product's operand.
-        float x[N][8], xz[BITS == 4 ? N : 1][8];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float by = vs[u][e] * per_R, z = BITS == 4 ? __builtin_fmaf(8.0f, vs[u][e], vz[u][e]) : 0.0f;
-                const int at = place(u, e);
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    x[n][at] = p[n][u][e] * by;
-                    if (BITS == 4) xz[n][at] = p[n][u][e] * z;
-                }
-            }
-        if (!all_seen) {
-            // (what only others of the rows see may be a NaN, and 0 times that one too)
-            branch();
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        const bool seen = t0 + 16 * u + 4 * g + e < end[n];
-                        const int at = place(u, e);
-                        x[n][at] = seen ? x[n][at] : 0.0f;
-                        if (BITS == 4) xz[n][at] = seen ? xz[n][at] : 0.0f;
-                    }
-        }
-        if (BITS == 4)
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) oz[n] += xz[n][k];
         v8h weights[N], rests[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -475,10 +476,9 @@ struct Rows {
     }
     __device__ __forceinline__ v4f channels(int n, int k, int e, float by, float z) const
     {
-        const float unit = R == 0.0f ? 1.0f : R * (1.0f / WEIGHT_UNIT) * by;               // (nothing met: 0, or the NaN of a NaN)
         v4f x;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = BITS == 4 ? __builtin_fmaf(o[n][4 * k + c][e], unit, z) : o[n][4 * k + c][e] * unit;
+        for (int c = 0; c < 4; ++c) x[c] = BITS == 4 ? __builtin_fmaf(o[n][4 * k + c][e], by, z) : o[n][4 * k + c][e] * by;
         return x;
     }
 };

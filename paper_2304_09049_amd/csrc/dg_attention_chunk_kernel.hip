@@ -14,7 +14,7 @@ namespace {
 constexpr int WAVES = 4, N = CHUNK_ROWS / (16 * WAVES);
 
 template <class T, int BITS, int DIM>
-__global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : 2) void attention_chunk_kernel(Args args)
+__global__ __launch_bounds__(64 * WAVES, DIM == 256 ? 1 : DIM == 64 ? 3 : 2) void attention_chunk_kernel(Args args)
 {
     typedef Unit<BITS, DIM> U;
     constexpr int RING = DIM == 256 && BITS == 8 ? 2 : 3, STAGE = 4 * U::BYTES;

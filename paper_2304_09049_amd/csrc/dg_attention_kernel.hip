@@ -7,9 +7,9 @@
 //
 // Numbers: codes become binary16 exactly.  A query row is scaled by a power of
 // two to a largest magnitude in [2^13, 2^14), so that bfloat16's range fits binary16 and nothing above 2^-28 of the row's largest loses a
-// bit.  Scores, shifts, sums and outputs are binary32.  A weight is rounded once, to binary16, as p * (value scale / R) * 2^10, where R is
-// a power of two no smaller than any value scale met so far: what is 2^-34 of the largest is still counted.  p = 2^(logit - shift); the shift is
-// the first tile's maximum, and is raised only when eight of a lane's weights add up to more than 16: any p is then at most 16, and weights stay below 2^15.
+// bit.  Scores, shifts, sums and outputs are binary32.  A weight is rounded once, to binary16 (twice, with what that left off, for binary16 outputs), as
+// 2^(logit - shift) times the token's value scale, the row's largest being kept between 2^4 and 2^14: what is 2^-28 of it is still counted.  Nothing of this
+// goes by other rows, or by what a row does not see: a row's bits are the same whatever stands beside it.
 //
 // What bounds it: for single tokens the cache's bytes, read once (one context of 131071 tokens, 32 heads on 8 of 128 channels, 8 bits: 59 us, 4.7 TB/s; 64 contexts of
 // up to 8192, 4 bits: 82 us, 3.7 TB/s: there the vector unit is as busy, 16 columns of a product for the 4 rows that there are), or, for short contexts, two launches
@@ -31,7 +31,7 @@ struct Kept {
     static constexpr int TILE_BYTES = 2 * Unit<BITS, DIM>::BYTES, LOADS = 2 * Unit<BITS, DIM>::LOADS;
     static constexpr int DEPTH = WAVES * 2 * TILE_BYTES <= 40960 ? 2 : 1, RINGS = WAVES * DEPTH * TILE_BYTES;
     static constexpr int SHARES = WAVES * 16 * (DIM + 4) * 4;
-    static constexpr int WAVES_PER_SIMD = DIM == 256 ? 1 : N == 2 ? 2 : DIM == 128 && BITS == 4 ? 3 : 4;
+    static constexpr int WAVES_PER_SIMD = DIM == 256 ? 1 : N == 2 ? (DIM == 64 ? 3 : 2) : DIM == 128 && BITS == 4 ? 3 : 4;
 };
 
 // 16 N rows of a cached head and a piece of the context by a workgroup, whose wavefronts take a tile in turn.
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(64 * WAVES, (Kept<BITS, DIM, N>::WAVES_PER_SIMD)) v
         float most = wave_m[0][r];
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) most = fmaxf(most, wave_m[k][r]);
-        const float mine = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);       // (a NaN stays one)
-        if (g == 0) wave_l[wave][r] = l * mine;
+        const float half = half_factor(m, l, most), mine = half * half;
+        if (g == 0) wave_l[wave][r] = l * half * half;
         if (16 * n + r < have)
 #pragma unroll
             for (int k = 0; k < DIM / 64; ++k)
@@ -173,9 +173,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args args)
     if (lane == 0) wave_max[wave] = most;
     __syncthreads();
     most = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
-    const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
-    weight[threadIdx.x] = w;
-    float total = dg_over_wave(l * w, DgAdd());
+    const float half = half_factor(m, l, most);
+    weight[threadIdx.x] = half * half;
+    float total = dg_over_wave(l * half * half, DgAdd());
     if (lane == 0) wave_sum[wave] = total;
     __syncthreads();
     v4f o = {};
@@ -210,8 +210,8 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(Args args)
     const bool mine = lane < args.pieces;
     const float m = mine ? args.shares.m[lane * rows + at] : -__builtin_inff(), l = mine ? args.shares.l[lane * rows + at] : 0.0f;
     const float most = dg_over_wave(m, DgMax());
-    const float w = m == -__builtin_inff() && l == 0.0f ? 0.0f : exp2_(m - most);
-    float total = dg_over_wave(l * w, DgAdd());
+    const float half = half_factor(m, l, most), w = half * half;
+    float total = dg_over_wave(l * half * half, DgAdd());
     float o[PER] = {};
     const float *from = args.shares.o + at * DIM + PER * lane;
     for (int k = 0; k < args.pieces; ++k) {
