@@ -435,7 +435,7 @@ size_t dg_cache_bytes(const dg_cache_desc *desc);
 /*
  * Quantise T tokens' keys and values ([T][heads][dim] of `type`, token and head strides apart, channels contiguous) into slots_dev[T].  A
  * negative slot, or one past the cache, is skipped; the other slots must differ from one another.  Nothing else in the cache changes.
- * Errors: DG_ERR_NULL; DG_ERR_SHAPE; DG_ERR_RANGE (slots, pages or caches too large); DG_ERR_UNSUPPORTED (bits, dim, type); DG_ERR_BUFFER
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (T * heads of 2^31 and more besides); DG_ERR_RANGE (slots, pages or caches too large, heads beyond 2^24); DG_ERR_UNSUPPORTED (bits, dim, type); DG_ERR_BUFFER
  * (cache_bytes, alignment).
  */
 dg_status dg_cache_write(const dg_cache_desc *desc, void *cache_dev, size_t cache_bytes, const void *k_dev, const void *v_dev, dg_dtype type,

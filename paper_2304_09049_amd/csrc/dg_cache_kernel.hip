@@ -301,28 +301,40 @@ void with_form(const DgCache &c, dg_dtype type, F f)
 // 25.1; 1024 3.85 either way; 256 3.6, by sixteen 3.2).
 static bool many(int64_t T, int32_t heads) { return T * heads >= 8192; }
 
-dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t T, const int64_t strides[4],
+// Tokens a launch takes: whole eights, so that what a wavefront leaves to the next one stays with it, and at most 2^26 (token, head) rows, 16 threads each.
+static int64_t tokens_a_launch(int32_t heads) { return std::max<int64_t>(((int64_t)1 << 26) / heads / 8 * 8, 8); }
+
+dg_status dg_launch_cache_write(const DgCache &c, const void *k, const void *v, dg_dtype type, int64_t tokens, const int64_t strides[4],
                                 const int32_t *slots, hipStream_t stream)
 {
-    const WriteArgs a = {c, k, v, strides[0], strides[1], strides[2], strides[3], slots, T};
-    with_form(c, type, [&](auto t, auto bits, auto dim) {
-        constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
-        if (many(T, c.heads)) cache_write_kernel<decltype(t), BITS, DIM, 8><<<(uint32_t)(((T + 7) / 8 * c.heads + 3) / 4), 256, 0, stream>>>(a);
-        else cache_write_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+    const int64_t size = dg_type_size(type);
+    dg_in_turns(tokens, tokens_a_launch(c.heads), [&](int64_t first, int64_t T) {
+        const WriteArgs a = {c, (const uint8_t *)k + first * strides[0] * size, (const uint8_t *)v + first * strides[2] * size, strides[0], strides[1], strides[2], strides[3],
+                             slots + first, T};
+        with_form(c, type, [&](auto t, auto bits, auto dim) {
+            constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
+            if (many(T, c.heads)) cache_write_kernel<decltype(t), BITS, DIM, 8><<<(uint32_t)(((T + 7) / 8 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+            else cache_write_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+        });
+        return DG_OK;
     });
     return dg_check_launch("dg_cache_write");
 }
 
-dg_status dg_launch_cache_read(const DgCache &c, const int32_t *slots, int64_t T, void *k, void *v, dg_dtype type, hipStream_t stream)
+dg_status dg_launch_cache_read(const DgCache &c, const int32_t *slots, int64_t tokens, void *k, void *v, dg_dtype type, hipStream_t stream)
 {
-    const ReadArgs a = {c, k, v, slots, T};
-    with_form(c, type, [&](auto t, auto bits, auto dim) {
-        constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
-        // Sixteen lanes a token, which then store 16 bytes each side by side (16384 tokens x 8 heads x 128 channels, 8 bits 30 us, by eight 45; 4096 10.6,
-        // 16.2); eight for many of 64 channels in 4 bits, where a lane of sixteen would have two bytes (16384 written and read 31.3 us, by sixteen 35.0).
-        constexpr int LANES = BITS == 4 && DIM == 64 ? 8 : 16;
-        if (many(T, c.heads)) cache_read_kernel<decltype(t), BITS, DIM, LANES><<<(uint32_t)(((T + 64 / LANES - 1) / (64 / LANES) * c.heads + 3) / 4), 256, 0, stream>>>(a);
-        else cache_read_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+    const int64_t token = c.heads * c.dim * dg_type_size(type);
+    dg_in_turns(tokens, tokens_a_launch(c.heads), [&](int64_t first, int64_t T) {
+        const ReadArgs a = {c, k ? (uint8_t *)k + first * token : nullptr, v ? (uint8_t *)v + first * token : nullptr, slots + first, T};
+        with_form(c, type, [&](auto t, auto bits, auto dim) {
+            constexpr int BITS = decltype(bits)::value, DIM = decltype(dim)::value;
+            // Sixteen lanes a token, which then store 16 bytes each side by side (16384 tokens x 8 heads x 128 channels, 8 bits 30 us, by eight 45; 4096 10.6,
+            // 16.2); eight for many of 64 channels in 4 bits, where a lane of sixteen would have two bytes (16384 written and read 31.3 us, by sixteen 35.0).
+            constexpr int LANES = BITS == 4 && DIM == 64 ? 8 : 16;
+            if (many(T, c.heads)) cache_read_kernel<decltype(t), BITS, DIM, LANES><<<(uint32_t)(((T + 64 / LANES - 1) / (64 / LANES) * c.heads + 3) / 4), 256, 0, stream>>>(a);
+            else cache_read_kernel<decltype(t), BITS, DIM, 16><<<(uint32_t)(((T + 3) / 4 * c.heads + 3) / 4), 256, 0, stream>>>(a);
+        });
+        return DG_OK;
     });
     return dg_check_launch("dg_cache_read");
 }

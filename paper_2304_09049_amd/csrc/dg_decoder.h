@@ -2,6 +2,8 @@
 // cache's layout and the launchers.  Internal; the public ABI is include/deepgemm_hip.h.
 #pragma once
 
+#include <algorithm>
+
 #include "dg_common.h"
 
 // ---- element types -----------------------------------------------------------------------------------------------------
@@ -163,6 +165,17 @@ __device__ __forceinline__ uint32_t dg_value_byte(uint32_t t, uint32_t d, uint32
 }
 
 // ---- launchers (each validates nothing: the API layer has done that) ---------------------------------------------------
+
+// f(first, count) for `total` rows, `most` a launch: HIP counts a grid's threads in 32 bits, and the kernels count rows in them.
+template <class F>
+dg_status dg_in_turns(int64_t total, int64_t most, F f)
+{
+    for (int64_t first = 0; first < total; first += most) {
+        const dg_status s = f(first, std::min(most, total - first));
+        if (s) return s;
+    }
+    return DG_OK;
+}
 
 // pad: K, or up to where a row's codes are cleared
 dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, int8_t *codes,

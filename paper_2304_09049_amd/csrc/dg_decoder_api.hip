@@ -54,10 +54,11 @@ dg_status check_cache(const char *what, const dg_cache_desc *d, const void *cach
     return DG_OK;
 }
 
-// (token, head) rows, a fourth of which have to fit a grid
+// (token, head) rows; eight tokens' have to fit a launch, which a call has as many of as it takes
 dg_status check_cache_tokens(const char *what, const dg_cache_desc *d, dg_dtype type, int64_t T, const int32_t *slots)
 {
     if (!known_type(type)) return dg_fail(DG_ERR_UNSUPPORTED, "%s: unknown element type %d", what, (int)type);
+    if (d->heads > 1 << 24) return dg_fail(DG_ERR_RANGE, "%s: %d heads (at most 2^24)", what, (int)d->heads);
     if (T < 0 || T > MOST_ROWS / d->heads) return dg_fail(DG_ERR_SHAPE, "%s: %lld tokens of %d heads", what, (long long)T, (int)d->heads);
     if (T > 0 && !slots) return dg_fail(DG_ERR_NULL, "%s: NULL slots", what);
     return DG_OK;

@@ -547,8 +547,11 @@ dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int
         typedef decltype(t) T;
         const auto launch = [&](auto threads, auto held) {
             constexpr int THREADS = decltype(threads)::value;
-            quantize_tokens_kernel<T, THREADS, decltype(held)::value><<<(uint32_t)N, THREADS, 0, stream>>>((const T *)x, (int32_t)K, (int32_t)pad, stride_n,
-                                                                                                         codes, stride_codes, scale);
+            dg_in_turns(N, 1 << 21, [&](int64_t n, int64_t count) {
+                quantize_tokens_kernel<T, THREADS, decltype(held)::value><<<(uint32_t)count, THREADS, 0, stream>>>((const T *)x + n * stride_n, (int32_t)K, (int32_t)pad,
+                                                                                                               stride_n, codes + n * stride_codes, stride_codes, scale + n);
+                return DG_OK;
+            });
         };
         const auto by_length = [&](auto threads) {
             const int64_t step = decltype(threads)::value * (16 / sizeof(T));
@@ -569,38 +572,63 @@ dg_status dg_launch_quantize_tokens(const void *x, dg_dtype type, int64_t N, int
 
 bool dg_linear_i8_fuses(int64_t N, int64_t K) { return N == 1 && K <= FUSED_BYTES; }
 
-dg_status dg_launch_linear_i8_fused(const DgGemmI8 &p, const void *x, dg_dtype x_type, dg_dtype type, hipStream_t stream)
+// f(a part of the product): channels and tokens whose workgroups, tiles of 2^16 results where there are many of both, are a grid.
+template <class F>
+static dg_status in_parts(const DgGemmI8 &p, dg_dtype type, F f)
 {
-    dg_with_type(type, [&](auto t) {
-        dg_with_type(x_type, [&](auto s) {
-            const Fused<decltype(s)> f = {(const decltype(s) *)x, (p.K + 127) / 128 * 128};
-            const uint32_t blocks = (p.M + 15) / 16, room = f.pitch;
-            if (few_channels(p, dg_simd_count() / 4)) gemm_i8_few_kernel<decltype(t), decltype(s), 16, 1, 1, true><<<blocks, 1024, room, stream>>>(p, f);
-            else gemm_i8_few_kernel<decltype(t), decltype(s), 8, 1, 1, true><<<blocks, 512, room, stream>>>(p, f);
+    return dg_in_turns(p.M, 1 << 24, [&](int64_t m, int64_t channels) {
+        return dg_in_turns(p.N, std::min<int64_t>(1 << 24, ((int64_t)1 << 38) / channels), [&](int64_t n, int64_t tokens) {
+            DgGemmI8 part = p;
+            part.W += m * p.stride_w;
+            part.scale_m += m;
+            part.bias = p.bias ? p.bias + m : nullptr;
+            part.A += n * p.stride_a;
+            part.scale_n += n;
+            part.out = (uint8_t *)p.out + (n * p.stride_out + m) * dg_type_size(type);
+            part.M = (int32_t)channels;
+            part.N = (int32_t)tokens;
+            f(part);
+            return DG_OK;
+        });
+    });
+}
+
+dg_status dg_launch_linear_i8_fused(const DgGemmI8 &all, const void *x, dg_dtype x_type, dg_dtype type, hipStream_t stream)
+{
+    in_parts(all, type, [&](const DgGemmI8 &p) {
+        dg_with_type(type, [&](auto t) {
+            dg_with_type(x_type, [&](auto s) {
+                const Fused<decltype(s)> f = {(const decltype(s) *)x, (p.K + 127) / 128 * 128};
+                const uint32_t blocks = (p.M + 15) / 16, room = f.pitch;
+                if (few_channels(p, dg_simd_count() / 4)) gemm_i8_few_kernel<decltype(t), decltype(s), 16, 1, 1, true><<<blocks, 1024, room, stream>>>(p, f);
+                else gemm_i8_few_kernel<decltype(t), decltype(s), 8, 1, 1, true><<<blocks, 512, room, stream>>>(p, f);
+                return 0;
+            });
             return 0;
         });
-        return 0;
     });
     return dg_check_launch("dg_linear_i8");
 }
 
-dg_status dg_launch_gemm_i8(const DgGemmI8 &p, dg_dtype type, hipStream_t stream)
+dg_status dg_launch_gemm_i8(const DgGemmI8 &all, dg_dtype type, hipStream_t stream)
 {
-    dg_with_type(type, [&](auto t) {
-        typedef decltype(t) T;
-        switch (form_of(p)) {
-        case Form::Few:
-            if (p.N <= 16) launch_few<T, 1>(p, stream);
-            else launch_few<T, 2>(p, stream);
-            break;
-        case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
-        case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
-        case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
-        case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
-        case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
-        case Form::Tile256x256: launch_tiles<T, 2, 4, 4, 2, 1, 2>(p, stream); break;
-        }
-        return 0;
+    in_parts(all, type, [&](const DgGemmI8 &p) {
+        dg_with_type(type, [&](auto t) {
+            typedef decltype(t) T;
+            switch (form_of(p)) {
+            case Form::Few:
+                if (p.N <= 16) launch_few<T, 1>(p, stream);
+                else launch_few<T, 2>(p, stream);
+                break;
+            case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
+            case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
+            case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
+            case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
+            case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
+            case Form::Tile256x256: launch_tiles<T, 2, 4, 4, 2, 1, 2>(p, stream); break;
+            }
+            return 0;
+        });
     });
     return dg_check_launch("dg_gemm_i8");
 }

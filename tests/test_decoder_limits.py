@@ -34,3 +34,11 @@ def test_a_large_page_needs_its_bytes():
     write = lambda n: dg.lib().dg_cache_write(ctypes.byref(d), FAKE, n, None, None, 0, 1, 256, 256, 256, 256, FAKE, None)  # noqa: E731
     assert write(cache_bytes(1, 2097152, 1, 256, 8) - 1) == BUFFER and write(16777216) == BUFFER
     assert write(cache_bytes(1, 2097152, 1, 256, 8)) == 1                  # enough: what is wrong now is a NULL
+
+
+def test_more_heads_than_a_launch_takes():
+    d = dg.cache_desc(1, 16, (1 << 24) + 1, 64, 8)
+    size = dg.dg_cache_bytes(d)
+    assert size == cache_bytes(1, 16, (1 << 24) + 1, 64, 8)
+    assert dg.lib().dg_cache_write(ctypes.byref(d), FAKE, size, FAKE, FAKE, 0, 1, 64, 64, 64, 64, FAKE, None) == RANGE
+    assert dg.lib().dg_cache_read(ctypes.byref(d), FAKE, size, FAKE, 1, FAKE, FAKE, 0, None) == RANGE

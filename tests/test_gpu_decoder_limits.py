@@ -40,3 +40,78 @@ def test_one_large_page(page_size, dim, bits):
                                 torch.zeros(1, 1, dtype=torch.int32, device="cuda"), 3, 33)
     exact, off = attention(q.float().numpy(), want[0][:33], want[1][:33], 30, dim ** -0.5, True, 2.0 ** -11)
     assert (np.abs(out.float().cpu().numpy() - exact) <= off).all()
+
+
+# A grid has fewer than 2^32 threads on an axis: these calls are more than one launch.
+
+
+def test_more_tokens_than_a_launch_quantises():
+    N = (1 << 24) + 1000
+    x = (torch.arange(N, device="cuda", dtype=torch.int32) % 251 + 1).half()[:, None] * torch.tensor([1.0, -1.0, 0.0, 1.0], device="cuda").half()
+    codes, scale = dg.dg_quantize_tokens(x)
+    assert torch.equal(scale, x[:, 0].float() / torch.full((), 127.0, device="cuda"))
+    assert (codes == torch.tensor([127, -127, 0, 127], dtype=torch.int8, device="cuda")).all()
+
+
+@pytest.mark.parametrize("N,fused", [(1, False), (1, True), (20, False)])
+def test_more_channels_than_a_launch_multiplies(N, fused):
+    M, K = (1 << 27) + 100, 16
+    W = torch.zeros(M, K, dtype=torch.int8, device="cuda")
+    step = torch.arange(M, device="cuda", dtype=torch.int32)
+    W[:, 3], W[:, 9] = (step % 127).to(torch.int8), (step // 127 % 97).to(torch.int8)
+    A = torch.zeros(N, K, dtype=torch.int8, device="cuda")
+    A[:, 3], A[:, 9] = 127, 1
+    sm = torch.ones(M, device="cuda")
+    sm[-50:] = 2.0
+    want = 127.0 * (step % 127).float() + (step // 127 % 97).float()
+    want[-50:] *= 2
+    if fused:
+        x = A.float()                                            # (its scale is 127 / 127: its codes are A)
+        got = dg.dg_linear_i8(W, x, sm)
+    else:
+        got = dg.dg_gemm_i8(W, A, sm, torch.ones(N, device="cuda"), dtype="float32")
+    for n in {0, N - 1}:
+        assert torch.equal(got[n], want)
+
+
+def test_more_tokens_than_a_launch_multiplies():
+    N, K = (1 << 29) + 100, 3
+    held = torch.zeros(N, K, dtype=torch.int8, device="cuda")
+    step = torch.arange(N, device="cuda", dtype=torch.int32)
+    held[:, 1] = (step % 113).to(torch.int8)
+    W = torch.tensor([[5, 1, 7], [0, -2, 0]], dtype=torch.int8, device="cuda")
+    got = dg.dg_gemm_i8(W, held, torch.ones(2, device="cuda"), torch.ones(1, device="cuda").expand(N).contiguous(), dtype="float16")
+    want = (step % 113).half()
+    assert torch.equal(got[:, 0], want) and torch.equal(got[:, 1], -2 * want)
+
+
+def test_more_rows_than_a_launch_writes():
+    T, heads = (1 << 26) + 37, 8
+    desc = dg.cache_desc(4, 16, heads, 64, 4)
+    cache = torch.zeros(dg.dg_cache_bytes(desc), dtype=torch.uint8, device="cuda")
+    slots = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    mine = [0, 5, 1 << 23, (1 << 23) + 1, (1 << 25) + 7, T - 2, T - 1]
+    slots[torch.tensor(mine, device="cuda")] = torch.arange(len(mine), dtype=torch.int32, device="cuda") * 7
+    x = torch.randn(1, heads, 64, generator=torch.Generator().manual_seed(0)).half()
+    one = x.cuda().expand(T, heads, 64)                          # (the same keys for every token, without the bytes)
+    dg.dg_cache_write(desc, cache, one, one, slots)
+    small = Cache(4, 16, heads, 64, 4)
+    small.write(np.arange(len(mine)) * 7, *(x.float().numpy().repeat(len(mine), 0) for _ in range(2)))
+    assert np.array_equal(cache.cpu().numpy(), small.bytes)
+
+
+def test_more_rows_than_a_launch_reads():
+    T, heads = (1 << 25) + 37, 8
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("not enough memory free")
+    desc = dg.cache_desc(4, 16, heads, 64, 4)
+    cache = torch.zeros(dg.dg_cache_bytes(desc), dtype=torch.uint8, device="cuda")
+    k = torch.randn(64, heads, 64, generator=torch.Generator().manual_seed(0)).half().cuda()
+    at = torch.arange(64, dtype=torch.int32, device="cuda")
+    dg.dg_cache_write(desc, cache, k, k, at)
+    want, _ = dg.dg_cache_read(desc, cache, at, torch.empty_like(k), None)
+    slots = torch.arange(T, device="cuda", dtype=torch.int32) * 7 % 64
+    got = torch.empty(T, heads, 64, dtype=torch.float16, device="cuda")
+    dg.dg_cache_read(desc, cache, slots, got, None)
+    for first in range(0, T, 1 << 22):
+        assert torch.equal(got[first:first + (1 << 22)], want[slots[first:first + (1 << 22)].long()])
