@@ -31,7 +31,13 @@ class PagedSequences:
         self.free = list(range(desc.pages))[::-1]
 
     def extend(self, new):
-        """Room for new[b] more tokens of each sequence -> (slots of the new tokens, q_start, ctx_len, table) on the device."""
+        """Room for new[b] more tokens of each sequence -> (slots of the new tokens, q_start, ctx_len, table) on the device.  Nothing changes where
+        the pages do not suffice (MemoryError)."""
+        if len(new) != len(self.pages) or min(new, default=0) < 0:
+            raise ValueError(f"new tokens {list(new)} for {len(self.pages)} sequences")
+        need = sum(-(-(length + n) // self.desc.page_size) - len(pages) for length, n, pages in zip(self.lengths, new, self.pages))
+        if need > len(self.free):
+            raise MemoryError(f"{need} more pages are needed, {len(self.free)} of {self.desc.pages} are free")
         slots, starts = [], [0]
         for b, n in enumerate(new):
             while len(self.pages[b]) * self.desc.page_size < self.lengths[b] + n:

@@ -104,7 +104,7 @@ def test_more_rows_than_a_launch_reads():
     T, heads = (1 << 25) + 37, 8
     if torch.cuda.mem_get_info()[0] < 60 << 30:
         pytest.skip("not enough memory free")
-    desc = dg.cache_desc(4, 16, heads, 64, 4)
+    desc = dg.cache_desc(4, 16, heads, 64, 8)
     cache = torch.zeros(dg.dg_cache_bytes(desc), dtype=torch.uint8, device="cuda")
     k = torch.randn(64, heads, 64, generator=torch.Generator().manual_seed(0)).half().cuda()
     at = torch.arange(64, dtype=torch.int32, device="cuda")
