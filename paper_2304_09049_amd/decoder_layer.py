@@ -80,10 +80,12 @@ class DecoderLayer:
         q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)          # (views: heads and tokens keep their strides)
         dg.dg_cache_write(sequences.desc, sequences.cache, k, v, slots)
         attended = dg.dg_paged_attention(sequences.desc, sequences.cache, q, q_start, ctx_len, table, max(new), max(sequences.lengths))
-        return x + dg.dg_linear_i8(self.out, attended.view(tokens, -1), self.out_scale)
+        return x + dg.dg_linear_i8(self.out, attended.view(tokens, self.heads * self.dim), self.out_scale)
 
     def feed_forward(self, h):
         M, K = self.ff_shape
+        if not h.shape[0]:                                        # (the calls around the tables take one row at least)
+            return torch.empty(0, M, dtype=h.dtype, device=h.device)
         packed = dg.dg_quantize_pack_activations(h.float(), h.shape[0], K, 1 / self.ff_step, 0.0, -2)
         y = torch.empty(h.shape[0], M, dtype=torch.float32, device=h.device)
         dg.dg_gemm_lut(self.lut, self.ff, packed, M, h.shape[0], K, out=y, scale=self.ff_scale * self.ff_step, strides=(1, M))
