@@ -61,12 +61,18 @@ class DecoderLayer:
         self.heads, self.kv_heads, self.dim, self.ff_step = heads, kv_heads, dim, ff_step
         self.qkv, self.qkv_scale = dg.dg_quantize_tokens(w_qkv)
         self.out, self.out_scale = dg.dg_quantize_tokens(w_out)
-        # 2 bits: code + level 0 -> -2, so that the four levels -2, -1, 0, 1 times the scale cover a channel
         self.ff_shape = w_ff.shape
-        self.ff_scale = w_ff.abs().amax(1) / 2
-        codes = torch.clamp(torch.round(w_ff / self.ff_scale[:, None]), -2, 1) + 2
-        self.ff = dg.dg_pack_weights(codes.to(torch.uint8).contiguous(), *self.ff_shape)
+        codes, self.ff_scale = self.two_bits(w_ff)
+        self.ff = dg.dg_pack_weights(codes, *self.ff_shape)
         self.lut = dg.dg_build_lut(self.LEVELS_W, self.LEVELS_A)
+
+    @staticmethod
+    def two_bits(w):
+        """Codes [out][in] and scales [out] of float32 weights: code + level 0 -> -2, so that the four levels -2, -1, 0, 1 times the scale cover a channel; a
+        channel of zeros has level 0 and scale 0."""
+        scale = w.abs().amax(1) / 2
+        codes = torch.clamp(torch.round(w / torch.where(scale > 0, scale, 1.0)[:, None]), -2, 1) + 2
+        return codes.to(torch.uint8).contiguous(), scale
 
     def step(self, x, sequences: PagedSequences, new):
         """x: [sum(new)][hidden] of the new tokens, sequence after sequence, float16 or bfloat16 -> the layer's output, the same shape."""

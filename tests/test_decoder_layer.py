@@ -1,8 +1,9 @@
 """The example layer's bookkeeping, without a GPU."""
 import pytest
+import torch
 
 from paper_2304_09049_amd import binding as dg
-from paper_2304_09049_amd.decoder_layer import PagedSequences
+from paper_2304_09049_amd.decoder_layer import DecoderLayer, PagedSequences
 
 
 def test_pages_go_to_the_sequences_as_tokens_come():
@@ -30,3 +31,10 @@ def test_a_pool_that_does_not_suffice_stays_as_it_was():
     assert ([list(p) for p in s.pages], list(s.lengths), list(s.free)) == before
     s.extend([1, 13])
     assert s.lengths == [17, 16] and not s.free
+
+
+def test_two_bit_weights_of_channels_that_are_zero():
+    w = torch.tensor([[2.0, -2.0, 0.4, -1.2], [0.0, 0.0, 0.0, 0.0], [0.0, 0.0, -1e-30, 0.0]])
+    codes, scale = DecoderLayer.two_bits(w)
+    assert codes.dtype == torch.uint8 and codes.tolist() == [[3, 0, 2, 1], [2, 2, 2, 2], [2, 2, 0, 2]]
+    assert scale.tolist() == [1.0, 0.0, w[2, 2].abs().item() / 2]

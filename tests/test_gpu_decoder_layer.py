@@ -24,3 +24,15 @@ def test_a_step_without_new_tokens():
     none = layer.step(x[:0], sequences, [0, 0])
     assert none.shape == (0, 256) and none.dtype == x.dtype
     assert torch.equal(sequences.cache, held) and sequences.lengths == [2, 3] and first.isfinite().all()
+
+
+def test_a_feed_forward_channel_of_zeros():
+    def change(w):
+        w[7] = 0
+        return w
+    layer, desc = layer_of(change)
+    sequences = PagedSequences(desc, 1, torch.device("cuda"))
+    x = torch.randn(20, 256, device="cuda").half()
+    h = layer.attend(x, sequences, [20])
+    y = layer.feed_forward(h)
+    assert y.isfinite().all() and (y[:, 7] == 0).all() and (y[:, 8] != 0).any()
