@@ -453,7 +453,7 @@ dg_status dg_cache_read(const dg_cache_desc *desc, const void *cache_dev, size_t
  * it sees, 0 if that is nothing.  One new token each is a decode step; a prompt, a chunk of one, drafted tokens, or queries over an
  * encoder's states (causal = 0) are the same call.
  * q_start[B + 1], ctx_len[B] and the table are device memory and are not checked on the host: token numbers are held to 0 ... T, a context
- * to the table's width, and a page number that is none of the cache's hides its tokens, as does nothing else.  max_q: no sequence has more new tokens
+ * to the table's width and to 2^31 - 65537, and a page number that is none of the cache's hides its tokens, as does nothing else.  max_q: no sequence has more new tokens
  * (later ones get no output).  max_ctx: about the longest context; how the work is cut goes by it, results are right whatever it is.
  * Codes enter the matrix instructions exactly; scores, softmax and sums are binary32; weights are rounded once, to binary16 with a scale of
  * their own (to two binary16 numbers for binary16 outputs).

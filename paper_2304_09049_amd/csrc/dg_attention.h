@@ -157,6 +157,10 @@ __device__ __forceinline__ uint32_t taken(uint32_t &at, const DgFastDiv &by)
     return n;
 }
 
+// A context's longest: a place a few stages past its end is still a 32-bit number (a table may name a page as often as it likes, so the cache's size
+// does not see to that).
+constexpr int32_t MOST_CONTEXT = INT32_MAX - 65536;
+
 // What a sequence's new tokens are, with everything that lies in device memory held to what the buffers have.
 struct Sequence {
     int32_t first, count, ctx, past;      // past: the context before its new tokens (negative if these are more than the context)
@@ -170,7 +174,7 @@ __device__ __forceinline__ Sequence sequence(const DgAttention &a, int b)
     const int start = ((Scalars)a.q_start)[b], stop = ((Scalars)a.q_start)[b + 1], ctx = ((Scalars)a.ctx_len)[b];
     s.first = min(max(start, 0), a.T);
     s.count = min(max(stop, s.first), a.T) - s.first;
-    s.ctx = (int32_t)min((int64_t)max(ctx, 0), (int64_t)a.table_width * a.cache.page_size);
+    s.ctx = (int32_t)min((int64_t)min(max(ctx, 0), MOST_CONTEXT), (int64_t)a.table_width * a.cache.page_size);
     s.past = s.ctx - s.count;
     s.count = min(s.count, a.max_q);
     return s;

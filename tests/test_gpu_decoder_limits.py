@@ -115,3 +115,21 @@ def test_more_rows_than_a_launch_reads():
     dg.dg_cache_read(desc, cache, slots, got, None)
     for first in range(0, T, 1 << 22):
         assert torch.equal(got[first:first + (1 << 22)], want[slots[first:first + (1 << 22)].long()])
+
+
+@pytest.mark.parametrize("rows", ["16", "32", "128"])
+def test_a_context_at_the_end_of_32_bits(rows, monkeypatch):
+    """A table that names one page 2^27 times, and a length at the end of its type: the softmax of the page's sixteen tokens."""
+    monkeypatch.setenv("DG_ATTENTION_ROWS", rows)
+    desc = dg.cache_desc(2, 16, 1, 64, 8)
+    cache = torch.zeros(dg.dg_cache_bytes(desc), dtype=torch.uint8, device="cuda")
+    k, v = (torch.randn(16, 1, 64, generator=torch.Generator().manual_seed(i)).half() for i in range(2))
+    at = torch.arange(16, 32, dtype=torch.int32, device="cuda")
+    dg.dg_cache_write(desc, cache, k.cuda(), v.cuda(), at)
+    k, v = (x.cpu().double()[:, 0] for x in dg.dg_cache_read(desc, cache, at))
+    table = torch.ones(1, 1 << 27, dtype=torch.int32, device="cuda")
+    q = torch.randn(2, 1, 64, generator=torch.Generator().manual_seed(2)).half()
+    out = dg.dg_paged_attention(desc, cache, q.cuda(), on_gpu(np.array([0, 2], np.int32)), on_gpu(np.array([2 ** 31 - 1], np.int32)), table, 2, 2 ** 31 - 70000)
+    want = torch.softmax(q[:, 0].double() @ k.t() * 0.125, -1) @ v
+    # (up to 2^18 additions one after another, each off by 2^-24 of a sum: what is tested is where tokens are read, not the last bits)
+    assert ((out[:, 0].cpu().double() - want).abs() <= 2.0 ** -5 * v.abs().max()).all()
