@@ -455,8 +455,9 @@ dg_status dg_cache_read(const dg_cache_desc *desc, const void *cache_dev, size_t
  * q_start[B + 1], ctx_len[B] and the table are device memory and are not checked on the host: token numbers are held to 0 ... T, a context
  * to the table's width and to 2^31 - 65537, and a page number that is none of the cache's hides its tokens, as does nothing else.  max_q: no sequence has more new tokens
  * (later ones get no output).  max_ctx: about the longest context; how the work is cut goes by it, results are right whatever it is.
- * Codes enter the matrix instructions exactly; scores, softmax and sums are binary32; weights are rounded once, to binary16 with a scale of
- * their own (to two binary16 numbers for binary16 outputs).
+ * Codes enter the matrix instructions exactly; scores, softmax and sums are binary32; weights (softmax times value scale) are rounded once, to
+ * binary16 relative to their row's largest, of which 2^-28 is still counted (to two binary16 numbers for binary16 outputs).  A row's result goes by its own
+ * query and by what it sees, not by other rows.
  * Rows of no sequence are not written.  work_dev: dg_paged_attention_work_bytes(...) bytes, 16-byte aligned (0 bytes: may be NULL).
  * Errors: DG_ERR_NULL; DG_ERR_SHAPE (Hq no multiple of heads, negative sizes); DG_ERR_RANGE (rows beyond 32 bits); DG_ERR_UNSUPPORTED;
  * DG_ERR_BUFFER.

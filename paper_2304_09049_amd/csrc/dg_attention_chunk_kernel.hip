@@ -3,9 +3,9 @@
 // A workgroup takes 128 rows of a cached head, 32 a wavefront: two blocks of 16, so that a code is turned into binary16 once for two products.  The
 // tokens go by in stages of 64, four units, one loaded by each wavefront into a ring in LDS that all four read.
 //
-// What bounds it is the vector unit: 32 tokens are 280 of its instructions for a wavefront (16 exponentials, 3.5 more for each weight of a lane, 96 for codes to binary16) beside
-// 32 matrix instructions, which it hardly overlaps (the one 67 % of the cycles, the other 30 %).  2048 queries of 32 heads on 8 of 128 channels against 32768 tokens,
-// 8 bits: 1.4 ms, 740 TFLOP/s.  Slower: four blocks of rows a wavefront (half the conversions, but one wavefront a SIMD: 2.3 ms); operands made once for all
+// What bounds it is the vector unit: 32 tokens are 285 of its instructions for a wavefront (16 exponentials, 4 more for each weight of a lane, 96 for codes to binary16) beside
+// 32 matrix instructions, which it hardly overlaps (the one 71 % of the cycles, the other 31 %).  2048 queries of 32 heads on 8 of 128 channels against 32768 tokens,
+// 8 bits: 1.39 ms, 770 TFLOP/s.  Slower, when it took 1.4 to 1.48 ms: four blocks of rows a wavefront (half the conversions, but one wavefront a SIMD: 2.3 ms); operands made once for all
 // four wavefronts and handed on through LDS (226 instructions, but a barrier every 32 tokens and four times the bytes from LDS: 1.56 ms).
 #include "dg_attention.h"
 

@@ -11,9 +11,9 @@
 // 2^(logit - shift) times the token's value scale, the row's largest being kept between 2^4 and 2^14: what is 2^-28 of it is still counted.  Nothing of this
 // goes by other rows, or by what a row does not see: a row's bits are the same whatever stands beside it.
 //
-// What bounds it: for single tokens the cache's bytes, read once (one context of 131071 tokens, 32 heads on 8 of 128 channels, 8 bits: 59 us, 4.7 TB/s; 64 contexts of
-// up to 8192, 4 bits: 82 us, 3.7 TB/s: there the vector unit is as busy, 16 columns of a product for the 4 rows that there are), or, for short contexts, two launches
-// and one tile's chain of latencies (one context of 1000: 8.1 us; of 250, one launch, 6.1); for many rows the vector unit (chunk kernel).
+// What bounds it: for single tokens the cache's bytes, read once (one context of 131071 tokens, 32 heads on 8 of 128 channels, 8 bits: 56 us, 4.9 TB/s; 64 contexts of
+// up to 8192, 4 bits: 80 us, 3.9 TB/s: there the vector unit is as busy, 16 columns of a product for the 4 rows that there are), or, for short contexts, two launches
+// and one tile's chain of latencies (one context of 1000: 8.2 us; of 250, one launch, 6.1); for many rows the vector unit (chunk kernel).
 #include <algorithm>
 #include <cstring>
 
@@ -31,6 +31,8 @@ struct Kept {
     static constexpr int TILE_BYTES = 2 * Unit<BITS, DIM>::BYTES, LOADS = 2 * Unit<BITS, DIM>::LOADS;
     static constexpr int DEPTH = WAVES * 2 * TILE_BYTES <= 40960 ? 2 : 1, RINGS = WAVES * DEPTH * TILE_BYTES;
     static constexpr int SHARES = WAVES * 16 * (DIM + 4) * 4;
+    // Two blocks of rows of 64 channels: three, at 168 registers (300 x 12 queries on 3000 tokens in 4 bits 45.7 us, by two 49.7).  256 channels: what the registers
+    // give, two for one block (one token on 8192, 32 heads on 8, 8 bits 16.0 us, 2.1 TB/s; 16 on up to 4096, 4 bits 37.6; 500 on 4000, 16 heads on 4, 8 bits 83).
     static constexpr int WAVES_PER_SIMD = DIM == 256 ? 1 : N == 2 ? (DIM == 64 ? 3 : 2) : DIM == 128 && BITS == 4 ? 3 : 4;
 };
 
@@ -235,11 +237,16 @@ struct Plan {
 
 // Rows: 16 a workgroup, whose wavefronts share its piece of the context, give most workgroups; 32 turn each code into binary16 once for two products; 128,
 // 32 a wavefront, load a token once for all of them and have nothing to join at the end, but wait for one another at every stage.  us with 16, 32, 128
-// (queries x sequences on contexts, heads / cached heads x channels):
-//     8 x 32 on 2048, 64/8 x 128        28    39    61        256 on 8192, 32/8 x 128, 4 bits     119    96   109
-//     64 on 16384, 32/8 x 128           56    60    64        300 x 12 on 3000 (ragged), 16/16 x 64, 4 bits   59   53   107
-//     1000 on 1000, 16/16 x 64          20    34    36        512 x 4 on 4096 (ragged), 32/8 x 128     131   130   151
-//     2048 x 2 on 2048, 32/8 x 128     255   241   171        2048 on 32768, 32/8 x 128   1850  1470  1400
+// (queries x sequences on contexts, heads / cached heads x channels; several sequences have lengths spread evenly up to these), the rule's choice marked:
+//     8 x 32 on 2048, 64/8 x 128       *23    28    55        256 on 8192, 32/8 x 128, 4 bits        92   *80    87
+//     64 on 16384, 32/8 x 128          *48    44    58        300 x 12 on 3000, 16/16 x 64, 4 bits   51   *50    99
+//     1000 on 1000, 16/16 x 64         *16    16    28        512 x 4 on 4096, 32/8 x 128           106  *113   133
+//     2048 x 2 on 2048, 32/8 x 128     172   179  *121        2048 on 32768, 32/8 x 128            1856  1437 *1378
+// and where its lines are, 32/8 x 128 but for the last:
+//     512 on 32768      502  *381   372        1024 on 8192    239  *196   199        2048 on 4096                 206  *166   156
+//     1024 on 32768     969  *740   721        2048 on 8192    437   344  *330        3000 on 3000                 169  *147   119
+//     1536 on 32768    1414 *1089  1370        1024 on 32768, 4 bits 1093 *924 950    4096 on 8192, 16/16 x 64     302   233  *265
+// So the lines are near where the sides meet for long contexts; a prompt of its own (3000 on 3000) and narrow heads lose 14 to 24 % on the wrong side of them.
 // Pieces: one workgroup a SIMD (half as many of 32 rows; more: 64 contexts of up to 8192, 4 bits, 92 us with one or two a SIMD, 107 with eight), pieces of 512
 // tokens at least; where that leaves compute units without a workgroup, pieces of 128, a tile a wavefront (one context of 1000 8.1 us, 8.9 by pieces of
 // 256; of 4000 8.8, 9.9; but four of 8192 by pieces of 256 23.0 for 19.4), or one piece, which needs no joining, of up to four tiles a wavefront (two with

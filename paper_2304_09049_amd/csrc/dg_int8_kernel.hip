@@ -510,7 +510,8 @@ void launch_tiles(const DgGemmI8 &p, hipStream_t stream)
 enum class Form { Few, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
 constexpr int FEW_TOKENS = 32;
 
-// The kernel for up to 32 tokens (16 x 4096 x 4096 6.4 us, 64 x 64 tiles 8.8; 32 tokens 8.1, 32 x 64 tiles 8.2), or the tile (channels x tokens) whose
+// The kernel for up to 32 tokens (16 x 4096 x 4096 6.6 us, 32 x 64 tiles 7.7; 32 tokens 8.5, 8.1; 32 x 1000 x 1000 6.0, 10.4; 32 x 12288 x 1024 6.9, 9.8; but
+// long sums of 24 and 32 tokens are faster in tiles: 24 x 8192 x 8192 19.1, 17.0; 32 x 8192 x 8192 20.0, 17.5; 32 x 2048 x 8192 13.1, 11.0), or the tile (channels x tokens) whose
 // rounds over the compute units, one workgroup each, cost least.  A round's cost by tile, us for K = 4096 and 8192: 32 x 64 8, 18; 64 x 64 10, 24; 128 x 64 15, 34;
 // 128 x 128 23, 46; 256 x 128 39, 72; 256 x 256 54, 104.  Of 60 products, 33 to 2048 tokens, this is within 3 % of the fastest tile on 58, 6 % on two (64 x 2048 x 8192
 // 11.7 us by 32 x 64, 15.0 by 64 x 64; 128 x 8192 x 8192 33.8, 24.1).
