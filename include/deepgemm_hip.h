@@ -469,6 +469,94 @@ dg_status dg_paged_attention(const dg_cache_desc *desc, const void *cache_dev, s
                              int32_t causal, void *out_dev, int64_t stride_ot, int64_t stride_oh, void *work_dev, size_t work_bytes,
                              void *hip_stream);
 
+/* ---- layers in microscaled 4-bit floating point, and layers of experts ------------------------------------------------------ */
+
+/*
+ * Rows of numbers in 4 bits with a power of two for every 32 neighbours (the microscaling format of the Open Compute Project with E2M1 elements and E8M0
+ * scales).  Of a block, elements 32 b ... 32 b + 31 of a row (the last one may be shorter), m = max|x|:
+ *     scale byte  clip(floor(log2 m) - 2, -127, 127) + 127, 0 for m = 0; the scale is s = 2^(byte - 127).  255 (NaN) where an element is an infinity or a NaN
+ *     code        the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| / s, 6 at most, ties to the even code: its place in that list, plus 8 where x has a sign;
+ *                 0 in a block of scale 255
+ *     value       the element times s; NaN where the byte is 255
+ * Layout: element k of a row has the half k % 2 (0: low) of byte k / 2; a row is whole blocks, ceil(K/32) * 16 bytes, codes from K on being 0; its scales are
+ * ceil(K/32) bytes.  Rows of codes begin on 16 bytes, rows of scales on 4 (else DG_ERR_BUFFER), and a row's last word of scales can be read whole (what is in the
+ * bytes past the scales does not matter).
+ */
+
+/*
+ * x_dev ([N][K] of `type`, rows stride_n elements apart) -> codes_dev (rows stride_codes bytes apart) and scales_dev (stride_scales).  Bytes behind a row's are not
+ * written.  1 <= K <= 2^24.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (N < 0, K <= 0, a stride below its row); DG_ERR_RANGE (K, N * K beyond 2^58); DG_ERR_UNSUPPORTED (type); DG_ERR_BUFFER.
+ */
+dg_status dg_quantize_mx4(const void *x_dev, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, uint8_t *codes_dev, int64_t stride_codes,
+                          uint8_t *scales_dev, int64_t stride_scales, void *hip_stream);
+/* The values of codes and scales, rounded to `type`: out_dev [N][K], rows stride_out elements apart.  Errors as above. */
+dg_status dg_dequantize_mx4(const uint8_t *codes_dev, int64_t stride_codes, const uint8_t *scales_dev, int64_t stride_scales, int64_t N, int64_t K,
+                            void *out_dev, dg_dtype type, int64_t stride_out, void *hip_stream);
+
+/*
+ * Product of two such matrices, weights W ([M] rows of K) and tokens A ([N]):
+ *     out[n][m] = sum_{k<K} W[m][k] * A[n][k] + bias[m]
+ * Products are exact; sums are binary32 (within one instruction's 64 or 128 products what lies 2^28 below the largest may be left off), the bias (binary32, may be NULL)
+ * is added and the result rounded once.  A block of scale 255 makes its row's results NaN.  out_dev: [N][M] of out_type, rows stride_out elements apart.
+ * The order of the sums goes by the sizes and alignment, so a call gives the same bits each time.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, a stride below its row); DG_ERR_RANGE (K beyond 2^24; M * N of 2^43 and more); DG_ERR_UNSUPPORTED; DG_ERR_BUFFER.
+ */
+dg_status dg_gemm_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_scales_dev, int64_t stride_ws, const uint8_t *A_dev, int64_t stride_a,
+                      const uint8_t *A_scales_dev, int64_t stride_as, int64_t M, int64_t N, int64_t K, const float *bias_m_dev, void *out_dev,
+                      dg_dtype out_type, int64_t stride_out, void *hip_stream);
+/*
+ * The layer from activations that are not quantised yet: dg_quantize_mx4 and dg_gemm_mx4 as one call, with their results.
+ * work_dev: work_bytes >= dg_linear_mx4_work_bytes(N, K) (else DG_ERR_BUFFER), 16-byte aligned; its contents are the library's.
+ */
+size_t dg_linear_mx4_work_bytes(int64_t N, int64_t K);
+dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_scales_dev, int64_t stride_ws, const void *x_dev, dg_dtype x_type,
+                        int64_t stride_x, int64_t M, int64_t N, int64_t K, const float *bias_m_dev, void *work_dev, size_t work_bytes, void *out_dev,
+                        dg_dtype out_type, int64_t stride_out, void *hip_stream);
+
+/*
+ * A router: to which `top` of E experts each token goes, and with what weights.
+ *     l[t][e] = sum_k x[t][k] * R[e][k]        summed in binary64, rounded to binary32
+ *     choice  = l (DG_ROUTE_SOFTMAX, _SOFTMAX_ALL) or sigmoid(l) (DG_ROUTE_SIGMOID; binary64), plus bias[e] if bias_e_dev is not NULL (binary64)
+ *     ids     the experts of the `top` largest choices, the largest first, among equals the lowest expert.  An expert whose choice is -infinity is not taken: where too few
+ *             are left the row ends with ids -1 and weights 0
+ *     weights (binary32), of the experts taken, times `factor`:   exp(l) / sum over the taken of exp(l);   exp(l) / sum over all of exp(l);
+ *             sigmoid(l) / sum over the taken of sigmoid(l) (0 where that is 0)
+ * A token with a NaN among its l or choices gets the experts 0 ... top - 1 and weights NaN: whatever is computed from it shows it.
+ * x_dev: [T][K] of x_type, rows stride_x elements apart; R_dev: [E][K] of r_type (x_type or DG_F32), stride_r.  ids_dev, weights_dev: contiguous [T][top].
+ * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned.  E <= 1024, top <= 64, K < 2^31.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (T < 0, K, E, top <= 0, top > E, a stride below its row); DG_ERR_RANGE (E, top, K, T * E of 2^31 and more); DG_ERR_UNSUPPORTED; DG_ERR_BUFFER.
+ */
+typedef enum { DG_ROUTE_SOFTMAX = 0, DG_ROUTE_SOFTMAX_ALL = 1, DG_ROUTE_SIGMOID = 2 } dg_route_mode;
+size_t dg_route_tokens_work_bytes(int64_t T, int64_t E);
+dg_status dg_route_tokens(const void *x_dev, dg_dtype x_type, int64_t T, int64_t K, int64_t stride_x, const void *R_dev, dg_dtype r_type, int64_t E,
+                          int64_t stride_r, const float *bias_e_dev, int64_t top, dg_route_mode mode, float factor, int32_t *ids_dev, float *weights_dev,
+                          void *work_dev, size_t work_bytes, void *hip_stream);
+
+/*
+ * Experts whose weights are held as above: for each, `up` of 2 * inner rows of `hidden` (the gates', then the others') and `down` of `hidden` rows of `inner`.
+ * Distances in bytes from row to row and from expert to expert; codes' are multiples of 16, scales' of 4.
+ */
+typedef struct {
+    int32_t experts, hidden, inner, reserved;           /* reserved: 0 */
+    const uint8_t *up, *up_scales, *down, *down_scales;
+    int64_t up_row, up_expert, up_scales_row, up_scales_expert;
+    int64_t down_row, down_expert, down_scales_row, down_scales_expert;
+} dg_experts_desc;
+/*
+ * The gated feed-forward of each token's experts e = ids[t][j], j < top:
+ *     g = gate_e x[t],  u = other_e x[t],  h = g / (1 + exp(-g)) * u,      out[t] = sum_j weights[t][j] * (down_e h)
+ * An id that is no expert is skipped (a token of which none is left gives 0); a token may name an expert twice.  x and out are binary16 or bfloat16 and enter exactly; sums are
+ * binary32; h is kept to 2^-17 of itself (two bfloat16 numbers); results are rounded once.  A token's results go by its own x, ids and weights only.  Only the weights of experts that are named are
+ * read, once for 64 tokens (for few tokens that reading is what a call costs): meant for tokens being decoded; more than a few hundred tokens are worked through in turns.
+ * x_dev: [T][hidden], rows stride_x elements apart; ids_dev, weights_dev: contiguous [T][top]; out_dev rows stride_out apart.  out_dev must not overlap x_dev.
+ * work_dev: dg_experts_mx4_work_bytes(...) bytes, 16-byte aligned.  top <= 64; hidden, inner <= 2^20; experts <= 2^16.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (a size <= 0, T < 0, a stride below its row); DG_ERR_RANGE; DG_ERR_UNSUPPORTED (type, reserved); DG_ERR_BUFFER.
+ */
+size_t dg_experts_mx4_work_bytes(int64_t T, int64_t top, int64_t hidden, int64_t inner);
+dg_status dg_experts_mx4(const dg_experts_desc *desc, const void *x_dev, dg_dtype type, int64_t T, int64_t stride_x, const int32_t *ids_dev,
+                         const float *weights_dev, int64_t top, void *work_dev, size_t work_bytes, void *out_dev, int64_t stride_out, void *hip_stream);
+
 #pragma GCC visibility pop
 #ifdef __cplusplus
 }

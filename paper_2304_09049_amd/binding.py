@@ -25,6 +25,7 @@ DG_KERNEL_ONEHOT_SMFMAC = 7
 KERNELS = {"auto": DG_KERNEL_AUTO, "perm": DG_KERNEL_PERM, "lds": DG_KERNEL_LDS,
            "mfma_i8": DG_KERNEL_MFMA_I8, "smalln": DG_KERNEL_SMALLN, "lut65k": DG_KERNEL_LUT65K,
            "onehot_mfma": DG_KERNEL_ONEHOT_MFMA, "onehot_smfmac": DG_KERNEL_ONEHOT_SMFMAC}
+ROUTE_MODES = {"softmax": 0, "softmax_all": 1, "sigmoid": 2}
 
 # every symbol include/deepgemm_hip.h declares
 EXPORTS = (
@@ -38,6 +39,8 @@ EXPORTS = (
     "dg_static_work_bytes", "dg_conv2d_lut_codes_static",
     "dg_quantize_tokens", "dg_gemm_i8", "dg_linear_i8_work_bytes", "dg_linear_i8", "dg_cache_bytes", "dg_cache_write", "dg_cache_read",
     "dg_paged_attention_work_bytes", "dg_paged_attention",
+    "dg_quantize_mx4", "dg_dequantize_mx4", "dg_gemm_mx4", "dg_linear_mx4_work_bytes", "dg_linear_mx4", "dg_route_tokens_work_bytes", "dg_route_tokens",
+    "dg_experts_mx4_work_bytes", "dg_experts_mx4",
 )
 
 
@@ -49,6 +52,14 @@ class ConvDesc(ctypes.Structure):
 class CacheDesc(ctypes.Structure):
     """A paged cache of quantised keys and values: its pages, their tokens, the heads, their channels, the bits of a code."""
     _fields_ = [(n, ctypes.c_int32) for n in ("pages", "page_size", "heads", "dim", "bits")]
+
+
+class ExpertsDesc(ctypes.Structure):
+    """Experts' weights in microscaled 4-bit floating point: how many, their sizes, where they lie (distances in bytes)."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("experts", "hidden", "inner", "reserved")]
+                + [(n, ctypes.c_void_p) for n in ("up", "up_scales", "down", "down_scales")]
+                + [(n, ctypes.c_int64) for n in ("up_row", "up_expert", "up_scales_row", "up_scales_expert",
+                                                 "down_row", "down_expert", "down_scales_row", "down_scales_expert")])
 
 
 class DgError(RuntimeError):
@@ -132,6 +143,19 @@ def lib() -> ctypes.CDLL:
     L.dg_paged_attention.argtypes = [desc, c_vp, c_sz, c_vp, c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_i64, c_i64, c_i64, c_i64,
                                      c_f, c_i32, c_vp, c_i64, c_i64, c_vp, c_sz, c_vp]
     L.dg_paged_attention.restype = c_int
+    L.dg_quantize_mx4.argtypes, L.dg_quantize_mx4.restype = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp], c_int
+    L.dg_dequantize_mx4.argtypes, L.dg_dequantize_mx4.restype = [c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_vp, c_int, c_i64, c_vp], c_int
+    L.dg_gemm_mx4.argtypes = [c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_int, c_i64, c_vp]
+    L.dg_gemm_mx4.restype = c_int
+    L.dg_linear_mx4_work_bytes.argtypes, L.dg_linear_mx4_work_bytes.restype = [c_i64, c_i64], c_sz
+    L.dg_linear_mx4.argtypes = [c_vp, c_i64, c_vp, c_i64, c_vp, c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_sz, c_vp, c_int, c_i64, c_vp]
+    L.dg_linear_mx4.restype = c_int
+    L.dg_route_tokens_work_bytes.argtypes, L.dg_route_tokens_work_bytes.restype = [c_i64, c_i64], c_sz
+    L.dg_route_tokens.argtypes = [c_vp, c_int, c_i64, c_i64, c_i64, c_vp, c_int, c_i64, c_i64, c_vp, c_i64, c_int, c_f, c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.dg_route_tokens.restype = c_int
+    L.dg_experts_mx4_work_bytes.argtypes, L.dg_experts_mx4_work_bytes.restype = [c_i64] * 4, c_sz
+    L.dg_experts_mx4.argtypes = [ctypes.POINTER(ExpertsDesc), c_vp, c_int, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_sz, c_vp, c_i64, c_vp]
+    L.dg_experts_mx4.restype = c_int
     _lib = L
     return L
 
@@ -519,6 +543,100 @@ def dg_paged_attention(desc: CacheDesc, cache, q, q_start, ctx_len, table, max_q
             work = _new(need, "uint8", q.device, stream)
     status = (_native or _load_native()).paged_attention(desc, cache, q, q_start, ctx_len, table, max_q, max_ctx,
                                                          desc.dim ** -0.5 if scale is None else scale, causal, out, work, stream)
+    if status:
+        _check(status)
+    return out
+
+
+# ---- layers in microscaled 4-bit floating point, and layers of experts --------------------------------------------------------
+
+
+def dg_quantize_mx4(x, codes=None, scales=None, stream=None):
+    """x: float32, float16 or bfloat16 device tensor [N][K] (rows may lie apart) -> (codes, scales): uint8 [N][16 * blocks], two codes a byte, and uint8
+    [N][blocks], a power of two for each block of 32.  The scales made here are rows of whole words of four bytes (a view)."""
+    blocks = -(-x.shape[1] // 32)
+    if codes is None:
+        codes = _new((x.shape[0], 16 * blocks), "uint8", x.device, stream)
+    if scales is None:
+        scales = _new((x.shape[0], -(-blocks // 4) * 4), "uint8", x.device, stream)[:, :blocks]
+    status = (_native or _load_native()).quantize_mx4(x, codes, scales, stream)
+    if status:
+        _check(status)
+    return codes, scales
+
+
+def dg_dequantize_mx4(codes, scales, K: Optional[int] = None, out=None, dtype=None, stream=None):
+    """The values [N][K] (K: all that the blocks hold, if it is not given) of codes and scales, of `dtype` (default float32) or out's."""
+    if out is None:
+        out = _new((codes.shape[0], 2 * codes.shape[1] if K is None else K), dtype or "float32", codes.device, stream)
+    elif K is not None and out.shape[1] != K:
+        raise ValueError(f"out must have {K} columns, got {out.shape[1]}")
+    status = (_native or _load_native()).dequantize_mx4(codes, scales, out, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def dg_gemm_mx4(W, W_scales, A, A_scales, bias=None, out=None, dtype=None, stream=None):
+    """Product of two quantised matrices, W [M rows] and A [N rows] of as many blocks -> [N][M] of `dtype` (or out's; default float32), plus the float32 bias[m] if
+    one is given."""
+    if out is None:
+        out = _new((A.shape[0], W.shape[0]), dtype or "float32", W.device, stream)
+    status = (_native or _load_native()).gemm_mx4(W, W_scales, A, A_scales, bias, out, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def dg_linear_mx4_work_bytes(N: int, K: int) -> int:
+    return int(lib().dg_linear_mx4_work_bytes(N, K))
+
+
+def dg_linear_mx4(W, W_scales, x, bias=None, work=None, out=None, stream=None):
+    """dg_quantize_mx4 and dg_gemm_mx4 as one call: x [N][K] -> [N][M] of x's dtype (or out's).  `work`: uint8, dg_linear_mx4_work_bytes(N, K)."""
+    if out is None:
+        out = _new((x.shape[0], W.shape[0]), x.dtype, W.device, stream)
+    if work is None:
+        work = _new(dg_linear_mx4_work_bytes(x.shape[0], x.shape[1]), "uint8", W.device, stream)
+    status = (_native or _load_native()).linear_mx4(W, W_scales, x, bias, work, out, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def dg_route_tokens_work_bytes(T: int, E: int) -> int:
+    return int(lib().dg_route_tokens_work_bytes(T, E))
+
+
+def dg_route_tokens(x, R, top: int, mode="softmax", bias=None, factor: float = 1.0, ids=None, weights=None, work=None, stream=None):
+    """A router R [E][K] (x's dtype or float32) on tokens x [T][K] -> (ids int32 [T][top], weights float32 [T][top]): the experts of the `top` largest logits
+    ("softmax": weights over those taken, "softmax_all": over all) or sigmoids ("sigmoid": normalised over those taken), with the float32 bias[e] added to what they are
+    chosen by; weights times `factor`.  `work`: uint8, dg_route_tokens_work_bytes(T, E)."""
+    if ids is None:
+        ids = _new((x.shape[0], top), "int32", x.device, stream)
+    if weights is None:
+        weights = _new((x.shape[0], top), "float32", x.device, stream)
+    if work is None:
+        work = _new(dg_route_tokens_work_bytes(x.shape[0], R.shape[0]), "uint8", x.device, stream)
+    status = (_native or _load_native()).route_tokens(x, R, top, ROUTE_MODES[mode] if isinstance(mode, str) else int(mode), bias, factor, ids, weights, work, stream)
+    if status:
+        _check(status)
+    return ids, weights
+
+
+def dg_experts_mx4_work_bytes(T: int, top: int, hidden: int, inner: int) -> int:
+    return int(lib().dg_experts_mx4_work_bytes(T, top, hidden, inner))
+
+
+def dg_experts_mx4(up, up_scales, down, down_scales, x, ids, weights, work=None, out=None, stream=None):
+    """The gated feed-forward of the experts that ids [T][top] (int32) name, added up with weights [T][top] (float32): x [T][hidden] float16 or bfloat16 -> the
+    same.  up: quantised [experts][2 * inner] rows of `hidden` (the gates' first), down: [experts][hidden] rows of `inner`, as dg_quantize_mx4 makes rows.
+    `work`: uint8, dg_experts_mx4_work_bytes(T, top, hidden, inner)."""
+    if out is None:
+        out = _new(x.shape, x.dtype, x.device, stream)
+    if work is None:
+        work = _new(dg_experts_mx4_work_bytes(x.shape[0], ids.shape[1], x.shape[1], up.shape[1] // 2), "uint8", x.device, stream)
+    status = (_native or _load_native()).experts_mx4(up, up_scales, down, down_scales, x, ids, weights, work, out, stream)
     if status:
         _check(status)
     return out

@@ -595,6 +595,169 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- microscaled 4-bit floating point, experts ----
+
+// A tensor on the current device, which is where a call without a stream of its own is launched, and the only one whose streams a call may be given.
+const at::Tensor &here(const at::Tensor &t, const char *name)
+{
+    const int current = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
+    if (t.device().index() != current) {
+        PyErr_Format(PyExc_ValueError, "%s must live on the current device (%d), not on %d", name, current, (int)t.device().index());
+        throw Failed();
+    }
+    return t;
+}
+template <class T>
+T *vector_here(PyObject *o, at::ScalarType type, int64_t count, const char *name, bool optional = false)
+{
+    T *p = vector<T>(o, type, count, name, optional);
+    if (o != Py_None) here(THPVariable_Unpack(o), name);
+    return p;
+}
+
+// Quantised rows as the binding has them: codes [...][rows][16 * blocks] and scales [...][rows][blocks], uint8; distances in bytes (those that no index takes are of any use to
+// the library's checks only).
+struct Mx4 {
+    const uint8_t *codes, *scales;
+    int64_t rows, blocks, row, expert = 0, scales_row, scales_expert = 0;
+    Mx4(PyObject *c, PyObject *s, int dims, const char *name, const char *scales_name)
+    {
+        const at::Tensor &tc = here(of_type(strided(c, dims, name), at::kByte, name), name);
+        const at::Tensor &ts = here(of_type(strided(s, dims, scales_name), at::kByte, scales_name), scales_name);
+        const int r = dims - 2;
+        rows = tc.size(r);
+        blocks = tc.size(r + 1) / 16;
+        if (tc.size(r + 1) % 16 != 0 || ts.size(r) != rows || ts.size(r + 1) != blocks || (r && ts.size(0) != tc.size(0))) {
+            PyErr_Format(PyExc_ValueError, "%s must be rows of 16 bytes a block, and %s as many rows of one byte a block", name, scales_name);
+            throw Failed();
+        }
+        codes = (const uint8_t *)tc.data_ptr();
+        scales = (const uint8_t *)ts.data_ptr();
+        row = rows > 1 ? tc.stride(r) : 16 * blocks;
+        scales_row = rows > 1 ? ts.stride(r) : (blocks + 3) / 4 * 4;
+        if (r && tc.size(0) > 1) {
+            expert = tc.stride(0);
+            scales_expert = ts.stride(0);
+        }
+    }
+};
+
+// (x, codes, scales, stream)
+PyObject *quantize_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&] {
+        const at::Tensor &x = here(strided(a[0], 2, "x"), "x");
+        const dg_dtype type = element_type(x, "x");
+        const Mx4 q(a[1], a[2], 2, "codes", "scales");
+        const int64_t N = x.size(0), K = x.size(1), sx = step(x, 0);
+        expect(q.rows == N && q.blocks == (K + 31) / 32, "codes must have x's rows, of its blocks of 32");
+        void *s = stream_of(a[3]);
+        const void *px = x.data_ptr();
+        RUN(dg_quantize_mx4(px, type, N, K, sx, const_cast<uint8_t *>(q.codes), q.row, const_cast<uint8_t *>(q.scales), q.scales_row, s));
+    });
+}
+
+// (codes, scales, out, stream)
+PyObject *dequantize_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&] {
+        const Mx4 q(a[0], a[1], 2, "codes", "scales");
+        const at::Tensor &out = here(strided(a[2], 2, "out"), "out");
+        const dg_dtype type = element_type(out, "out");
+        const int64_t N = out.size(0), K = out.size(1), so = step(out, 0);
+        expect(q.rows == N && q.blocks == (K + 31) / 32, "out must have the codes' rows, of their blocks of 32");
+        void *s = stream_of(a[3]), *po = out.data_ptr();
+        RUN(dg_dequantize_mx4(q.codes, q.row, q.scales, q.scales_row, N, K, po, type, so, s));
+    });
+}
+
+// (W, W_scales, A, A_scales, bias, out, stream)
+PyObject *gemm_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const Mx4 W(a[0], a[1], 2, "W", "W_scales"), A(a[2], a[3], 2, "A", "A_scales");
+        const at::Tensor &out = here(strided(a[5], 2, "out"), "out");
+        expect(A.blocks == W.blocks, "A and W must have the same number of columns");
+        expect(out.size(0) == A.rows && out.size(1) == W.rows, "out must be [tokens][channels]");
+        const float *bias = vector_here<float>(a[4], at::kFloat, W.rows, "bias", true);
+        const dg_dtype type = element_type(out, "out");
+        void *s = stream_of(a[6]), *po = out.data_ptr();
+        const int64_t so = step(out, 0);
+        RUN(dg_gemm_mx4(W.codes, W.row, W.scales, W.scales_row, A.codes, A.row, A.scales, A.scales_row, W.rows, A.rows, 32 * W.blocks, bias, po, type, so, s));
+    });
+}
+
+// (W, W_scales, x, bias, work, out, stream)
+PyObject *linear_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const Mx4 W(a[0], a[1], 2, "W", "W_scales");
+        const at::Tensor &x = here(strided(a[2], 2, "x"), "x"), &out = here(strided(a[5], 2, "out"), "out");
+        const int64_t N = x.size(0), K = x.size(1);
+        expect((K + 31) / 32 == W.blocks, "x and W must have the same number of columns");
+        expect(out.size(0) == N && out.size(1) == W.rows, "out must be [tokens][channels]");
+        const float *bias = vector_here<float>(a[3], at::kFloat, W.rows, "bias", true);
+        void *work = device_ptr(a[4], at::kByte, "work");
+        const size_t bytes = bytes_of(a[4]);
+        const dg_dtype xt = element_type(x, "x"), type = element_type(out, "out");
+        void *s = stream_of(a[6]), *po = out.data_ptr();
+        const void *px = x.data_ptr();
+        const int64_t sx = step(x, 0), so = step(out, 0);
+        RUN(dg_linear_mx4(W.codes, W.row, W.scales, W.scales_row, px, xt, sx, W.rows, N, K, bias, work, bytes, po, type, so, s));
+    });
+}
+
+// (x, R, top, mode, bias, factor, ids, weights, work, stream)
+PyObject *route_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        const at::Tensor &x = here(strided(a[0], 2, "x"), "x"), &R = here(strided(a[1], 2, "R"), "R");
+        const dg_dtype xt = element_type(x, "x"), rt = element_type(R, "R");
+        const int64_t T = x.size(0), K = x.size(1), E = R.size(0), top = integer(a[2]);
+        expect(R.size(1) == K, "x and R must have the same number of columns");
+        const dg_route_mode mode = (dg_route_mode)integer(a[3]);
+        const float *bias = vector_here<float>(a[4], at::kFloat, E, "bias", true);
+        const float factor = (float)real(a[5]);
+        const int64_t choices = top > 0 && top <= E ? T * top : 0;
+        int32_t *ids = vector_here<int32_t>(a[6], at::kInt, choices, "ids");
+        float *weights = vector_here<float>(a[7], at::kFloat, choices, "weights");
+        void *work = device_ptr(a[8], at::kByte, "work");
+        const size_t bytes = bytes_of(a[8]);
+        void *s = stream_of(a[9]);
+        const void *px = x.data_ptr(), *pr = R.data_ptr();
+        const int64_t sx = step(x, 0), sr = step(R, 0);
+        RUN(dg_route_tokens(px, xt, T, K, sx, pr, rt, E, sr, bias, top, mode, factor, ids, weights, work, bytes, s));
+    });
+}
+
+// (up, up_scales, down, down_scales, x, ids, weights, work, out, stream)
+PyObject *experts_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        const Mx4 up(a[0], a[1], 3, "up", "up_scales"), down(a[2], a[3], 3, "down", "down_scales");
+        const at::Tensor &x = here(strided(a[4], 2, "x"), "x"), &out = here(strided(a[8], 2, "out"), "out");
+        const at::Tensor &ids = here(of_type(strided(a[5], 2, "ids"), at::kInt, "ids"), "ids");
+        const dg_dtype type = element_type(x, "x");
+        const int64_t E = THPVariable_Unpack(a[0]).size(0), T = x.size(0), K = x.size(1), F = up.rows / 2, top = ids.size(1);
+        expect(element_type(out, "out") == type && out.sizes() == x.sizes(), "out must have x's shape and dtype");
+        expect(THPVariable_Unpack(a[2]).size(0) == E, "up and down must have as many experts");
+        expect(up.rows % 2 == 0 && up.blocks == (K + 31) / 32, "up must be [experts][2 * inner][hidden] in blocks of 32");
+        expect(down.rows == K && down.blocks == (F + 31) / 32, "down must be [experts][hidden][inner] in blocks of 32");
+        expect(ids.size(0) == T && ids.is_contiguous(), "ids must be contiguous, [tokens][choices]");
+        expect(E <= INT32_MAX && K <= INT32_MAX && F <= INT32_MAX, "too many experts or channels");
+        const float *weights = vector_here<float>(a[6], at::kFloat, T * top, "weights");
+        void *work = device_ptr(a[7], at::kByte, "work");
+        const size_t bytes = bytes_of(a[7]);
+        void *s = stream_of(a[9]), *po = out.data_ptr();
+        const void *px = x.data_ptr();
+        const int32_t *pi = (const int32_t *)ids.data_ptr();
+        const int64_t sx = step(x, 0), so = step(out, 0);
+        const dg_experts_desc d = {(int32_t)E, (int32_t)K, (int32_t)F, 0, up.codes, up.scales, down.codes, down.scales, up.row, up.expert, up.scales_row,
+                                   up.scales_expert, down.row, down.expert, down.scales_row, down.scales_expert};
+        RUN(dg_experts_mx4(&d, px, type, T, sx, pi, weights, top, work, bytes, po, so, s));
+    });
+}
+
 // (ConvDesc, CacheDesc): binding's types, whose instances alone are taken for a geometry
 PyObject *use_desc(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -622,6 +785,8 @@ PyMethodDef methods[] = {
     METHOD("quantize_pack_activations", quantize_pack_activations), METHOD("dequantize", dequantize),
     METHOD("quantize_tokens", quantize_tokens), METHOD("gemm_i8", gemm_i8), METHOD("linear_i8", linear_i8),
     METHOD("cache_write", cache_write), METHOD("cache_read", cache_read), METHOD("paged_attention", paged_attention),
+    METHOD("quantize_mx4", quantize_mx4), METHOD("dequantize_mx4", dequantize_mx4), METHOD("gemm_mx4", gemm_mx4), METHOD("linear_mx4", linear_mx4),
+    METHOD("route_tokens", route_tokens), METHOD("experts_mx4", experts_mx4),
     METHOD("use_desc", use_desc),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Tensors in, the C ABI's status out.", -1, methods,

@@ -1,4 +1,4 @@
-// What the kernels of a quantised decoder layer share (8-bit products, the paged cache, the attention on it): element types, the
+// What the kernels of a quantised decoder layer share (8-bit and 4-bit products, the paged cache, the attention on it, experts): element types, the
 // cache's layout and the launchers.  Internal; the public ABI is include/deepgemm_hip.h.
 #pragma once
 
@@ -30,6 +30,17 @@ template <class T, int COUNT>
 __device__ __forceinline__ void dg_store_vec(T *p, const DgVec<T, COUNT> &v)
 {
     __builtin_memcpy(p, &v, sizeof(v));
+}
+
+// Elements k ... k + 7 of a row; those at K and beyond are 0 and are not read.
+template <class T>
+__device__ __forceinline__ DgVec<T, 8> dg_eight(const T *row, int32_t k, int32_t K)
+{
+    if (k + 8 <= K) return dg_load_vec<T, 8>(row + k);
+    DgVec<T, 8> v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.e[i] = k + i < K ? row[k + i] : T(0.0f);
+    return v;
 }
 
 // f(element type) for a dg_dtype that the API layer has checked.
@@ -211,3 +222,52 @@ struct DgAttention {
 };
 int64_t dg_attention_work_bytes(const DgAttention &p);
 dg_status dg_launch_attention(const DgAttention &p, dg_dtype type, hipStream_t stream);
+
+// ---- microscaled 4-bit floating point ------------------------------------------------------------------------------------
+
+// A scale's byte as a binary32 number: 2^(byte - 127), NaN for 255.
+__device__ __forceinline__ float dg_mx_scale(uint32_t byte)
+{
+    const uint32_t bits = byte == 0 ? 0x00400000u : byte << 23;
+    return __uint_as_float(byte == 255 ? 0x7FC00000u : bits);
+}
+
+dg_status dg_launch_quantize_mx4(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, uint8_t *codes, int64_t stride_codes,
+                                 uint8_t *scales, int64_t stride_scales, hipStream_t stream);
+dg_status dg_launch_dequantize_mx4(const uint8_t *codes, int64_t stride_codes, const uint8_t *scales, int64_t stride_scales, int64_t N, int64_t K,
+                                   void *out, dg_dtype type, int64_t stride_out, hipStream_t stream);
+struct DgGemmMx4 {
+    const uint8_t *W, *W_scales, *A, *A_scales;
+    int64_t stride_w, stride_ws, stride_a, stride_as;    // bytes from row to row
+    int32_t M, N, blocks;                                // blocks of 32 in a row
+    const float *bias;
+    void *out;
+    int64_t stride_out;                                  // elements from token to token
+};
+dg_status dg_launch_gemm_mx4(const DgGemmMx4 &p, dg_dtype type, hipStream_t stream);
+
+struct DgRoute {
+    const void *x, *R;
+    int64_t stride_x, stride_r;                          // elements
+    int32_t T, K, E, top;
+    const float *bias;
+    dg_route_mode mode;
+    float factor;
+    int32_t *ids;
+    float *weights;
+    float *logits;                                       // [T][E]
+};
+dg_status dg_launch_route(const DgRoute &p, dg_dtype x_type, dg_dtype r_type, hipStream_t stream);
+
+struct DgExperts {
+    dg_experts_desc d;
+    const void *x;
+    void *out;
+    int64_t stride_x, stride_out;                        // elements
+    const int32_t *ids;
+    const float *weights;
+    int32_t T, top;
+    void *work;
+};
+int64_t dg_experts_work_bytes(int64_t T, int64_t top, int64_t hidden, int64_t inner);
+dg_status dg_launch_experts(const DgExperts &p, dg_dtype type, hipStream_t stream);

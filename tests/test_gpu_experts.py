@@ -1,0 +1,223 @@
+"""A router and layers of experts on the GPU against 64 bits: choices are equal, sums within what their rounding allows."""
+import pytest
+import torch
+
+import mx4_reference as ref
+from paper_2304_09049_amd import binding as dg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAN, INF = float("nan"), float("inf")
+
+
+def check_route(x, R, top, mode, bias=None, factor=1.0):
+    """Weights: exp and sigmoid of binary32, a sum of at most 1024 of them, one quotient and one product."""
+    got = dg.dg_route_tokens(x.to(DEV), R.to(DEV), top, mode=mode, bias=None if bias is None else bias.to(DEV), factor=factor)
+    ids, weights = ref.route(x, R, top, mode, bias, factor)
+    assert torch.equal(got[0].cpu(), ids)
+    # an exponent is a difference of binary32 numbers: its rounding counts as many times as it is large, up to where exp is 0
+    ref.assert_within(got[1], weights, weights.abs() * 2.0 ** -24 * 400 + 1e-30)
+    return got
+
+
+@pytest.mark.parametrize("mode", ["softmax", "softmax_all", "sigmoid"])
+@pytest.mark.parametrize("T,K,E,top,dtype,rdtype,bias", [(1, 1, 1, 1, "f32", "f32", False), (1, 4096, 64, 4, "bf16", "bf16", False), (3, 33, 5, 5, "f16", "f16", True),
+                                                         (17, 1000, 60, 6, "bf16", "f32", True), (16, 64, 128, 8, "f16", "f32", False), (70, 257, 200, 3, "f32", "f32", True),
+                                                         (5, 100, 1000, 64, "bf16", "bf16", True), (33, 520, 256, 1, "bf16", "bf16", False), (2, 5000, 300, 8, "f32", "f32", True),
+                                                         (600, 96, 31, 7, "f16", "f16", True), (1, 7943, 513, 16, "bf16", "f32", False)])
+def test_route(T, K, E, top, dtype, rdtype, bias, mode):
+    gen = torch.Generator().manual_seed(T + K + E)
+    x = torch.randn(T, K + 3, generator=gen).to(ref.TYPES[dtype])[:, 1:K + 1]
+    R = (torch.randn(E, K + 5, generator=gen) * K ** -0.5).to(ref.TYPES[rdtype])[:, 2:K + 2]
+    check_route(x, R, top, mode, 0.3 * torch.randn(E, generator=gen) if bias else None, 2.5)
+
+
+@pytest.mark.parametrize("E", [8, 64, 100, 257, 700])
+def test_route_takes_the_lowest_of_equals(E):
+    gen = torch.Generator().manual_seed(E)
+    R = torch.randn(4, 64, generator=gen)[torch.randint(0, 4, (E,), generator=gen)].bfloat16()       # four different rows
+    x = torch.randn(9, 64, generator=gen).bfloat16()
+    x[4] = 0                                                          # all logits equal (zeros of both signs)
+    for mode in ("softmax", "sigmoid"):
+        ids, w = check_route(x, R, 8, mode)
+        assert ids[4].tolist() == list(range(8))
+
+
+def test_route_experts_that_are_out():
+    gen = torch.Generator().manual_seed(1)
+    x, R = torch.randn(5, 40, generator=gen), torch.randn(70, 40, generator=gen)
+    bias = torch.full((70,), -INF)
+    bias[[3, 68]] = torch.tensor([0.5, -0.5])
+    for mode in ("softmax", "softmax_all", "sigmoid"):
+        ids, w = check_route(x, R, 4, mode, bias)
+        assert (ids[:, 2:] == -1).all() and (w[:, 2:] == 0).all() and (w[:, :2] > 0).all()
+        ids, w = check_route(x, R, 3, mode, torch.full((70,), -INF))
+        assert (ids == -1).all() and (w == 0).all()
+    low = torch.full((2, 4), -300.0)
+    ids, w = dg.dg_route_tokens(low.to(DEV), torch.ones(3, 4, device=DEV), 2, mode="sigmoid")
+    assert ids.tolist() == [[0, 1]] * 2 and (w == 0).all()            # sigmoids of -1200 are 0 in binary32
+
+
+def test_route_shows_what_is_no_number():
+    gen = torch.Generator().manual_seed(2)
+    x, R = torch.randn(6, 40, generator=gen), torch.randn(70, 40, generator=gen)
+    clean = check_route(x, R, 3, "softmax")
+    x[2, 7], x[4, 39] = NAN, NAN
+    for mode in ("softmax", "softmax_all", "sigmoid"):
+        ids, w = check_route(x, R, 3, mode)
+        assert ids[2].tolist() == [0, 1, 2] and torch.isnan(w[[2, 4]]).all() and not torch.isnan(w[[0, 1, 3, 5]]).any()
+        if mode == "softmax":
+            assert torch.equal(ids[[0, 1, 3, 5]], clean[0][[0, 1, 3, 5]]) and torch.equal(w[[0, 1, 3, 5]], clean[1][[0, 1, 3, 5]])
+    bias = torch.zeros(70)
+    bias[9] = NAN
+    assert torch.isnan(check_route(x, R, 3, "sigmoid", bias)[1]).all()
+
+
+def make_experts(gen, E, K, F, apart=0):
+    """Quantised weights of experts on the device, rows and experts `apart` blocks (codes) and words (scales) further from one another, 255 wherever nothing is; and their values."""
+    out = []
+    for rows, size in ((2 * F, K), (K, F)):
+        w = torch.randn(E * rows, size, generator=gen) * (0.5 + torch.rand(E * rows, 1, generator=gen)) * size ** -0.5
+        codes, scales = ref.quantize(w)
+        blocks = scales.shape[1]
+        pc = torch.full((E, rows + apart, 16 * (blocks + apart)), 255, dtype=torch.uint8)
+        ps = torch.full((E, rows + apart, -(-blocks // 4) * 4 + 4 * apart), 255, dtype=torch.uint8)
+        pc[:, :rows, :16 * blocks], ps[:, :rows, :blocks] = ref.pack(codes).view(E, rows, -1), scales.view(E, rows, -1)
+        out += [pc.to(DEV)[:, :rows, :16 * blocks], ps.to(DEV)[:, :rows, :blocks], ref.values(ref.pack(codes), scales, size).view(E, rows, size)]
+    return out
+
+
+def check_experts(weights_held, x, ids, weights):
+    up, ups, vu, down, downs, vd = weights_held
+    T, K = x.shape
+    room = torch.full((T + 1, K + 6), 5.0, dtype=x.dtype, device=DEV)
+    wide = torch.full((T, K + 9), NAN, dtype=x.dtype)
+    wide[:, 3:K + 3] = x
+    out = dg.dg_experts_mx4(up, ups, down, downs, wide.to(DEV)[:, 3:K + 3], ids.to(DEV), weights.to(DEV), out=room[:T, 1:K + 1])
+    want, off = ref.experts(vu, vd, x.double(), ids, weights, x.dtype)
+    ref.assert_within(out, want, off)
+    assert (room[:, 0] == 5).all() and (room[:, K + 1:] == 5).all() and (room[T] == 5).all()
+    assert torch.equal(dg.dg_experts_mx4(up, ups, down, downs, x.to(DEV), ids.to(DEV), weights.to(DEV)).nan_to_num(3), out.nan_to_num(3))
+    return out
+
+
+def choices(gen, T, E, top):
+    return torch.stack([torch.randperm(E, generator=gen)[:top] for _ in range(T)]).to(torch.int32), torch.softmax(torch.randn(T, top, generator=gen), -1)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,E,top,K,F,apart", [(1, 1, 1, 1, 1, 0), (1, 8, 2, 256, 128, 0), (1, 64, 4, 160, 96, 1), (3, 4, 4, 33, 17, 0), (5, 60, 5, 100, 130, 2), (16, 8, 2, 512, 160, 0),
+                                               (37, 6, 3, 131, 65, 1), (64, 3, 1, 96, 64, 0), (40, 200, 2, 64, 33, 0), (130, 5, 2, 70, 40, 0), (9, 16, 8, 1056, 544, 0)])
+def test_experts(T, E, top, K, F, apart, dtype):
+    gen = torch.Generator().manual_seed(T * 31 + E + K + F)
+    held = make_experts(gen, E, K, F, apart)
+    check_experts(held, torch.randn(T, K, generator=gen).to(ref.TYPES[dtype]), *choices(gen, T, E, top))
+
+
+@pytest.mark.parametrize("T,top", [(300, 2), (700, 1), (70, 64)])
+def test_experts_in_turns(T, top):
+    gen = torch.Generator().manual_seed(T)
+    held = make_experts(gen, 66, 32, 32)
+    check_experts(held, torch.randn(T, 32, generator=gen).bfloat16(), *choices(gen, T, 66, top))
+
+
+def test_experts_that_are_none_or_named_twice():
+    gen = torch.Generator().manual_seed(4)
+    held = make_experts(gen, 5, 96, 48)
+    x = torch.randn(20, 96, generator=gen).bfloat16()
+    ids = torch.randint(-2, 7, (20, 3), generator=gen).to(torch.int32)
+    ids[3], ids[4], ids[5] = torch.tensor([[-1, 5, 2 ** 31 - 1], [2, 2, 2], [-2 ** 31, 1, 1]], dtype=torch.int32)
+    out = check_experts(held, x, ids, torch.randn(20, 3, generator=gen))
+    assert (out[3] == 0).all()
+    for t in (1, 2):                                                  # fewer pairs than experts
+        check_experts(held, x[3:3 + t], ids[3:3 + t, :1], torch.ones(t, 1))
+        check_experts(held, x[4:4 + t], ids[4:4 + t, :2], torch.randn(t, 2, generator=gen))
+    everyone = torch.full((20, 1), 3, dtype=torch.int32)
+    check_experts(held, x, everyone, torch.rand(20, 1, generator=gen))
+    assert (check_experts(held, x, torch.full((20, 2), -1, dtype=torch.int32), torch.full((20, 2), NAN)) == 0).all()
+
+
+@pytest.mark.parametrize("T", [2, 40])
+def test_experts_show_what_is_no_number_where_it_is(T):
+    gen = torch.Generator().manual_seed(6)
+    held = make_experts(gen, 6, 100, 70)
+    x = torch.randn(T, 100, generator=gen).bfloat16()
+    ids, w = choices(gen, T, 5, 2)                                    # (expert 5 is nobody's)
+    clean = check_experts(held, x, ids, w)
+    held[1][5], held[4][5] = 255, 255
+    assert torch.equal(check_experts(held, x, ids, w), clean)
+    x[T - 1, 50] = NAN
+    out = check_experts(held, x, ids, w)
+    assert torch.isnan(out[T - 1]).all() and torch.equal(out[:T - 1], clean[:T - 1])
+    # a block of a row of `down` makes a channel no number, one of `up` all of them
+    x[T - 1, 50] = 0.0
+    e = int(ids[0, 0])
+    held[4][e, 13, 2], held[5][e, 13, 64:] = 255, NAN
+    out = check_experts(held, x, ids, w)
+    assert torch.isnan(out[0, 13]) and torch.isnan(out).sum() == (ids == e).any(1).sum()
+    held[1][e, 75, 3], held[2][e, 75, 96:] = 255, NAN
+    out = check_experts(held, x, ids, w)
+    assert torch.equal(torch.isnan(out).any(1).cpu(), (ids == e).any(1))
+
+
+def test_experts_large_values_stay():
+    gen = torch.Generator().manual_seed(8)
+    held = make_experts(gen, 4, 64, 64)
+    x = (torch.randn(6, 64, generator=gen) * 1e4).bfloat16()          # gates of thousands: exp(-g) overflows to where silu is 0
+    check_experts(held, x, *choices(gen, 6, 4, 2))
+    check_experts(held, torch.zeros(6, 64, dtype=torch.float16), *choices(gen, 6, 4, 2))
+
+
+def test_a_layer_on_a_stream_and_in_a_graph():
+    gen = torch.Generator().manual_seed(9)
+    T, E, top, K, F = 12, 16, 4, 128, 96
+    up, ups, _, down, downs, _ = make_experts(gen, E, K, F)
+    x, R = torch.randn(T, K, generator=gen).bfloat16().to(DEV), torch.randn(E, K, generator=gen).bfloat16().to(DEV)
+
+    def layer(**kw):
+        ids, w = dg.dg_route_tokens(x, R, top, **kw)
+        return ids, w, dg.dg_experts_mx4(up, ups, down, downs, x, ids, w, **kw)
+
+    want = layer()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = layer(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ids, w, out = (torch.zeros_like(t) for t in want)
+    works = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (dg.dg_route_tokens_work_bytes(T, E), dg.dg_experts_mx4_work_bytes(T, top, K, F))]
+    graphs = []
+    for _ in range(2):                                                # two graphs of one workspace, replayed behind one another
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            dg.dg_route_tokens(x, R, top, ids=ids, weights=w, work=works[0])
+            dg.dg_experts_mx4(up, ups, down, downs, x, ids, w, work=works[1], out=out)
+    for i in range(4):
+        x.copy_(torch.randn(T, K, generator=gen).bfloat16())
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((ids, w, out), layer()))
+
+
+def test_no_tokens():
+    gen = torch.Generator().manual_seed(10)
+    up, ups, _, down, downs, _ = make_experts(gen, 2, 64, 32)
+    x = torch.empty(0, 64, device=DEV, dtype=torch.float16)
+    ids, w = dg.dg_route_tokens(x, torch.zeros(2, 64, device=DEV), 1)
+    assert ids.shape == (0, 1) and dg.dg_experts_mx4(up, ups, down, downs, x, ids, w).shape == (0, 64)
+
+
+def test_binding_shapes():
+    gen = torch.Generator().manual_seed(10)
+    up, ups, _, down, downs, _ = make_experts(gen, 2, 64, 32)
+    x, ids, w = torch.zeros(3, 64, device=DEV, dtype=torch.float16), torch.zeros(3, 1, device=DEV, dtype=torch.int32), torch.ones(3, 1, device=DEV)
+    for bad, match in (((up, ups, down, downs, x[:, :32], ids, w), "hidden"), ((up, ups, down[:, :33], downs[:, :33], x, ids, w), "down must be"), ((up, ups, down[:1], downs[:1], x, ids, w), "as many experts"),
+                       ((up, ups, down, downs, x, ids[:2], w), "ids"), ((up, ups, down, downs, x, ids, w[:2]), "weights"), ((up, ups, down, downs, x, ids.long(), w), "dtype")):
+        with pytest.raises(ValueError, match=match):
+            dg.dg_experts_mx4(*bad)
+    with pytest.raises(dg.DgError, match="DG_ERR_UNSUPPORTED"):
+        dg.dg_experts_mx4(up, ups, down, downs, x.float(), ids, w)
+    with pytest.raises(ValueError, match="columns"):
+        dg.dg_route_tokens(x, torch.zeros(2, 32, device=DEV), 1)
+    with pytest.raises(ValueError, match="elements"):
+        dg.dg_route_tokens(x, torch.zeros(2, 64, device=DEV), 2, ids=ids, weights=w)

@@ -1,0 +1,171 @@
+"""Microscaled 4-bit floating point on the GPU: quantising and reading back by the byte, products within what the rounding of their sums allows."""
+import pytest
+import torch
+
+import mx4_reference as ref
+from paper_2304_09049_amd import binding as dg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def rows(gen, N, K, dtype, spread=3.0):
+    """Numbers of many sizes, zeros and both zeros' signs among them."""
+    x = torch.randn(N, K, generator=gen) * torch.exp(torch.randn(N, K, generator=gen) * spread)
+    x[torch.rand(N, K, generator=gen) < 0.05] = 0.0
+    x[torch.rand(N, K, generator=gen) < 0.02] = -0.0
+    return x.clamp(-6e4, 6e4).to(dtype)
+
+
+def held(gen, N, K, apart=0):
+    """Quantised normal numbers as a program holds them, codes and scales `apart` words further from row to row, with 255 in every byte that is no scale's."""
+    x = torch.randn(N, K, generator=gen) * (0.5 + torch.rand(N, 1, generator=gen))
+    codes, scales = ref.quantize(x)
+    blocks = scales.shape[1]
+    pc = torch.full((N, 16 * (blocks + apart)), 255, dtype=torch.uint8)
+    ps = torch.full((N, -(-blocks // 4) * 4 + 4 * apart), 255, dtype=torch.uint8)
+    pc[:, :16 * blocks], ps[:, :blocks] = ref.pack(codes), scales
+    return pc.to(DEV)[:, :16 * blocks], ps.to(DEV)[:, :blocks], ref.values(ref.pack(codes), scales, K)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 4096), (3, 31), (5, 32), (2, 33), (17, 100), (9, 5003), (300, 64), (4, 1000)])
+def test_quantize(N, K, dtype):
+    gen = torch.Generator().manual_seed(N * 10007 + K)
+    x = rows(gen, N, K, ref.TYPES[dtype])
+    codes, scales = ref.quantize(x)
+    blocks = scales.shape[1]
+    wide = torch.full((N, K + 5), 3.0, dtype=x.dtype)
+    wide[:, 2:K + 2] = x                                             # (rows that begin anywhere)
+    room_c, room_s = torch.full((N + 1, 16 * blocks + 16), 77, dtype=torch.uint8, device=DEV), torch.full((N + 1, 4 * blocks + 4), 77, dtype=torch.uint8, device=DEV)
+    dg.dg_quantize_mx4(wide.to(DEV)[:, 2:K + 2], room_c[:N, :16 * blocks], room_s[:N, :blocks])
+    assert torch.equal(room_c[:N, :16 * blocks].cpu(), ref.pack(codes)) and torch.equal(room_s[:N, :blocks].cpu(), scales)
+    assert (room_c[:, 16 * blocks:] == 77).all() and (room_s[:, blocks:] == 77).all() and (room_c[N] == 77).all() and (room_s[N] == 77).all()
+    got = dg.dg_quantize_mx4(x.to(DEV))
+    assert torch.equal(got[0].cpu(), ref.pack(codes)) and torch.equal(got[1].cpu(), scales)
+    want = ref.values(ref.pack(codes), scales, K)
+    for to in ref.TYPES.values():
+        out = torch.full((N, K + 3), 9.0, dtype=to, device=DEV)
+        dg.dg_dequantize_mx4(room_c[:N, :16 * blocks], room_s[:N, :blocks], K, out=out[:, 1:K + 1])
+        assert torch.equal(out[:, 1:K + 1].cpu(), want.to(to)) and (out[:, 0] == 9).all() and (out[:, K + 1:] == 9).all()
+    assert torch.equal(dg.dg_dequantize_mx4(*got, K).cpu().double(), want)
+
+
+def test_quantize_the_ends_of_the_range():
+    tiny, huge = 2.0 ** -149, torch.finfo(torch.float32).max
+    x = torch.zeros(8, 64)
+    x[0, :4] = torch.tensor([tiny, -tiny, 3 * tiny, 2.0 ** -127])
+    x[1, :3] = torch.tensor([huge, -huge, 2.0 ** 120])
+    x[2, :2] = torch.tensor([2.0 ** -126, 2.0 ** -128])
+    x[3, 5], x[3, 40] = float("inf"), 1.0
+    x[4, 31], x[4, 32] = float("nan"), 1.0
+    x[5, 0] = -float("inf")
+    x[6, 0], x[6, 1] = 7.9999, -1e-30
+    codes, scales = ref.quantize(x)
+    got = dg.dg_quantize_mx4(x.to(DEV))
+    assert torch.equal(got[0].cpu(), ref.pack(codes)) and torch.equal(got[1].cpu(), scales)
+    assert scales[3].tolist() == [255, 125] and scales[4].tolist() == [255, 125]
+    out, want = dg.dg_dequantize_mx4(*got).cpu(), ref.values(ref.pack(codes), scales, 64)
+    assert torch.equal(out.double().nan_to_num(5), want.nan_to_num(5)) and torch.equal(torch.isnan(out), torch.isnan(want))
+
+
+def test_every_code_and_scale_is_read_back():
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 1)
+    packed = (torch.arange(16)[None, :] | ((15 - torch.arange(16)[None, :]) << 4)).to(torch.uint8).repeat(256, 1)
+    room = torch.zeros(256, 4, dtype=torch.uint8)
+    room[:, :1] = scales
+    want = ref.values(packed, scales, 32)
+    for to in ref.TYPES.values():
+        got = dg.dg_dequantize_mx4(packed.to(DEV), room.to(DEV)[:, :1], dtype=to).cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(7, 8, 9), want.to(to).nan_to_num(7, 8, 9))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N,M,K,bias,apart", [(1, 1, 1, True, 0), (1, 16, 32, False, 1), (2, 17, 100, True, 0), (5, 33, 256, False, 2), (16, 64, 1000, True, 3),
+                                              (17, 100, 2048, False, 0), (31, 257, 4128, True, 1), (33, 65, 544, True, 0), (64, 64, 512, False, 0), (100, 333, 1111, True, 2),
+                                              (130, 515, 288, False, 0), (257, 260, 96, True, 1), (300, 1030, 2600, True, 0), (1, 5000, 8200, True, 0)])
+def test_product(N, M, K, bias, apart, dtype):
+    gen = torch.Generator().manual_seed(N * 7 + M * 131 + K)
+    W, Ws, w = held(gen, M, K, apart)
+    A, As, a = held(gen, N, K, (apart + 1) % 3)
+    b = torch.randn(M, generator=gen) if bias else None
+    want, off = ref.product(a, w, b, ref.TYPES[dtype])
+    room = torch.full((N + 1, M + 7), 5.0, dtype=ref.TYPES[dtype], device=DEV)
+    out = dg.dg_gemm_mx4(W, Ws, A, As, bias=None if b is None else b.to(DEV), out=room[:N, 3:M + 3])
+    ref.assert_within(out, want, off)
+    assert (room[:, :3] == 5).all() and (room[:, M + 3:] == 5).all() and (room[N] == 5).all()
+    again = dg.dg_gemm_mx4(W, Ws, A, As, bias=None if b is None else b.to(DEV), dtype=ref.TYPES[dtype])
+    assert torch.equal(again, out)                                    # the same sums in the same order
+
+
+@pytest.mark.parametrize("N", [1, 20, 200])
+def test_a_block_that_is_none_reaches_its_row_only(N):
+    gen = torch.Generator().manual_seed(3)
+    M, K = 70, 700
+    W, Ws, w = held(gen, M, K)
+    A, As, a = held(gen, N, K)
+    Ws[11, 21], As[N - 1, 3] = 255, 255
+    w[11, 672:], a[N - 1, 96:128] = float("nan"), float("nan")
+    want, off = ref.product(a, w, None, torch.float32)
+    assert torch.isnan(want).sum() == M + N - 1
+    ref.assert_within(dg.dg_gemm_mx4(W, Ws, A, As), want, off)
+
+
+@pytest.mark.parametrize("N,K,dtype", [(0, 64, "bf16"), (1, 4096, "bf16"), (1, 77, "f32"), (7, 2000, "f16"), (40, 333, "f32"), (200, 1024, "bf16")])
+def test_linear_is_quantize_and_product(N, K, dtype):
+    gen = torch.Generator().manual_seed(N + K)
+    W, Ws, _ = held(gen, 150, K)
+    x = rows(gen, N, K + 3, ref.TYPES[dtype], 1.0).to(DEV)[:, 1:K + 1]
+    bias = torch.randn(150, generator=gen).to(DEV)
+    got = dg.dg_linear_mx4(W, Ws, x, bias=bias)
+    assert got.dtype == x.dtype and got.shape == (N, 150)
+    if N:
+        codes, scales = dg.dg_quantize_mx4(x)
+        want, off = ref.product(ref.values(codes.cpu(), scales.cpu(), K), ref.values(W.cpu(), Ws.cpu(), K), bias.cpu(), x.dtype)
+        ref.assert_within(got, want, off)
+
+
+def test_no_tokens():
+    W, Ws = dg.dg_quantize_mx4(torch.randn(5, 64, device=DEV))
+    none = torch.empty(0, 64, device=DEV)
+    codes, scales = dg.dg_quantize_mx4(none)
+    assert codes.shape == (0, 32) and scales.shape == (0, 2) and dg.dg_dequantize_mx4(codes, scales).shape == (0, 64)
+    assert dg.dg_gemm_mx4(W, Ws, codes, scales).shape == (0, 5)
+
+
+def test_streams_and_graphs():
+    gen = torch.Generator().manual_seed(5)
+    W, Ws, w = held(gen, 200, 640)
+    x = torch.randn(50, 640, generator=gen).bfloat16().to(DEV)
+    want = dg.dg_linear_mx4(W, Ws, x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = dg.dg_linear_mx4(W, Ws, x, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    work, out = torch.empty(dg.dg_linear_mx4_work_bytes(50, 640), dtype=torch.uint8, device=DEV), torch.zeros_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dg.dg_linear_mx4(W, Ws, x, work=work, out=out)
+    for i in range(3):
+        x.copy_(torch.randn(50, 640, generator=gen).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, dg.dg_linear_mx4(W, Ws, x))
+
+
+def test_binding_shapes():
+    W, Ws = dg.dg_quantize_mx4(torch.randn(5, 64, device=DEV))
+    A, As = dg.dg_quantize_mx4(torch.randn(3, 96, device=DEV))
+    with pytest.raises(ValueError, match="same number of columns"):
+        dg.dg_gemm_mx4(W, Ws, A, As)
+    with pytest.raises(ValueError, match="16 bytes a block"):
+        dg.dg_gemm_mx4(W, Ws[:4], A, As)
+    with pytest.raises(ValueError, match="16 bytes a block"):
+        dg.dg_dequantize_mx4(A[:, :40], As)
+    with pytest.raises(ValueError, match=r"\[tokens\]\[channels\]"):
+        dg.dg_gemm_mx4(W, Ws, W, Ws, out=torch.empty(5, 6, device=DEV))
+    with pytest.raises(ValueError, match="dtype"):
+        dg.dg_gemm_mx4(W, Ws, W, Ws, bias=torch.zeros(5, device=DEV, dtype=torch.float16))
+    with pytest.raises(dg.DgError, match="DG_ERR_BUFFER"):
+        dg.dg_gemm_mx4(W, torch.zeros(5, 3, dtype=torch.uint8, device=DEV)[:, :2], W, Ws)
