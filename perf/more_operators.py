@@ -217,7 +217,8 @@ def _activations(gen, rows, K, dtype):
 def _weights(gen, rows, K):
     """A layer's weights, each row of its own size, quantised and packed."""
     W = torch.randn(rows, K, device="cuda", generator=gen) * ((0.5 + torch.rand(rows, 1, device="cuda", generator=gen)) / math.sqrt(K))
-    return _pack(*_quantize(W))
+    packed, scales = _pack(*_quantize(W))
+    return packed.to(torch.uint8), scales
 
 
 def _router(case, gen):
@@ -253,7 +254,8 @@ def prepare(case, seed):
         if kind == "linear":
             state["x"] = x
         else:
-            state["A"], state["A_scales"] = _pack(*_quantize(x.float()))
+            A, state["A_scales"] = _pack(*_quantize(x.float()))
+            state["A"] = A.to(torch.uint8)
         return state
     if kind == "experts":
         x = _activations(gen, case["T"], case["K"], case["dtype"])
