@@ -1,11 +1,15 @@
 // Rows quantised to microscaled 4-bit floating point and read back, and products of such rows.
+#include <cstring>
+
 #include "dg_decoder.h"
+#include "dg_lds_dma.h"
 
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 
 // ---- quantising and reading back -----------------------------------------------------------------------------------------
@@ -231,6 +235,266 @@ void launch_few(const DgGemmMx4 &p, hipStream_t stream)
     gemm_mx4_few_kernel<T, 8, 1, 1><<<dim3((p.M + 15) / 16, (p.N + 15) / 16), 512, 0, stream>>>(p);
 }
 
+// ---- many tokens: tiles --------------------------------------------------------------------------------------------------
+//
+// KS groups of WM x WN wavefronts compute 32 WM TM channels x 32 WN TN tokens, TM x TN blocks of 32 x 32 a wavefront; a group takes 256 positions of K, 128 bytes of a row, of a
+// round's 256 KS, and the groups' sums meet in LDS at the end, in the groups' order.  The rounds are a ring in LDS: the next ones' loads, which write LDS themselves, are in
+// flight while one is multiplied.  A row's 128 bytes lie as eight blocks of 16, block c of row r at place c ^ (r / 2 % 8), so that the 16 lanes that an LDS read serves together find
+// 16 different ones.  v_mfma_scale_f32_32x32x64_f8f6f4: lane (r, g) holds block g of two of row r, and names the byte of a register that is its scale: the four steps' are the four bytes.
+// Scales come 16 bytes of a row at a time, 512 positions, by loads of 64 rows.
+
+struct TileArgs {
+    DgGemmMx4 p;
+    int32_t tiles_m, tiles_n;
+    DgFastDiv by_group, by_rest;         // tile order: groups of GROUP rows of tiles
+    int32_t rest;                        // rows of the last group
+};
+constexpr int GROUP = 4;
+
+template <int STEP>
+__device__ __forceinline__ v16f multiply(const v4i &w, const v4i &a, const v16f &c, int ws, int as)
+{
+    const v8i x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, STEP, ws, STEP, as);
+}
+
+template <class T, int WM, int WN, int TM, int TN, int KS, int RING>
+__global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileArgs args)
+{
+    constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128;
+    constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);       // loads of 8 rows a wavefront makes of its group's stage
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole loads, and the same places in each");
+    // Scales: what one load brings of 64 rows, the weights' first; CHUNKS of 512 positions in a round, or (KS = 1) one in two rounds.
+    constexpr int SCALES_M = (BM + 63) / 64, SCALES_N = (BN + 63) / 64, CHUNK = (SCALES_M + SCALES_N) * 1024, CHUNKS = KS > 1 ? KS / 2 : 1;
+    constexpr int CHUNK_RING = KS > 1 ? RING : RING <= 3 ? 2 : 4, SCALE_LOADS = (SCALES_M + SCALES_N) * CHUNKS;
+    constexpr int RESULTS = WAVES * 32 * (32 * TM + 4) * 4, ROOM = RING * STAGE * KS > RESULTS ? RING * STAGE * KS : RESULTS;
+    static_assert(ROOM + CHUNK * CHUNKS * CHUNK_RING <= 160 * 1024, "a compute unit's LDS");
+    __shared__ __align__(1024) uint8_t room[ROOM];
+    __shared__ __align__(1024) uint8_t scale_room[CHUNK * CHUNKS * CHUNK_RING];
+    const DgGemmMx4 &p = args.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % WAVES);
+    const int share = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / WAVES), of_all = wave + WAVES * share;
+    uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room + share * RING;          // (each group has a ring of its own)
+
+    // Neighbouring workgroups go to different dies (eight): each die takes a run of tiles of its own, and walks it in groups of GROUP rows
+    // of tiles, so that what it reads twice is in its own cache.
+    const uint32_t tiles = (uint32_t)args.tiles_m * args.tiles_n, die = blockIdx.x & 7, in_die = blockIdx.x >> 3;
+    const uint32_t tile = die * (tiles >> 3) + min(die, tiles & 7) + in_die;
+    const uint32_t group = dg_fdiv(tile, args.by_group), left = tile - group * (GROUP * args.tiles_n);
+    const bool last = (int32_t)(group * GROUP) + GROUP > args.tiles_m;
+    const uint32_t column = last ? dg_fdiv(left, args.by_rest) : left / GROUP;
+    const int32_t m0 = (int32_t)(group * GROUP + left - column * (last ? args.rest : GROUP)) * BM, n0 = (int32_t)column * BN;
+
+    // what this lane loads: block (lane % 8) ^ ... of row 8 q + lane / 8
+    const int piece = (lane & 7) ^ ((((wave & 1) << 2) + (lane >> 4)) & 7);
+    const int32_t have_w = min(p.M - m0, BM), have_a = min(p.N - n0, BN);
+    constexpr uint32_t NOWHERE = 0xF0000000u;
+    uint32_t offset[LOADS];
+    const auto row_of = [&](int i) { return (wave + WAVES * (i < LOADS_M ? i : i - LOADS_M)) * 8 + (lane >> 3); };
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const uint32_t stride = (uint32_t)(i < LOADS_M ? p.stride_w : p.stride_a);
+        offset[i] = row_of(i) < (i < LOADS_M ? have_w : have_a) ? row_of(i) * stride + 16 * piece : NOWHERE;
+    }
+    const auto buffer = [&](const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes) {
+        return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
+    };
+    const dg_v4i buffer_w = buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_a = buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
+    const int32_t scale_bytes = (p.blocks + 3) / 4 * 4;
+    const dg_v4i buffer_ws = buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes), buffer_as = buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
+    const uint32_t lds = dg_lds_address(room) + share * (RING * STAGE) + 1024 * wave, scale_lds = dg_lds_address(scale_room);
+
+    const auto fetch = [&](int32_t round, int to) {
+        // (the scales before the codes: the waits below count a round's loads of codes, and what was asked for before them is in with them)
+        if (KS > 1 || round % 2 == 0) {
+            const int32_t chunk = KS > 1 ? round * CHUNKS : round / 2, ring = KS > 1 ? to : chunk % CHUNK_RING;
+#pragma unroll
+            for (int i = 0; i < (SCALE_LOADS + WAVES * KS - 1) / (WAVES * KS); ++i) {
+                const int load = of_all + i * (WAVES * KS), c = load / (SCALES_M + SCALES_N), block = load % (SCALES_M + SCALES_N);
+                if (load >= SCALE_LOADS) break;
+                const bool weights = block < SCALES_M;
+                const int row = 64 * (weights ? block : block - SCALES_M) + lane;
+                const int32_t k = 16 * (chunk + c);
+                const uint32_t at = row < (weights ? have_w : have_a) && k < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + k : NOWHERE;
+                dg_load16_to_lds(weights ? buffer_ws : buffer_as, at, scale_lds + ring * (CHUNK * CHUNKS) + load * 1024);
+            }
+        }
+        const int32_t b = 8 * (round * KS + share);
+        const bool past = b + piece >= p.blocks;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t at = past ? NOWHERE : offset[i] + 16 * b;
+            dg_load16_to_lds(i < LOADS_M ? buffer_w : buffer_a, at, lds + to * STAGE + i * (1024 * WAVES));
+        }
+    };
+    const int r = lane & 31, g = lane >> 5, wm = wave % WM, wn = wave / WM;
+    const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
+    v16f acc[TM][TN] = {};
+    // 64 positions at a time; the operands of the next ones are read before these are multiplied
+    v4i wk[2][TM], ak[2][TN];
+    int ws[TM], as[TN];
+    const auto read = [&](int now, int s) {
+        const uint8_t *w = stages[now] + wm * (TM * 4096) + (first ^ (s * 32)), *a = stages[now] + BM * 128 + wn * (TN * 4096) + (first ^ (s * 32));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) wk[s & 1][i] = *(const v4i *)(w + i * 4096);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ak[s & 1][j] = *(const v4i *)(a + j * 4096);
+    };
+    // a lane's four of a row's eight scales; those past the row are 0 (its codes are, and 0 by whatever lies there might be no number)
+    const auto read_scales = [&](int32_t round, int now) {
+        const int32_t ring = KS > 1 ? now : (round / 2) % CHUNK_RING, have = p.blocks - 8 * (round * KS + share);
+        const uint8_t *at = scale_room + ring * (CHUNK * CHUNKS) + (share / 2) * CHUNK + 8 * (KS > 1 ? share & 1 : round & 1) + 16 * r;
+        const uint32_t which = g ? 0x07050301u : 0x06040200u;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const uint2 s = *(const uint2 *)(at + 512 * (wm * TM + i));
+            ws[i] = (int)__builtin_amdgcn_perm(s.y, s.x, which);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const uint2 s = *(const uint2 *)(at + 1024 * SCALES_M + 512 * (wn * TN + j));
+            as[j] = (int)__builtin_amdgcn_perm(s.y, s.x, which);
+        }
+        if (have < 8) {
+            const int count = have > g ? (have - g + 1) / 2 : 0;                      // blocks g, g + 2 ... below `have`
+            const int mask = count >= 4 ? -1 : (int)((1u << (8 * count)) - 1u);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) ws[i] &= mask;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) as[j] &= mask;
+        }
+    };
+    const auto step = [&](int now, auto s_) {
+        constexpr int s = decltype(s_)::value;
+        if (s < 3) read(now, s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = multiply<s>(wk[s & 1][i], ak[s & 1][j], acc[i][j], ws[i], as[j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A round's loads are waited for when its turn comes; the barrier after that says that every wavefront's are in, and that all are done with
+    // the round before, whose place the loads of RING - 1 ahead then take.  (Past the end of K there is nothing to load; the waits count on
+    // loads, so they go on, from outside the buffers: zeros, which nothing reads.)
+    const int32_t rounds = (p.blocks + 8 * KS - 1) / (8 * KS);
+    for (int i = 0; i < RING - 1; ++i) fetch(i, i);
+    int now = 0, to = RING - 1;
+    for (int32_t round = 0; round < rounds; ++round) {
+        dg_wait_for_loads<(RING - 2) * LOADS>();
+        __syncthreads();
+        read_scales(round, now);
+        read(now, 0);
+        fetch(round + RING - 1, to);
+        step(now, std::integral_constant<int, 0>{});
+        step(now, std::integral_constant<int, 1>{});
+        step(now, std::integral_constant<int, 2>{});
+        step(now, std::integral_constant<int, 3>{});
+        now = now + 1 == RING ? 0 : now + 1;
+        to = to + 1 == RING ? 0 : to + 1;
+    }
+    dg_wait_for_loads<0>();
+    // The results go by way of LDS, a wavefront's 32 tokens at a time: rows of channels leave side by side.
+    constexpr int PITCH = 32 * TM + 4, LANES = 8 * TM, ROWS = 64 / LANES;
+    __syncthreads();
+    float *mine = (float *)room + wave * (32 * PITCH);
+    if constexpr (KS > 1) {
+        // the other groups' sums, one group after another
+        static_assert(TM * TN * 4096 * WAVES <= ROOM, "a group's sums fit");
+        float4 *const sums = (float4 *)room + wave * (TM * TN * 256) + lane;
+#pragma unroll 1
+        for (int from = 1; from < KS; ++from) {
+            if (share == from)
+#pragma unroll
+                for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const v16f &c = acc[i / TN][i % TN];
+                        sums[(4 * i + e) * 64] = make_float4(c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]);
+                    }
+            __syncthreads();
+            if (share == 0)
+#pragma unroll
+                for (int i = 0; i < TM * TN; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 x = sums[(4 * i + e) * 64];
+                        v16f &c = acc[i / TN][i % TN];
+                        c[4 * e] += x.x;
+                        c[4 * e + 1] += x.y;
+                        c[4 * e + 2] += x.z;
+                        c[4 * e + 3] += x.w;
+                    }
+            __syncthreads();
+        }
+        if (share) return;
+    }
+    const int32_t m = m0 + wm * (32 * TM) + 4 * (lane % LANES), have = min(p.M - m, 4);
+    float bias[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = p.bias && e < have ? p.bias[m + e] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *(v4f *)(mine + r * PITCH + 32 * i + 8 * e + 4 * g) = (v4f){acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        const int32_t first_n = n0 + (wn * TN + j) * 32, end = min(p.N - first_n, 32);
+#pragma unroll 1
+        for (int t = lane / LANES; t < end; t += ROWS) {
+            const v4f sum = *(const v4f *)(mine + t * PITCH + 4 * (lane % LANES));
+            T *out = (T *)p.out + (int64_t)(first_n + t) * p.stride_out + m;
+            DgVec<T, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y.e[e] = dg_from_float<T>(p.bias ? sum[e] + bias[e] : sum[e]);
+            if (have >= 4) dg_store_vec<T, 4>(out, y);
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) out[e] = y.e[e];
+        }
+    }
+}
+
+template <class T, int WM, int WN, int TM, int TN, int KS, int RING>
+void launch_tiles(const DgGemmMx4 &p, hipStream_t stream)
+{
+    TileArgs a = {p, (p.M + 32 * WM * TM - 1) / (32 * WM * TM), (p.N + 32 * WN * TN - 1) / (32 * WN * TN), {}, {}, 0};
+    a.by_group = dg_make_div((uint32_t)GROUP * a.tiles_n);
+    a.rest = a.tiles_m % GROUP ? a.tiles_m % GROUP : GROUP;
+    a.by_rest = dg_make_div((uint32_t)a.rest);
+    gemm_mx4_tile_kernel<T, WM, WN, TM, TN, KS, RING><<<(uint32_t)a.tiles_m * a.tiles_n, 64 * WM * WN * KS, 0, stream>>>(a);
+}
+
+enum class Form { Few, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
+constexpr int FEW_TOKENS = 32;
+
+Form form_of(const DgGemmMx4 &p)
+{
+    static const struct {
+        Form form;
+        int32_t m, n, cost;
+        const char *name;
+    } tiles[] = {{Form::Tile32x64, 32, 64, 22, "32x64"}, {Form::Tile64x64, 64, 64, 28, "64x64"}, {Form::Tile128x64, 128, 64, 40, "128x64"}, {Form::Tile128x128, 128, 128, 54, "128x128"},
+                 {Form::Tile256x128, 256, 128, 85, "256x128"}, {Form::Tile256x256, 256, 256, 124, "256x256"}};
+    const char *forced = dg_override("DG_GEMM_MX4_TILE");
+    const int64_t units = dg_simd_count() / 4, far = (int64_t)1 << 22;       // (a tile's rows lie within 2^30 bytes)
+    Form best = Form::Few;
+    if (p.stride_w >= far || p.stride_a >= far || p.stride_ws >= far || p.stride_as >= far) return best;
+    if (!forced && p.N <= FEW_TOKENS) return best;
+    int64_t least = INT64_MAX;
+    for (const auto &t : tiles) {
+        if (forced && !strcmp(forced, t.name)) return t.form;
+        const int64_t count = ((p.M + t.m - 1) / t.m) * (int64_t)((p.N + t.n - 1) / t.n), cost = (count + units - 1) / units * t.cost;
+        if (cost < least) {
+            least = cost;
+            best = t.form;
+        }
+    }
+    return p.N <= FEW_TOKENS || (forced && !strcmp(forced, "few")) ? Form::Few : best;
+}
+
 }   // namespace
 
 dg_status dg_launch_quantize_mx4(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, uint8_t *codes, int64_t stride_codes,
@@ -276,7 +540,16 @@ dg_status dg_launch_gemm_mx4(const DgGemmMx4 &all, dg_dtype type, hipStream_t st
             p.M = (int32_t)channels;
             p.N = (int32_t)tokens;
             dg_with_type(type, [&](auto t) {
-                launch_few<decltype(t)>(p, stream);
+                typedef decltype(t) T;
+                switch (form_of(p)) {
+                case Form::Few: launch_few<T>(p, stream); break;
+                case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
+                case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
+                case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
+                case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
+                case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
+                case Form::Tile256x256: launch_tiles<T, 2, 4, 4, 2, 1, 2>(p, stream); break;
+                }
                 return 0;
             });
             return DG_OK;

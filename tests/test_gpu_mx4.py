@@ -98,6 +98,18 @@ def test_product(N, M, K, bias, apart, dtype):
     assert torch.equal(again, out)                                    # the same sums in the same order
 
 
+@pytest.mark.parametrize("tile", ["few", "32x64", "64x64", "128x64", "128x128", "256x128", "256x256"])
+@pytest.mark.parametrize("N,M,K,apart", [(1, 1, 32, 0), (70, 90, 100, 0), (300, 300, 1024, 0), (65, 129, 1312, 1), (257, 520, 2080, 0), (40, 1100, 4444, 3), (1030, 33, 800, 2)])
+def test_product_by_every_tile(N, M, K, apart, tile, monkeypatch):
+    gen = torch.Generator().manual_seed(N * 7 + M * 131 + K)
+    W, Ws, w = held(gen, M, K, apart)
+    A, As, a = held(gen, N, K, apart)
+    bias = torch.randn(M, generator=gen)
+    want, off = ref.product(a, w, bias, torch.float32)
+    monkeypatch.setenv("DG_GEMM_MX4_TILE", tile)
+    ref.assert_within(dg.dg_gemm_mx4(W, Ws, A, As, bias=bias.to(DEV)), want, off)
+
+
 @pytest.mark.parametrize("N", [1, 20, 200])
 def test_a_block_that_is_none_reaches_its_row_only(N):
     gen = torch.Generator().manual_seed(3)
