@@ -251,6 +251,27 @@ struct TileArgs {
 };
 constexpr int GROUP = 4;
 
+// Where tile `number` lies.  Neighbouring workgroups go to different dies (eight): each die takes a run of tiles of its own, and walks it in groups of GROUP rows
+// of tiles, so that what it reads twice is in its own cache.
+template <int BM, int BN>
+__device__ __forceinline__ void place_of(const TileArgs &args, uint32_t number, int32_t &m0, int32_t &n0)
+{
+    const uint32_t tiles = (uint32_t)args.tiles_m * args.tiles_n, die = number & 7, in_die = number >> 3;
+    const uint32_t tile = die * (tiles >> 3) + min(die, tiles & 7) + in_die;
+    const uint32_t group = dg_fdiv(tile, args.by_group), left = tile - group * (GROUP * args.tiles_n);
+    const bool last = (int32_t)(group * GROUP) + GROUP > args.tiles_m;
+    const uint32_t column = last ? dg_fdiv(left, args.by_rest) : left / GROUP;
+    m0 = (int32_t)(group * GROUP + left - column * (last ? args.rest : GROUP)) * BM;
+    n0 = (int32_t)column * BN;
+}
+
+constexpr uint32_t NOWHERE = 0xF0000000u;                // an offset that no buffer has: loads from there are zeros
+// `have` rows from `first` on, of which `bytes` can be read.
+__device__ __forceinline__ dg_v4i rows_buffer(const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes)
+{
+    return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
+}
+
 template <int STEP>
 __device__ __forceinline__ v16f multiply(const v4i &w, const v4i &a, const v16f &c, int ws, int as)
 {
@@ -276,19 +297,12 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
     const int share = KS == 1 ? 0 : __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / WAVES), of_all = wave + WAVES * share;
     uint8_t (*const stages)[STAGE] = (uint8_t(*)[STAGE])room + share * RING;          // (each group has a ring of its own)
 
-    // Neighbouring workgroups go to different dies (eight): each die takes a run of tiles of its own, and walks it in groups of GROUP rows
-    // of tiles, so that what it reads twice is in its own cache.
-    const uint32_t tiles = (uint32_t)args.tiles_m * args.tiles_n, die = blockIdx.x & 7, in_die = blockIdx.x >> 3;
-    const uint32_t tile = die * (tiles >> 3) + min(die, tiles & 7) + in_die;
-    const uint32_t group = dg_fdiv(tile, args.by_group), left = tile - group * (GROUP * args.tiles_n);
-    const bool last = (int32_t)(group * GROUP) + GROUP > args.tiles_m;
-    const uint32_t column = last ? dg_fdiv(left, args.by_rest) : left / GROUP;
-    const int32_t m0 = (int32_t)(group * GROUP + left - column * (last ? args.rest : GROUP)) * BM, n0 = (int32_t)column * BN;
+    int32_t m0, n0;
+    place_of<BM, BN>(args, blockIdx.x, m0, n0);
 
     // what this lane loads: block (lane % 8) ^ ... of row 8 q + lane / 8
     const int piece = (lane & 7) ^ ((((wave & 1) << 2) + (lane >> 4)) & 7);
     const int32_t have_w = min(p.M - m0, BM), have_a = min(p.N - n0, BN);
-    constexpr uint32_t NOWHERE = 0xF0000000u;
     uint32_t offset[LOADS];
     const auto row_of = [&](int i) { return (wave + WAVES * (i < LOADS_M ? i : i - LOADS_M)) * 8 + (lane >> 3); };
 #pragma unroll
@@ -296,12 +310,9 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
         const uint32_t stride = (uint32_t)(i < LOADS_M ? p.stride_w : p.stride_a);
         offset[i] = row_of(i) < (i < LOADS_M ? have_w : have_a) ? row_of(i) * stride + 16 * piece : NOWHERE;
     }
-    const auto buffer = [&](const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes) {
-        return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
-    };
-    const dg_v4i buffer_w = buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_a = buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
     const int32_t scale_bytes = (p.blocks + 3) / 4 * 4;
-    const dg_v4i buffer_ws = buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes), buffer_as = buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
+    const dg_v4i buffer_w = rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_a = rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
+    const dg_v4i buffer_ws = rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes), buffer_as = rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
     const uint32_t lds = dg_lds_address(room) + share * (RING * STAGE) + 1024 * wave, scale_lds = dg_lds_address(scale_room);
 
     const auto fetch = [&](int32_t round, int to) {
@@ -457,14 +468,262 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
     }
 }
 
-template <class T, int WM, int WN, int TM, int TN, int KS, int RING>
-void launch_tiles(const DgGemmMx4 &p, hipStream_t stream)
+// ---- many tokens: wide tiles, one behind another ---------------------------------------------------------------------------
+//
+// WM x WN wavefronts of TM x TN blocks of 32 x 32, stages of 256 positions as above, two of them: one is multiplied in four steps, the other on its way.
+// A compute unit's address unit takes a load's 64 lanes in 16 cycles and more, and a wavefront that asks for more waits with its products: the loads of a stage are spread between the
+// products of two steps.  The last step has its operands in registers: before it the next stage's loads are waited for, and after the barrier, which says that every wavefront's are in and that
+// all have read this stage, the next one's first operands are read and this place is loaded anew.
+// Such tiles leave room for one workgroup a compute unit, which would have nothing to multiply while a tile's results leave and the next one's first stages arrive: a workgroup takes tile
+// after tile, and its loads run on into the next tile's stages.
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+template <class T, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN) void gemm_mx4_stream_kernel(TileArgs args)
 {
-    TileArgs a = {p, (p.M + 32 * WM * TM - 1) / (32 * WM * TM), (p.N + 32 * WN * TN - 1) / (32 * WN * TN), {}, {}, 0};
+    constexpr int WAVES = WM * WN, BM = 32 * WM * TM, BN = 32 * WN * TN, STAGE = (BM + BN) * 128;
+    constexpr int LOADS_M = BM / (8 * WAVES), LOADS = (BM + BN) / (8 * WAVES);                               // of 8 rows
+    constexpr int SCALES_M = BM / 64, SCALE_LOADS = (BM + BN) / 64, CHUNK = SCALE_LOADS * 1024;              // of 64 rows, 512 positions
+    static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && WAVES % 2 == 0 && BM % 64 == 0 && BN % 64 == 0 && TM % 2 == 0, "whole loads, whole lines of results");
+    // results leave 16 tokens at a time, a line of 128 bytes of each; a store is eight of them
+    constexpr int LINE = 128 / sizeof(T), STORES = TM * TN * (int)sizeof(T);
+    __shared__ __align__(1024) uint8_t room[2 * STAGE];
+    __shared__ __align__(1024) uint8_t scale_room[2 * CHUNK];
+    __shared__ __align__(1024) uint8_t way_out[WAVES][2048];
+    const DgGemmMx4 &p = args.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, g = lane >> 5, wm = wave % WM, wn = wave / WM;
+    const uint32_t tiles = (uint32_t)args.tiles_m * args.tiles_n, grid = gridDim.x;
+    const int32_t stages = (p.blocks + 7) / 8, scale_bytes = (p.blocks + 3) / 4 * 4;
+
+    // ---- loads: of tile `loading`, stage `ahead`, into place `to` ----
+    const int piece = (lane & 7) ^ ((((wave & 1) << 2) + (lane >> 4)) & 7);
+    const uint32_t lds = dg_lds_address(room) + 1024 * wave, scale_lds = dg_lds_address(scale_room);
+    uint32_t loading = blockIdx.x, offset[LOADS];
+    int32_t ahead = 0, load_w, load_a, to = 0, scale_to = 0;
+    dg_v4i buffer_w, buffer_a, buffer_ws, buffer_as;
+    const auto begin_loading = [&] {
+        int32_t m, n;
+        place_of<BM, BN>(args, loading, m, n);
+        load_w = min(p.M - m, BM);
+        load_a = min(p.N - n, BN);
+        buffer_w = rows_buffer(p.W, m, p.stride_w, load_w, 16 * p.blocks);
+        buffer_a = rows_buffer(p.A, n, p.stride_a, load_a, 16 * p.blocks);
+        buffer_ws = rows_buffer(p.W_scales, m, p.stride_ws, load_w, scale_bytes);
+        buffer_as = rows_buffer(p.A_scales, n, p.stride_as, load_a, scale_bytes);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const bool weights = i < LOADS_M;
+            const int row = (wave + WAVES * (weights ? i : i - LOADS_M)) * 8 + (lane >> 3);
+            offset[i] = row < (weights ? load_w : load_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece : NOWHERE;
+        }
+    };
+    const auto load_scales = [&] {
+        if (ahead % 2 != 0) return;
+#pragma unroll
+        for (int i = 0; i < (SCALE_LOADS + WAVES - 1) / WAVES; ++i) {
+            const int load = wave + i * WAVES;
+            if (load >= SCALE_LOADS) break;
+            const bool weights = load < SCALES_M;
+            const int row = 64 * (weights ? load : load - SCALES_M) + lane;
+            const uint32_t at = row < (weights ? load_w : load_a) && 8 * ahead < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + 8 * ahead : NOWHERE;
+            dg_load16_to_lds(weights ? buffer_ws : buffer_as, at, scale_lds + scale_to * CHUNK + load * 1024);
+        }
+        scale_to ^= 1;
+    };
+    const auto load_codes = [&](int i) {
+        const uint32_t at = 8 * ahead + piece >= p.blocks ? NOWHERE : offset[i] + 128 * ahead;
+        dg_load16_to_lds(i < LOADS_M ? buffer_w : buffer_a, at, lds + to * STAGE + i * (1024 * WAVES));
+    };
+    const auto next_loads = [&] {
+        to ^= 1;
+        if (++ahead == stages && loading + grid < tiles) {      // (behind the last tile there is nothing to load: from nowhere come zeros, which nothing reads)
+            loading += grid;
+            ahead = 0;
+            begin_loading();
+        }
+    };
+
+    // ---- operands ----
+    const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
+    v16f acc[TM][TN] = {};
+    v4i wk[2][TM], ak[2][TN];
+    uint2 ws_next[TM], as_next[TN];                                  // (a stage's scales are read before the stage before is done with its own)
+    int ws[TM], as[TN];
+    const auto read = [&](int now, int s) {
+        const uint8_t *w = room + now * STAGE + wm * (TM * 4096) + (first ^ (s * 32)), *a = room + now * STAGE + BM * 128 + wn * (TN * 4096) + (first ^ (s * 32));
+#pragma unroll
+        for (int i = 0; i < TM; ++i) wk[s & 1][i] = *(const v4i *)(w + i * 4096);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ak[s & 1][j] = *(const v4i *)(a + j * 4096);
+    };
+    const auto read_scales = [&](int32_t t, int ring) {
+        const uint8_t *at = scale_room + ring * CHUNK + 8 * (t % 2) + 16 * r;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) ws_next[i] = *(const uint2 *)(at + 512 * (wm * TM + i));
+#pragma unroll
+        for (int j = 0; j < TN; ++j) as_next[j] = *(const uint2 *)(at + 16 * BM + 512 * (wn * TN + j));
+    };
+    const auto take_scales = [&](int32_t t) {
+        const uint32_t which = g ? 0x07050301u : 0x06040200u;
+        const int32_t have = p.blocks - 8 * t, count = have > g ? (have - g + 1) / 2 : 0;                   // blocks g, g + 2 ... below `have`
+        const int mask = count >= 4 ? -1 : (int)((1u << (8 * count)) - 1u);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) ws[i] = (int)__builtin_amdgcn_perm(ws_next[i].y, ws_next[i].x, which) & mask;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) as[j] = (int)__builtin_amdgcn_perm(as_next[j].y, as_next[j].x, which) & mask;
+    };
+    // Step s.  Between the products of step 3 half of a stage's loads, and with `more` the others as well; between those of step 0, with `more`, the others.  (Products know no order but
+    // that of their operands: without the asm line all of a stage's are put behind its barrier.)
+    const auto step = [&](auto s_, bool more) __attribute__((always_inline)) {
+        constexpr int s = decltype(s_)::value, HALF = LOADS / 2;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i) {
+            acc[i / TN][i % TN] = multiply<s>(wk[s & 1][i / TN], ak[s & 1][i % TN], acc[i / TN][i % TN], ws[i / TN], as[i % TN]);
+            asm volatile("" : "+v"(acc[i / TN][i % TN]));
+            if constexpr (s == 3) {
+#pragma unroll
+                for (int l = i * HALF / (TM * TN); l < (i + 1) * HALF / (TM * TN); ++l) load_codes(l);
+            }
+            if constexpr (s == 0 || s == 3) {
+                if (more)
+#pragma unroll
+                    for (int l = i * (LOADS - HALF) / (TM * TN); l < (i + 1) * (LOADS - HALF) / (TM * TN); ++l) load_codes(HALF + l);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    begin_loading();
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+        load_scales();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_codes(i);
+        if (t == 0) next_loads();
+    }
+    dg_wait_for_loads<LOADS>();
+    __syncthreads();
+    int now = 0, scales_now = 0;
+    bool asked = true, stored = false;                               // the stage behind this has been asked for whole; stores of the last tile are under way
+    read_scales(0, 0);
+    read(0, 0);
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += grid) {
+#pragma unroll 1
+        for (int32_t t = 0; t < stages; ++t) {
+            const bool over = t + 1 == stages;
+            take_scales(t);
+            read(now, 1);
+            step(Int<0>{}, !asked);
+            read(now, 2);
+            step(Int<1>{}, false);
+            read(now, 3);
+            step(Int<2>{}, false);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (stored) dg_wait_for_loads<STORES>();                 // (the stage was asked for before they were)
+            else dg_wait_for_loads<0>();
+            stored = false;
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            next_loads();
+            if (over || t % 2 == 1) scales_now ^= 1;
+            read_scales(over ? 0 : t + 1, scales_now);
+            read(now ^ 1, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            load_scales();
+            asked = over;
+            step(Int<3>{}, over);
+            now ^= 1;
+        }
+        int32_t m0, n0;
+        place_of<BM, BN>(args, tile, m0, n0);
+        if (p.bias) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                float bias[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) bias[e] = p.bias[min(m0 + 32 * (TM * wm + i) + 8 * (e / 4) + 4 * g + e % 4, p.M - 1)];
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j][e] += bias[e];
+            }
+        }
+        uint8_t *const mine = way_out[wave];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int c = 0; c < 32 * TM / LINE; ++c) {               // lines of channels
+                constexpr int BLOCKS = LINE / 32;                    // of 32 channels in one
+                const int32_t m = m0 + 32 * TM * wm + LINE * c;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (r / 16 == h) {
+#pragma unroll
+                        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const v16f &sum = acc[BLOCKS * c + b][j];
+                                const int32_t at = 32 * b + 8 * e + 4 * g;
+                                DgVec<T, 4> y;
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) y.e[k] = dg_from_float<T>(sum[4 * e + k]);
+                                const uint32_t byte = at * sizeof(T), row = r % 16;
+                                __builtin_memcpy(mine + row * 128 + ((byte / 16 ^ (row / 2 & 7)) * 16 + byte % 16), &y, sizeof(y));
+                            }
+                    }
+                    asm volatile("" ::: "memory");                   // (what other lanes of the wavefront wrote: to LDS their order is that of the instructions)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        constexpr int COUNT = 16 / sizeof(T);
+                        const uint32_t row = 8 * q + lane / 8;
+                        DgVec<T, COUNT> y;
+                        __builtin_memcpy(&y, mine + row * 128 + (((lane & 7) ^ (row / 2 & 7)) * 16), 16);
+                        const int32_t n = n0 + 32 * (TN * wn + j) + 16 * h + row, channel = m + COUNT * (lane & 7);
+                        T *out = (T *)p.out + (int64_t)n * p.stride_out + channel;
+                        if (n < p.N && channel + COUNT <= p.M) {
+                            dg_store_vec<T, COUNT>(out, y);
+                        } else if (n < p.N) {
+#pragma unroll
+                            for (int e = 0; e < COUNT - 1; ++e)
+                                if (channel + e < p.M) out[e] = y.e[e];
+                        }
+                    }
+                    asm volatile("" ::: "memory");
+                }
+            }
+        stored = m0 + BM <= p.M && n0 + BN <= p.N;
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = v16f{};
+    }
+    dg_wait_for_loads<0>();
+}
+
+TileArgs tiles_of(const DgGemmMx4 &p, int32_t bm, int32_t bn)
+{
+    TileArgs a = {p, (p.M + bm - 1) / bm, (p.N + bn - 1) / bn, {}, {}, 0};
     a.by_group = dg_make_div((uint32_t)GROUP * a.tiles_n);
     a.rest = a.tiles_m % GROUP ? a.tiles_m % GROUP : GROUP;
     a.by_rest = dg_make_div((uint32_t)a.rest);
+    return a;
+}
+
+template <class T, int WM, int WN, int TM, int TN, int KS, int RING>
+void launch_tiles(const DgGemmMx4 &p, hipStream_t stream)
+{
+    const TileArgs a = tiles_of(p, 32 * WM * TM, 32 * WN * TN);
     gemm_mx4_tile_kernel<T, WM, WN, TM, TN, KS, RING><<<(uint32_t)a.tiles_m * a.tiles_n, 64 * WM * WN * KS, 0, stream>>>(a);
+}
+
+template <class T, int WM, int WN, int TM, int TN>
+void launch_stream(const DgGemmMx4 &p, hipStream_t stream)
+{
+    const TileArgs a = tiles_of(p, 32 * WM * TM, 32 * WN * TN);
+    const uint32_t tiles = (uint32_t)a.tiles_m * a.tiles_n, units = (uint32_t)dg_simd_count() / 4;
+    // (tiles are places of eight dies; and with a stage of its own a tile would need a third place for its scales)
+    gemm_mx4_stream_kernel<T, WM, WN, TM, TN><<<p.blocks > 8 && units % 8 == 0 ? std::min(tiles, units) : tiles, 64 * WM * WN, 0, stream>>>(a);
 }
 
 enum class Form { Few, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
@@ -476,8 +735,8 @@ Form form_of(const DgGemmMx4 &p)
         Form form;
         int32_t m, n, cost;
         const char *name;
-    } tiles[] = {{Form::Tile32x64, 32, 64, 22, "32x64"}, {Form::Tile64x64, 64, 64, 28, "64x64"}, {Form::Tile128x64, 128, 64, 40, "128x64"}, {Form::Tile128x128, 128, 128, 54, "128x128"},
-                 {Form::Tile256x128, 256, 128, 85, "256x128"}, {Form::Tile256x256, 256, 256, 124, "256x256"}};
+    } tiles[] = {{Form::Tile32x64, 32, 64, 28, "32x64"}, {Form::Tile64x64, 64, 64, 33, "64x64"}, {Form::Tile128x64, 128, 64, 43, "128x64"}, {Form::Tile128x128, 128, 128, 57, "128x128"},
+                 {Form::Tile256x128, 256, 128, 92, "256x128"}, {Form::Tile256x256, 256, 256, 120, "256x256"}};
     const char *forced = dg_override("DG_GEMM_MX4_TILE");
     const int64_t units = dg_simd_count() / 4, far = (int64_t)1 << 22;       // (a tile's rows lie within 2^30 bytes)
     Form best = Form::Few;
@@ -548,7 +807,7 @@ dg_status dg_launch_gemm_mx4(const DgGemmMx4 &all, dg_dtype type, hipStream_t st
                 case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
                 case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
                 case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
-                case Form::Tile256x256: launch_tiles<T, 2, 4, 4, 2, 1, 2>(p, stream); break;
+                case Form::Tile256x256: launch_stream<T, 2, 4, 4, 2>(p, stream); break;
                 }
                 return 0;
             });

@@ -99,7 +99,7 @@ def test_product(N, M, K, bias, apart, dtype):
 
 
 @pytest.mark.parametrize("tile", ["few", "32x64", "64x64", "128x64", "128x128", "256x128", "256x256"])
-@pytest.mark.parametrize("N,M,K,apart", [(1, 1, 32, 0), (70, 90, 100, 0), (300, 300, 1024, 0), (65, 129, 1312, 1), (257, 520, 2080, 0), (40, 1100, 4444, 3), (1030, 33, 800, 2)])
+@pytest.mark.parametrize("N,M,K,apart", [(1, 1, 32, 0), (70, 90, 100, 0), (300, 300, 1024, 0), (65, 129, 1312, 1), (257, 520, 2080, 0), (40, 1100, 4444, 3), (1030, 33, 800, 2), (2100, 8300, 512, 0), (513, 33000, 768, 0)])
 def test_product_by_every_tile(N, M, K, apart, tile, monkeypatch):
     gen = torch.Generator().manual_seed(N * 7 + M * 131 + K)
     W, Ws, w = held(gen, M, K, apart)
