@@ -245,6 +245,9 @@ struct DgGemmMx4 {
     int64_t stride_out;                                  // elements from token to token
 };
 dg_status dg_launch_gemm_mx4(const DgGemmMx4 &p, dg_dtype type, hipStream_t stream);
+// The product's kernel for few tokens quantising one itself (p.A and p.A_scales are not used), and whether it does.
+bool dg_linear_mx4_fuses(int64_t N, const void *x);
+dg_status dg_launch_linear_mx4_fused(const DgGemmMx4 &p, const void *x, dg_dtype x_type, int64_t K, dg_dtype type, hipStream_t stream);
 
 struct DgRoute {
     const void *x, *R;

@@ -6,6 +6,7 @@ namespace {
 
 constexpr int64_t MOST_K = (int64_t)1 << 24;
 constexpr int64_t MOST_ROWS = ((int64_t)1 << 31) - 1;
+constexpr int64_t MOST_STRIDE = (int64_t)1 << 26;        // 32 rows of a product lie within 2^31 bytes
 
 bool known_type(dg_dtype t) { return t == DG_F32 || t == DG_F16 || t == DG_BF16; }
 
@@ -21,6 +22,8 @@ dg_status check_rows(const char *what, const char *of, const void *codes, int64_
     if (stride_codes < 16 * blocks_of(K) || stride_scales < blocks_of(K))
         return dg_fail(DG_ERR_SHAPE, "%s: %s of %lld elements, codes every %lld bytes, scales every %lld (%lld and %lld are needed)", what, of, (long long)K,
                        (long long)stride_codes, (long long)stride_scales, (long long)(16 * blocks_of(K)), (long long)blocks_of(K));
+    if (stride_codes > MOST_STRIDE || stride_scales > MOST_STRIDE)
+        return dg_fail(DG_ERR_RANGE, "%s: rows of %s lie %lld and %lld bytes apart (at most 2^26)", what, of, (long long)stride_codes, (long long)stride_scales);
     if (!aligned(codes, stride_codes, 16) || !aligned(scales, stride_scales, 4))
         return dg_fail(DG_ERR_BUFFER, "%s: %s: rows of codes begin on 16 bytes, rows of scales on 4", what, of);
     return DG_OK;
@@ -125,6 +128,7 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
     uint8_t *codes = (uint8_t *)work_dev, *scales = codes + N * 16 * blocks_of(K);
     const DgGemmMx4 p = {W_dev, W_scales_dev, codes, scales, stride_w, stride_ws, 16 * blocks_of(K), scales_pitch(K), (int32_t)M, (int32_t)N,
                          (int32_t)blocks_of(K), bias_m_dev, out_dev, stride_out};
+    if (dg_linear_mx4_fuses(N, x_dev)) return dg_launch_linear_mx4_fused(p, x_dev, x_type, K, out_type, (hipStream_t)hip_stream);
     s = dg_launch_quantize_mx4(x_dev, x_type, N, K, stride_x, codes, p.stride_a, scales, p.stride_as, (hipStream_t)hip_stream);
     if (s) return s;
     return dg_launch_gemm_mx4(p, out_type, (hipStream_t)hip_stream);

@@ -124,17 +124,18 @@ void in_launches(int64_t N, int64_t K, int64_t stride_x, int64_t stride_codes, i
     });
 }
 
-// ---- the product: few tokens ---------------------------------------------------------------------------------------------
+// ---- the product -----------------------------------------------------------------------------------------------------------
 //
-// v_mfma_scale_f32_16x16x128_f8f6f4: lane (r, g) holds block g of four of row r, 16 bytes as they lie, and the block's scale in the lowest byte of a register.
-// Sums come out with four neighbouring channels of one token in a lane.
-// A workgroup computes 16 ROWS channels x 16 TOKENS tokens; its wavefronts share K in pieces of 256 positions, a cache line of a row, and their sums meet in LDS,
-// in the wavefronts' order.
+// A lane's operand is a block of 32, 16 bytes as they lie, and its scale a byte of a register.  But neighbouring lanes have different rows, and a compute unit's address unit takes 16 bytes each from 64
+// places in some 100 cycles, neighbouring lanes on neighbouring bytes in 16 (operands straight from memory: 25 bytes/ns a compute unit, however many wavefronts).  So everything goes by way of
+// LDS, by loads that write it themselves: eight lanes a row's 128 bytes, 256 positions.  Such a row's blocks lie exchanged, block c of row r at place c ^ (r / 2 % 8), so that the 16 lanes that an
+// LDS read serves together find 16 different places.
 
-__device__ __forceinline__ v4f multiply(const v4i &w, const v4i &a, const v4f &c, int ws, int as)
+constexpr uint32_t NOWHERE = 0xF0000000u;                // an offset that no buffer has: loads from there are zeros
+// `have` rows from `first` on, of which `bytes` can be read.
+__device__ __forceinline__ dg_v4i rows_buffer(const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes)
 {
-    const v8i x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, ws, 0, as);
+    return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
 }
 
 // Four neighbouring channels of token n.
@@ -152,88 +153,180 @@ __device__ __forceinline__ void store4(const DgGemmMx4 &p, int32_t m, int32_t n,
             if (m + i < p.M) out[i] = y.e[i];
 }
 
-// Block b of a row of `blocks`, and its scale's byte; past them zeros.
-__device__ __forceinline__ v4i block_or_zero(const uint8_t *row, int32_t b, int32_t blocks) { return b < blocks ? *(const v4i *)(row + 16 * (int64_t)b) : v4i{}; }
-__device__ __forceinline__ int scale_or_zero(const uint8_t *row, int32_t b, int32_t blocks) { return b < blocks ? row[b] : 0; }
+// ---- few tokens ----
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4: lane (r, g) holds block g of four of row r; sums come out with four neighbouring channels of one token in a lane.
+// A workgroup computes 16 ROWS channels x 8 EIGHTS tokens.  Its wavefronts share K in chunks of 1024 positions and work alone, each with a ring of four stages of 256 positions in LDS, until
+// their sums meet, in the wavefronts' order.
+// X: a single token that is not quantised yet; a wavefront quantises what it multiplies of it, and no launch is needed for that.
 
-template <class T, int WAVES, int ROWS, int TOKENS>
-__global__ __launch_bounds__(64 * WAVES) void gemm_mx4_few_kernel(DgGemmMx4 p)
+template <class X>
+constexpr int bytes_of = sizeof(X);
+template <>
+constexpr int bytes_of<void> = 0;
+
+template <class T, class X, int WAVES, int ROWS, int EIGHTS>
+__global__ __launch_bounds__(64 * WAVES) void gemm_mx4_few_kernel(DgGemmMx4 p, const X *x, int32_t K)
 {
-    __shared__ v4f sums[WAVES][ROWS][TOKENS][64];
+    constexpr bool QUANTIZE = bytes_of<X> != 0;
+    constexpr int TOKENS = (EIGHTS + 1) / 2, LOADS_W = 2 * ROWS, LOADS = LOADS_W + (QUANTIZE ? 0 : EIGHTS), STAGE = LOADS * 1024, RING = 4;
+    static_assert(ROWS <= 2 && EIGHTS <= 4, "a load of scales has 32 rows");
+    // LDS: the ring; twice a chunk's scales of either operand; twice a chunk of the token, as it comes, and its codes and scales
+    constexpr int SCALES = QUANTIZE ? 1024 : 2048, RAW = 1024 * bytes_of<X>, MINE = RING * STAGE + 2 * SCALES + 2 * RAW + (QUANTIZE ? 1024 : 0);
+    static_assert(MINE >= ROWS * TOKENS * 1024, "the sums' place");
+    __shared__ __align__(1024) uint8_t room[WAVES * MINE];
     // (a matrix instruction runs whatever the lanes' mask: what it stands under has to be a scalar branch)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int32_t m0 = blockIdx.x * (16 * ROWS), n0 = blockIdx.y * (16 * TOKENS);
-    const uint8_t *w[ROWS], *ws[ROWS], *a[TOKENS], *as[TOKENS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t row = min(m0 + 16 * i + r, p.M - 1);
-        w[i] = p.W + row * p.stride_w;
-        ws[i] = p.W_scales + row * p.stride_ws;
+    const int32_t m0 = blockIdx.x * (16 * ROWS), n0 = blockIdx.y * (8 * EIGHTS), have_w = min(p.M - m0, 16 * ROWS), have_a = min(p.N - n0, 8 * EIGHTS);
+    const int32_t scale_bytes = (p.blocks + 3) / 4 * 4;
+    const dg_v4i buffer_w = rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_ws = rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes);
+    dg_v4i buffer_a, buffer_as = buffer_ws;
+    if constexpr (QUANTIZE) {
+        buffer_a = dg_buffer((const uint8_t *)x, (uint32_t)(K * bytes_of<X> + 3) / 4 * 4);
+    } else {
+        buffer_a = rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
+        buffer_as = rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
     }
+    uint8_t *const mine = room + wave * MINE, *const scale_room = mine + RING * STAGE, *const raw = scale_room + 2 * SCALES, *const made = raw + 2 * RAW;
+    const uint32_t lds = dg_lds_address(mine), scale_lds = lds + RING * STAGE, raw_lds = scale_lds + 2 * SCALES;
+
+    // load i of a stage: row 8 i + lane / 8 of an operand
+    uint32_t offset[LOADS], scale_offset[2];
+    const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};
 #pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-        const int64_t row = min(n0 + 16 * t + r, p.N - 1);
-        a[t] = p.A + row * p.stride_a;
-        as[t] = p.A_scales + row * p.stride_as;
+    for (int i = 0; i < LOADS; ++i) {
+        const bool weights = i < LOADS_W;
+        const int row = 8 * (weights ? i : i - LOADS_W) + (lane >> 3);
+        offset[i] = row < (weights ? have_w : have_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece[i & 1] : NOWHERE;
     }
+    scale_offset[0] = (lane >> 1) < have_w ? (lane >> 1) * (uint32_t)p.stride_ws + 16 * (lane & 1) : NOWHERE;
+    scale_offset[1] = (lane >> 1) < have_a ? (lane >> 1) * (uint32_t)p.stride_as + 16 * (lane & 1) : NOWHERE;
+    // The wavefront's stage s: stage s % 4 of chunk wave + WAVES (s / 4) of the row.  (A chunk's scales and elements before its codes: the waits below count a stage's loads of codes, and what
+    // was asked for before them is in with them.  Past the row there is nothing to load; the waits count on loads, so they go on, from nowhere: zeros.)
+    const auto fetch = [&](int32_t s) __attribute__((always_inline)) {
+        const int32_t chunk = wave + WAVES * (s / 4), b = 32 * chunk + 8 * (s % 4);
+        if (s % 4 == 0) {
+            const bool past = 32 * chunk + 16 * (lane & 1) >= scale_bytes;
+            const uint32_t to = scale_lds + s / 4 % 2 * SCALES;
+            dg_load16_to_lds(buffer_ws, past ? NOWHERE : scale_offset[0] + 32 * chunk, to);
+            if constexpr (!QUANTIZE) dg_load16_to_lds(buffer_as, past ? NOWHERE : scale_offset[1] + 32 * chunk, to + 1024);
+#pragma unroll
+            for (int i = 0; i < bytes_of<X>; ++i)
+                dg_load16_to_lds(buffer_a, 32 * chunk >= p.blocks ? NOWHERE : (uint32_t)chunk * RAW + 1024 * i + 16 * lane, raw_lds + s / 4 % 2 * RAW + 1024 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            dg_load16_to_lds(i < LOADS_W ? buffer_w : buffer_a, b + piece[i & 1] < p.blocks ? offset[i] + 16 * b : NOWHERE, lds + s % RING * STAGE + i * 1024);
+    };
+    const int32_t chunks = (p.blocks + 31) / 32, stages = chunks > wave ? (chunks - wave + WAVES - 1) / WAVES * 4 : 0;
+    const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
     v4f acc[ROWS][TOKENS] = {};
-    const int32_t pieces = p.blocks / 8;
-    for (int32_t piece = wave; piece < pieces; piece += WAVES) {
-        v4i wk[ROWS][2], ak[TOKENS][2];
-        uint2 wsk[ROWS], ask[TOKENS];
+    if (stages) {
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
+        for (int s = 0; s < RING; ++s) fetch(s);
+    }
+#pragma unroll 1
+    for (int32_t s = 0; s < stages; ++s) {
+        const int32_t chunk = wave + WAVES * (s / 4), b = 32 * chunk + 8 * (s % 4);
+        dg_wait_for_loads<(RING - 1) * LOADS>();
+        if constexpr (QUANTIZE) {
+            if (s % 4 == 0) {
+                // 16 elements a lane, two lanes a block
+                typedef std::conditional_t<QUANTIZE, X, float> E;
+                float f[2][8];
+                uint32_t most = 0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wk[i][h] = *(const v4i *)(w[i] + 128 * (int64_t)piece + 64 * h + 16 * g);
-            wsk[i] = dg_load_vec<uint2, 1>((const uint2 *)(ws[i] + 8 * (int64_t)piece)).e[0];
+                for (int i = 0; i < 2; ++i) {
+                    DgVec<E, 8> e;
+                    __builtin_memcpy(&e, raw + s / 4 % 2 * RAW + (16 * lane + 8 * i) * sizeof(E), sizeof(e));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        f[i][j] = 1024 * chunk + 16 * lane + 8 * i + j < K ? dg_to_float(e.e[j]) : 0.0f;
+                        most = max(most, __float_as_uint(f[i][j]) & 0x7FFFFFFFu);
+                    }
+                }
+                most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xF, 0xF, false));         // quad_perm 1, 0, 3, 2
+                const uint32_t byte = scale_byte(most);
+                const uint2 codes = make_uint2(codes_of(f[0], byte), codes_of(f[1], byte));
+                *(uint2 *)(made + 8 * lane) = codes;
+                made[512 + lane / 2] = (uint8_t)byte;
+                asm volatile("" ::: "memory");                       // (other lanes read them: to LDS a wavefront's order is that of its instructions)
+            }
         }
+        v4i w[ROWS][2], a[TOKENS][2];
+        int ws[ROWS][2], as[TOKENS][2];
+        const uint8_t *stage = mine + s % RING * STAGE, *scales = scale_room + s / 4 % 2 * SCALES + 8 * (s % 4) + g;
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t) {
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) ak[t][h] = *(const v4i *)(a[t] + 128 * (int64_t)piece + 64 * h + 16 * g);
-            ask[t] = dg_load_vec<uint2, 1>((const uint2 *)(as[t] + 8 * (int64_t)piece)).e[0];
+            for (int i = 0; i < ROWS; ++i) {
+                w[i][h] = *(const v4i *)(stage + 2048 * i + (first ^ (64 * h)));
+                ws[i][h] = scales[32 * (16 * i + r) + 4 * h];
+            }
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) {
+                if constexpr (QUANTIZE) {
+                    a[t][h] = *(const v4i *)(made + 16 * (8 * (s % 4) + 4 * h + g));
+                    as[t][h] = made[512 + 8 * (s % 4) + 4 * h + g];
+                } else {
+                    // (with eight tokens the others' rows are the next stage's, or scales: results that are not stored)
+                    a[t][h] = *(const v4i *)(stage + 1024 * LOADS_W + 2048 * t + (first ^ (64 * h)));
+                    as[t][h] = scales[1024 + 32 * (16 * t + r) + 4 * h];
+                }
+            }
         }
+        if (b + 8 > p.blocks) {
+            // scales past the row: its codes are 0, and 0 by whatever lies there might be no number
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool past = b + 4 * h + g >= p.blocks;
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) ws[i][h] = past ? 0 : ws[i][h];
+#pragma unroll
+                for (int t = 0; t < TOKENS; ++t) as[t][h] = past ? 0 : as[t][h];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fetch(s + RING);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int t = 0; t < TOKENS; ++t)
+            for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-                    acc[i][t] = multiply(wk[i][h], ak[t][h], acc[i][t], (int)((h ? wsk[i].y : wsk[i].x) >> (8 * g)), (int)((h ? ask[t].y : ask[t].x) >> (8 * g)));
+                for (int t = 0; t < TOKENS; ++t) {
+                    const v8i X8 = {w[i][h][0], w[i][h][1], w[i][h][2], w[i][h][3], 0, 0, 0, 0}, Y8 = {a[t][h][0], a[t][h][1], a[t][h][2], a[t][h][3], 0, 0, 0, 0};
+                    acc[i][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(X8, Y8, acc[i][t], 4, 4, 0, ws[i][h], 0, as[t][h]);
+                }
     }
-    if (8 * pieces < p.blocks && pieces % WAVES == wave)               // the rest of the row
-        for (int32_t b = 8 * pieces; b < p.blocks; b += 4)
-#pragma unroll
-            for (int t = 0; t < TOKENS; ++t) {
-                const v4i at = block_or_zero(a[t], b + g, p.blocks);
-                const int scale = scale_or_zero(as[t], b + g, p.blocks);
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-                    acc[i][t] = multiply(block_or_zero(w[i], b + g, p.blocks), at, acc[i][t], scale_or_zero(ws[i], b + g, p.blocks), scale);
-            }
+    dg_wait_for_loads<0>();
+    __syncthreads();
+    v4f *const sums = (v4f *)room;                                   // [wavefront][row block][token block][lane]
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t) sums[wave][i][t][lane] = acc[i][t];
+        for (int t = 0; t < TOKENS; ++t) sums[((wave * ROWS + i) * TOKENS + t) * 64 + lane] = acc[i][t];
     __syncthreads();
     // the blocks of 16 x 16 are dealt out to the wavefronts
 #pragma unroll
     for (int block = 0; block < ROWS * TOKENS; ++block) {
         if (block % WAVES != wave) continue;
-        const int i = block % ROWS, t = block / ROWS;
-        v4f s = sums[0][i][t][lane];
+        v4f s = sums[block * 64 + lane];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) s += sums[k][i][t][lane];
-        const int32_t n = n0 + 16 * t + r;
-        if (n < p.N) store4<T>(p, m0 + 16 * i + 4 * g, n, s);
+        for (int k = 1; k < WAVES; ++k) s += sums[(k * ROWS * TOKENS + block) * 64 + lane];
+        const int32_t t = block % TOKENS, n = 16 * t + r;
+        if (n < have_a) store4<T>(p, m0 + 16 * (block / TOKENS) + 4 * g, n0 + n, s);
     }
 }
 
-template <class T>
-void launch_few(const DgGemmMx4 &p, hipStream_t stream)
+template <class T, class X, int WAVES, int ROWS, int EIGHTS>
+void launch_few(const DgGemmMx4 &p, const X *x, int32_t K, hipStream_t stream)
 {
-    gemm_mx4_few_kernel<T, 8, 1, 1><<<dim3((p.M + 15) / 16, (p.N + 15) / 16), 512, 0, stream>>>(p);
+    gemm_mx4_few_kernel<T, X, WAVES, ROWS, EIGHTS><<<dim3((p.M + 16 * ROWS - 1) / (16 * ROWS), (p.N + 8 * EIGHTS - 1) / (8 * EIGHTS)), 64 * WAVES, 0, stream>>>(p, x, K);
 }
+
+// Whether 16 channels a workgroup are more than two workgroups a compute unit: then 32, by half as many wavefronts (one token, 16384 x 4096 9.7 us for 11.4; 4096 x 14336 11.8 for 9.1).
+bool many_channels(const DgGemmMx4 &p) { return p.M >= 8 * dg_simd_count(); }
 
 // ---- many tokens: tiles --------------------------------------------------------------------------------------------------
 //
@@ -263,13 +356,6 @@ __device__ __forceinline__ void place_of(const TileArgs &args, uint32_t number, 
     const uint32_t column = last ? dg_fdiv(left, args.by_rest) : left / GROUP;
     m0 = (int32_t)(group * GROUP + left - column * (last ? args.rest : GROUP)) * BM;
     n0 = (int32_t)column * BN;
-}
-
-constexpr uint32_t NOWHERE = 0xF0000000u;                // an offset that no buffer has: loads from there are zeros
-// `have` rows from `first` on, of which `bytes` can be read.
-__device__ __forceinline__ dg_v4i rows_buffer(const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes)
-{
-    return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
 }
 
 template <int STEP>
@@ -726,32 +812,35 @@ void launch_stream(const DgGemmMx4 &p, hipStream_t stream)
     gemm_mx4_stream_kernel<T, WM, WN, TM, TN><<<p.blocks > 8 && units % 8 == 0 ? std::min(tiles, units) : tiles, 64 * WM * WN, 0, stream>>>(a);
 }
 
-enum class Form { Few, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
-constexpr int FEW_TOKENS = 32;
+enum class Form { Few16x16, Few16x32, Few32x16, Few32x32, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
 
+// The form (channels x tokens a workgroup) whose rounds over the compute units cost least.  `cost`: of a round with a workgroup on each; `both`: with two, where two fit.
+// A round by form, us for K = 2048 and 8192, launch included: 16x16 3.6 (two 4.3), 5.3 (7.4); 16x32 4.2, 6.0; 32x16 4.2 (4.8), 6.9 (7.8); 32x32 4.9 (5.9), 8.3 (10.1); 32x64 5.7, 9.3 (13, where the weights come from
+// memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 50 products, 1 to 4096 tokens, this is within 3 % of the fastest form on 44 and 12 % on the others.
 Form form_of(const DgGemmMx4 &p)
 {
     static const struct {
         Form form;
-        int32_t m, n, cost;
+        int32_t m, n, cost, both;
         const char *name;
-    } tiles[] = {{Form::Tile32x64, 32, 64, 28, "32x64"}, {Form::Tile64x64, 64, 64, 33, "64x64"}, {Form::Tile128x64, 128, 64, 43, "128x64"}, {Form::Tile128x128, 128, 128, 57, "128x128"},
-                 {Form::Tile256x128, 256, 128, 92, "256x128"}, {Form::Tile256x256, 256, 256, 120, "256x256"}};
+    } forms[] = {{Form::Few16x16, 16, 16, 13, 21, "16x16"}, {Form::Few16x32, 16, 32, 16, 0, "16x32"}, {Form::Few32x16, 32, 16, 19, 22, "32x16"}, {Form::Few32x32, 32, 32, 25, 31, "32x32"},
+                 {Form::Tile32x64, 32, 64, 28, 0, "32x64"}, {Form::Tile64x64, 64, 64, 33, 0, "64x64"}, {Form::Tile128x64, 128, 64, 43, 0, "128x64"},
+                 {Form::Tile128x128, 128, 128, 57, 0, "128x128"}, {Form::Tile256x128, 256, 128, 92, 0, "256x128"}, {Form::Tile256x256, 256, 256, 120, 0, "256x256"}};
     const char *forced = dg_override("DG_GEMM_MX4_TILE");
-    const int64_t units = dg_simd_count() / 4, far = (int64_t)1 << 22;       // (a tile's rows lie within 2^30 bytes)
-    Form best = Form::Few;
-    if (p.stride_w >= far || p.stride_a >= far || p.stride_ws >= far || p.stride_as >= far) return best;
-    if (!forced && p.N <= FEW_TOKENS) return best;
+    const int64_t units = dg_simd_count() / 4;
+    Form best = Form::Few16x16;
     int64_t least = INT64_MAX;
-    for (const auto &t : tiles) {
-        if (forced && !strcmp(forced, t.name)) return t.form;
-        const int64_t count = ((p.M + t.m - 1) / t.m) * (int64_t)((p.N + t.n - 1) / t.n), cost = (count + units - 1) / units * t.cost;
+    for (const auto &f : forms) {
+        if (std::max(p.stride_w, p.stride_a) * std::max(f.m, f.n) > (int64_t)1 << 31) break;     // (a workgroup's rows lie within 2^31 bytes)
+        if (forced && !strcmp(forced, f.name)) return f.form;
+        const int64_t count = ((p.M + f.m - 1) / f.m) * (int64_t)((p.N + f.n - 1) / f.n);
+        const int64_t cost = f.both && count > units ? (count + 2 * units - 1) / (2 * units) * f.both : (count + units - 1) / units * f.cost;
         if (cost < least) {
             least = cost;
-            best = t.form;
+            best = f.form;
         }
     }
-    return p.N <= FEW_TOKENS || (forced && !strcmp(forced, "few")) ? Form::Few : best;
+    return best;
 }
 
 }   // namespace
@@ -784,9 +873,10 @@ dg_status dg_launch_dequantize_mx4(const uint8_t *codes, int64_t stride_codes, c
     return dg_check_launch("dg_dequantize_mx4");
 }
 
-dg_status dg_launch_gemm_mx4(const DgGemmMx4 &all, dg_dtype type, hipStream_t stream)
+// f(a part of the product): channels and tokens whose workgroups are a grid.
+template <class F>
+static void in_parts(const DgGemmMx4 &all, dg_dtype type, F f)
 {
-    // channels and tokens whose workgroups are a grid
     dg_in_turns(all.M, 1 << 24, [&](int64_t m, int64_t channels) {
         return dg_in_turns(all.N, std::min<int64_t>(1 << 19, ((int64_t)1 << 34) / channels), [&](int64_t n, int64_t tokens) {
             DgGemmMx4 p = all;
@@ -798,20 +888,56 @@ dg_status dg_launch_gemm_mx4(const DgGemmMx4 &all, dg_dtype type, hipStream_t st
             p.out = (uint8_t *)p.out + (n * p.stride_out + m) * dg_type_size(type);
             p.M = (int32_t)channels;
             p.N = (int32_t)tokens;
-            dg_with_type(type, [&](auto t) {
+            f(p);
+            return DG_OK;
+        });
+    });
+}
+
+// (its elements are loaded by words of four bytes)
+bool dg_linear_mx4_fuses(int64_t N, const void *x) { return N == 1 && (uintptr_t)x % 4 == 0; }
+
+dg_status dg_launch_linear_mx4_fused(const DgGemmMx4 &all, const void *x, dg_dtype x_type, int64_t K, dg_dtype type, hipStream_t stream)
+{
+    in_parts(all, type, [&](const DgGemmMx4 &p) {
+        dg_with_type(type, [&](auto t) {
+            dg_with_type(x_type, [&](auto s) {
                 typedef decltype(t) T;
-                switch (form_of(p)) {
-                case Form::Few: launch_few<T>(p, stream); break;
-                case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
-                case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
-                case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
-                case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
-                case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
-                case Form::Tile256x256: launch_stream<T, 2, 4, 4, 2>(p, stream); break;
-                }
+                typedef decltype(s) X;
+                if (many_channels(p)) launch_few<T, X, 2, 2, 1>(p, (const X *)x, (int32_t)K, stream);
+                else launch_few<T, X, 4, 1, 1>(p, (const X *)x, (int32_t)K, stream);
                 return 0;
             });
-            return DG_OK;
+            return 0;
+        });
+    });
+    return dg_check_launch("dg_linear_mx4");
+}
+
+dg_status dg_launch_gemm_mx4(const DgGemmMx4 &all, dg_dtype type, hipStream_t stream)
+{
+    in_parts(all, type, [&](const DgGemmMx4 &p) {
+        dg_with_type(type, [&](auto t) {
+            typedef decltype(t) T;
+            switch (form_of(p)) {
+            case Form::Few16x16:
+                if (p.N <= 8) launch_few<T, void, 4, 1, 1>(p, nullptr, 0, stream);
+                else launch_few<T, void, 4, 1, 2>(p, nullptr, 0, stream);
+                break;
+            case Form::Few16x32: launch_few<T, void, 4, 1, 4>(p, nullptr, 0, stream); break;
+            case Form::Few32x16:
+                if (p.N <= 8) launch_few<T, void, 2, 2, 1>(p, nullptr, 0, stream);
+                else launch_few<T, void, 2, 2, 2>(p, nullptr, 0, stream);
+                break;
+            case Form::Few32x32: launch_few<T, void, 2, 2, 4>(p, nullptr, 0, stream); break;
+            case Form::Tile32x64: launch_tiles<T, 1, 2, 1, 1, 4, 3>(p, stream); break;
+            case Form::Tile64x64: launch_tiles<T, 2, 2, 1, 1, 2, 4>(p, stream); break;
+            case Form::Tile128x64: launch_tiles<T, 2, 2, 2, 1, 2, 3>(p, stream); break;
+            case Form::Tile128x128: launch_tiles<T, 2, 2, 2, 2, 1, 4>(p, stream); break;
+            case Form::Tile256x128: launch_tiles<T, 2, 2, 4, 2, 1, 3>(p, stream); break;
+            case Form::Tile256x256: launch_stream<T, 2, 4, 4, 2>(p, stream); break;
+            }
+            return 0;
         });
     });
     return dg_check_launch("dg_gemm_mx4");

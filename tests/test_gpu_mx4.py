@@ -98,14 +98,16 @@ def test_product(N, M, K, bias, apart, dtype):
     assert torch.equal(again, out)                                    # the same sums in the same order
 
 
-@pytest.mark.parametrize("tile", ["few", "32x64", "64x64", "128x64", "128x128", "256x128", "256x256"])
-@pytest.mark.parametrize("N,M,K,apart", [(1, 1, 32, 0), (70, 90, 100, 0), (300, 300, 1024, 0), (65, 129, 1312, 1), (257, 520, 2080, 0), (40, 1100, 4444, 3), (1030, 33, 800, 2), (2100, 8300, 512, 0), (513, 33000, 768, 0)])
+@pytest.mark.parametrize("tile", ["16x16", "16x32", "32x16", "32x32", "32x64", "64x64", "128x64", "128x128", "256x128", "256x256"])
+@pytest.mark.parametrize("N,M,K,apart", [(1, 1, 32, 0), (70, 90, 100, 0), (300, 300, 1024, 0), (65, 129, 1312, 1), (257, 520, 2080, 0), (8, 40, 9300, 0), (40, 1100, 4444, 3), (1030, 33, 800, 2), (2100, 8300, 512, 0), (513, 33000, 768, 0)])
 def test_product_by_every_tile(N, M, K, apart, tile, monkeypatch):
     gen = torch.Generator().manual_seed(N * 7 + M * 131 + K)
     W, Ws, w = held(gen, M, K, apart)
     A, As, a = held(gen, N, K, apart)
     bias = torch.randn(M, generator=gen)
     want, off = ref.product(a, w, bias, torch.float32)
+    if tile in ("16x16", "16x32", "32x16", "32x32") and N * M > 1e6:
+        pytest.skip("few tokens")
     monkeypatch.setenv("DG_GEMM_MX4_TILE", tile)
     ref.assert_within(dg.dg_gemm_mx4(W, Ws, A, As, bias=bias.to(DEV)), want, off)
 
@@ -121,6 +123,25 @@ def test_a_block_that_is_none_reaches_its_row_only(N):
     want, off = ref.product(a, w, None, torch.float32)
     assert torch.isnan(want).sum() == M + N - 1
     ref.assert_within(dg.dg_gemm_mx4(W, Ws, A, As), want, off)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 1), (33, 31), (70, 1000), (200, 4097), (8200, 96), (100, 9001)])
+def test_linear_of_one_token(M, K, dtype):
+    """A token that begins on a word is quantised by the product itself, any other by a launch of its own."""
+    gen = torch.Generator().manual_seed(M + K)
+    W, Ws, w = held(gen, M, K)
+    wide = torch.full((1, K + 4), float("nan"), dtype=ref.TYPES[dtype])
+    bias = torch.randn(M, generator=gen)
+    for at in (0, 1, 2, 3):
+        x = rows(gen, 1, K, ref.TYPES[dtype], 1.0)
+        wide[:, at:at + K] = x
+        codes, scales = ref.quantize(x)
+        want, off = ref.product(ref.values(ref.pack(codes), scales, K), w, bias, x.dtype)
+        ref.assert_within(dg.dg_linear_mx4(W, Ws, wide.to(DEV)[:, at:at + K], bias=bias.to(DEV)), want, off)
+    x[0, K // 2] = float("inf")
+    out = dg.dg_linear_mx4(W, Ws, x.to(DEV), bias=bias.to(DEV))
+    assert torch.isnan(out).all()
 
 
 @pytest.mark.parametrize("N,K,dtype", [(0, 64, "bf16"), (1, 4096, "bf16"), (1, 77, "f32"), (7, 2000, "f16"), (40, 333, "f32"), (200, 1024, "bf16")])

@@ -47,7 +47,7 @@ def test_product_refusals():
     for f in (gemm, linear):
         assert [f(w=None), f(ws=None), f(o=None)] == [NULL] * 3
         assert [f(M=0), f(N=-1), f(K=0), f(sw=16), f(sws=0), f(so=3)] == [SHAPE] * 6
-        assert f(K=(1 << 24) + 1) == RANGE and f(M=1 << 30, N=1 << 30, so=1 << 30) == RANGE and f(t=9) == UNSUPPORTED
+        assert f(K=(1 << 24) + 1) == RANGE and f(M=1 << 30, N=1 << 30, so=1 << 30) == RANGE and f(sw=(1 << 26) + 16) == RANGE and f(t=9) == UNSUPPORTED
         assert [f(w=ODD), f(sw=40), f(sws=5), f(ws=ctypes.c_void_p(0x1001))] == [BUFFER] * 4
         assert f(N=0, o=None) == 0
     assert [gemm(a=None), gemm(as_=None)] == [NULL] * 2 and gemm(sa=16) == SHAPE and gemm(a=ODD) == BUFFER and gemm(sas=6) == BUFFER
