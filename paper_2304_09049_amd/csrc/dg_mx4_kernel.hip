@@ -1,8 +1,7 @@
 // Rows quantised to microscaled 4-bit floating point and read back, and products of such rows.
 #include <cstring>
 
-#include "dg_decoder.h"
-#include "dg_lds_dma.h"
+#include "dg_mx4.h"
 
 namespace {
 
@@ -131,13 +130,6 @@ void in_launches(int64_t N, int64_t K, int64_t stride_x, int64_t stride_codes, i
 // LDS, by loads that write it themselves: eight lanes a row's 128 bytes, 256 positions.  Such a row's blocks lie exchanged, block c of row r at place c ^ (r / 2 % 8), so that the 16 lanes that an
 // LDS read serves together find 16 different places.
 
-constexpr uint32_t NOWHERE = 0xF0000000u;                // an offset that no buffer has: loads from there are zeros
-// `have` rows from `first` on, of which `bytes` can be read.
-__device__ __forceinline__ dg_v4i rows_buffer(const uint8_t *rows, int64_t first, int64_t stride, int32_t have, int32_t bytes)
-{
-    return dg_buffer(rows + first * stride, (uint32_t)((have - 1) * (uint32_t)stride + bytes));
-}
-
 // Four neighbouring channels of token n.
 template <class T>
 __device__ __forceinline__ void store4(const DgGemmMx4 &p, int32_t m, int32_t n, const v4f &sum)
@@ -179,13 +171,13 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx4_few_kernel(DgGemmMx4 p, c
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t m0 = blockIdx.x * (16 * ROWS), n0 = blockIdx.y * (8 * EIGHTS), have_w = min(p.M - m0, 16 * ROWS), have_a = min(p.N - n0, 8 * EIGHTS);
     const int32_t scale_bytes = (p.blocks + 3) / 4 * 4;
-    const dg_v4i buffer_w = rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_ws = rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes);
+    const dg_v4i buffer_w = dg_rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_ws = dg_rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes);
     dg_v4i buffer_a, buffer_as = buffer_ws;
     if constexpr (QUANTIZE) {
         buffer_a = dg_buffer((const uint8_t *)x, (uint32_t)(K * bytes_of<X> + 3) / 4 * 4);
     } else {
-        buffer_a = rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
-        buffer_as = rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
+        buffer_a = dg_rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
+        buffer_as = dg_rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
     }
     uint8_t *const mine = room + wave * MINE, *const scale_room = mine + RING * STAGE, *const raw = scale_room + 2 * SCALES, *const made = raw + 2 * RAW;
     const uint32_t lds = dg_lds_address(mine), scale_lds = lds + RING * STAGE, raw_lds = scale_lds + 2 * SCALES;
@@ -197,10 +189,10 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx4_few_kernel(DgGemmMx4 p, c
     for (int i = 0; i < LOADS; ++i) {
         const bool weights = i < LOADS_W;
         const int row = 8 * (weights ? i : i - LOADS_W) + (lane >> 3);
-        offset[i] = row < (weights ? have_w : have_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece[i & 1] : NOWHERE;
+        offset[i] = row < (weights ? have_w : have_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece[i & 1] : DG_NOWHERE;
     }
-    scale_offset[0] = (lane >> 1) < have_w ? (lane >> 1) * (uint32_t)p.stride_ws + 16 * (lane & 1) : NOWHERE;
-    scale_offset[1] = (lane >> 1) < have_a ? (lane >> 1) * (uint32_t)p.stride_as + 16 * (lane & 1) : NOWHERE;
+    scale_offset[0] = (lane >> 1) < have_w ? (lane >> 1) * (uint32_t)p.stride_ws + 16 * (lane & 1) : DG_NOWHERE;
+    scale_offset[1] = (lane >> 1) < have_a ? (lane >> 1) * (uint32_t)p.stride_as + 16 * (lane & 1) : DG_NOWHERE;
     // The wavefront's stage s: stage s % 4 of chunk wave + WAVES (s / 4) of the row.  (A chunk's scales and elements before its codes: the waits below count a stage's loads of codes, and what
     // was asked for before them is in with them.  Past the row there is nothing to load; the waits count on loads, so they go on, from nowhere: zeros.)
     const auto fetch = [&](int32_t s) __attribute__((always_inline)) {
@@ -208,15 +200,15 @@ __global__ __launch_bounds__(64 * WAVES) void gemm_mx4_few_kernel(DgGemmMx4 p, c
         if (s % 4 == 0) {
             const bool past = 32 * chunk + 16 * (lane & 1) >= scale_bytes;
             const uint32_t to = scale_lds + s / 4 % 2 * SCALES;
-            dg_load16_to_lds(buffer_ws, past ? NOWHERE : scale_offset[0] + 32 * chunk, to);
-            if constexpr (!QUANTIZE) dg_load16_to_lds(buffer_as, past ? NOWHERE : scale_offset[1] + 32 * chunk, to + 1024);
+            dg_load16_to_lds(buffer_ws, past ? DG_NOWHERE : scale_offset[0] + 32 * chunk, to);
+            if constexpr (!QUANTIZE) dg_load16_to_lds(buffer_as, past ? DG_NOWHERE : scale_offset[1] + 32 * chunk, to + 1024);
 #pragma unroll
             for (int i = 0; i < bytes_of<X>; ++i)
-                dg_load16_to_lds(buffer_a, 32 * chunk >= p.blocks ? NOWHERE : (uint32_t)chunk * RAW + 1024 * i + 16 * lane, raw_lds + s / 4 % 2 * RAW + 1024 * i);
+                dg_load16_to_lds(buffer_a, 32 * chunk >= p.blocks ? DG_NOWHERE : (uint32_t)chunk * RAW + 1024 * i + 16 * lane, raw_lds + s / 4 % 2 * RAW + 1024 * i);
         }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
-            dg_load16_to_lds(i < LOADS_W ? buffer_w : buffer_a, b + piece[i & 1] < p.blocks ? offset[i] + 16 * b : NOWHERE, lds + s % RING * STAGE + i * 1024);
+            dg_load16_to_lds(i < LOADS_W ? buffer_w : buffer_a, b + piece[i & 1] < p.blocks ? offset[i] + 16 * b : DG_NOWHERE, lds + s % RING * STAGE + i * 1024);
     };
     const int32_t chunks = (p.blocks + 31) / 32, stages = chunks > wave ? (chunks - wave + WAVES - 1) / WAVES * 4 : 0;
     const uint32_t first = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
@@ -394,11 +386,11 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const uint32_t stride = (uint32_t)(i < LOADS_M ? p.stride_w : p.stride_a);
-        offset[i] = row_of(i) < (i < LOADS_M ? have_w : have_a) ? row_of(i) * stride + 16 * piece : NOWHERE;
+        offset[i] = row_of(i) < (i < LOADS_M ? have_w : have_a) ? row_of(i) * stride + 16 * piece : DG_NOWHERE;
     }
     const int32_t scale_bytes = (p.blocks + 3) / 4 * 4;
-    const dg_v4i buffer_w = rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_a = rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
-    const dg_v4i buffer_ws = rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes), buffer_as = rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
+    const dg_v4i buffer_w = dg_rows_buffer(p.W, m0, p.stride_w, have_w, 16 * p.blocks), buffer_a = dg_rows_buffer(p.A, n0, p.stride_a, have_a, 16 * p.blocks);
+    const dg_v4i buffer_ws = dg_rows_buffer(p.W_scales, m0, p.stride_ws, have_w, scale_bytes), buffer_as = dg_rows_buffer(p.A_scales, n0, p.stride_as, have_a, scale_bytes);
     const uint32_t lds = dg_lds_address(room) + share * (RING * STAGE) + 1024 * wave, scale_lds = dg_lds_address(scale_room);
 
     const auto fetch = [&](int32_t round, int to) {
@@ -412,7 +404,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
                 const bool weights = block < SCALES_M;
                 const int row = 64 * (weights ? block : block - SCALES_M) + lane;
                 const int32_t k = 16 * (chunk + c);
-                const uint32_t at = row < (weights ? have_w : have_a) && k < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + k : NOWHERE;
+                const uint32_t at = row < (weights ? have_w : have_a) && k < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + k : DG_NOWHERE;
                 dg_load16_to_lds(weights ? buffer_ws : buffer_as, at, scale_lds + ring * (CHUNK * CHUNKS) + load * 1024);
             }
         }
@@ -420,7 +412,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
         const bool past = b + piece >= p.blocks;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const uint32_t at = past ? NOWHERE : offset[i] + 16 * b;
+            const uint32_t at = past ? DG_NOWHERE : offset[i] + 16 * b;
             dg_load16_to_lds(i < LOADS_M ? buffer_w : buffer_a, at, lds + to * STAGE + i * (1024 * WAVES));
         }
     };
@@ -594,15 +586,15 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_mx4_stream_kernel(TileArgs 
         place_of<BM, BN>(args, loading, m, n);
         load_w = min(p.M - m, BM);
         load_a = min(p.N - n, BN);
-        buffer_w = rows_buffer(p.W, m, p.stride_w, load_w, 16 * p.blocks);
-        buffer_a = rows_buffer(p.A, n, p.stride_a, load_a, 16 * p.blocks);
-        buffer_ws = rows_buffer(p.W_scales, m, p.stride_ws, load_w, scale_bytes);
-        buffer_as = rows_buffer(p.A_scales, n, p.stride_as, load_a, scale_bytes);
+        buffer_w = dg_rows_buffer(p.W, m, p.stride_w, load_w, 16 * p.blocks);
+        buffer_a = dg_rows_buffer(p.A, n, p.stride_a, load_a, 16 * p.blocks);
+        buffer_ws = dg_rows_buffer(p.W_scales, m, p.stride_ws, load_w, scale_bytes);
+        buffer_as = dg_rows_buffer(p.A_scales, n, p.stride_as, load_a, scale_bytes);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const bool weights = i < LOADS_M;
             const int row = (wave + WAVES * (weights ? i : i - LOADS_M)) * 8 + (lane >> 3);
-            offset[i] = row < (weights ? load_w : load_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece : NOWHERE;
+            offset[i] = row < (weights ? load_w : load_a) ? row * (uint32_t)(weights ? p.stride_w : p.stride_a) + 16 * piece : DG_NOWHERE;
         }
     };
     const auto load_scales = [&] {
@@ -613,13 +605,13 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_mx4_stream_kernel(TileArgs 
             if (load >= SCALE_LOADS) break;
             const bool weights = load < SCALES_M;
             const int row = 64 * (weights ? load : load - SCALES_M) + lane;
-            const uint32_t at = row < (weights ? load_w : load_a) && 8 * ahead < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + 8 * ahead : NOWHERE;
+            const uint32_t at = row < (weights ? load_w : load_a) && 8 * ahead < scale_bytes ? row * (uint32_t)(weights ? p.stride_ws : p.stride_as) + 8 * ahead : DG_NOWHERE;
             dg_load16_to_lds(weights ? buffer_ws : buffer_as, at, scale_lds + scale_to * CHUNK + load * 1024);
         }
         scale_to ^= 1;
     };
     const auto load_codes = [&](int i) {
-        const uint32_t at = 8 * ahead + piece >= p.blocks ? NOWHERE : offset[i] + 128 * ahead;
+        const uint32_t at = 8 * ahead + piece >= p.blocks ? DG_NOWHERE : offset[i] + 128 * ahead;
         dg_load16_to_lds(i < LOADS_M ? buffer_w : buffer_a, at, lds + to * STAGE + i * (1024 * WAVES));
     };
     const auto next_loads = [&] {
