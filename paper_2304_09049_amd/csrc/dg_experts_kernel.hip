@@ -18,7 +18,7 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int MOST_PAIRS = 4096;         // of a turn: their numbers are 16-bit
 constexpr int MOST_TOKENS = 256;
-constexpr int FEW_PAIRS = 32;            // each pair by itself
+constexpr int FEW_PAIRS = 16;            // each pair by itself
 
 // Rows of activations as the products take them: PLANES of bfloat16 whose sum is the number, rows that begin on 4 bytes, `pitch` elements from the next, `size` of them counting; from there to the next multiple
 // of 8 they are 0.
@@ -277,13 +277,13 @@ __global__ __launch_bounds__(512) void experts_few_down_kernel(DgExperts p, Rows
 
 // ---- more pairs: an expert's together --------------------------------------------------------------------------------------
 //
-// A workgroup has four times 16 channels of `up` (gates and others) or 32 of `down`, a wavefront each, and 16 COLUMNS of the expert's pairs at a time.  A wavefront's rows come into a ring of its own, the pairs'
-// activations into one that all four read.  With fewer pairs than experts a workgroup's slot is a pair, whose expert it takes unless an earlier pair names it too, otherwise an expert.
+// A wavefront has 16 channels of `up` (gates and others) or 32 of `down`, a workgroup 16 COLUMNS of the expert's pairs at a time.  A wavefront's rows come into a ring of its own, the pairs' activations into one that
+// all of the workgroup's read.  With fewer pairs than experts a workgroup's slot is a pair, whose expert it takes unless an earlier pair names it too, otherwise an expert.
 
-template <bool UP, int COLUMNS, int PLANES, int RING>
-__global__ __launch_bounds__(256) void experts_kernel(DgExperts p, Rows rows, Work work)
+template <bool UP, int WAVES, int COLUMNS, int PLANES, int RING>
+__global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows rows, Work work)
 {
-    constexpr int WAVES = 4, LOADS_X = 2 * COLUMNS * PLANES, LOADS = 4 + LOADS_X, STAGE_W = 4096, STAGE_X = COLUMNS * PLANES * 8192, SCALES = 1024;
+    constexpr int LOADS_X = 8 * COLUMNS * PLANES / WAVES, LOADS = 4 + LOADS_X, STAGE_W = 4096, STAGE_X = COLUMNS * PLANES * 8192, SCALES = 1024;
     __shared__ __align__(1024) uint8_t room[RING * (WAVES * STAGE_W + STAGE_X) + WAVES * 2 * SCALES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t pairs = p.T * p.top, slot = blockIdx.y, blocks = ((UP ? p.d.hidden : p.d.inner) + 31) / 32;
@@ -295,13 +295,20 @@ __global__ __launch_bounds__(256) void experts_kernel(DgExperts p, Rows rows, Wo
     uint16_t *const list = (uint16_t *)mine;
     const auto find = [&](int32_t from) __attribute__((always_inline)) {
         int32_t n = 0;
-        for (int32_t at = 0; at < pairs; at += 64) {
-            const bool is = at + lane < pairs && p.ids[at + lane] == expert;
-            const uint64_t which = __ballot(is);
-            if (by_pair && n == 0 && which && at + __builtin_ctzll(which) != slot) return 0;
-            const int32_t number = n + __builtin_popcountll(which & ((1ull << lane) - 1)) - from;
-            if (is && number >= 0 && number < 16 * COLUMNS) list[number] = (uint16_t)(at + lane);
-            n += __builtin_popcountll(which);
+        for (int32_t first = 0; first < pairs; first += 512) {
+            int32_t ids[8];                                          // (asked for together: one after another each would be a wait)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ids[i] = first + 64 * i + lane < pairs ? p.ids[first + 64 * i + lane] : -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool is = ids[i] == expert;
+                const uint64_t which = __ballot(is);
+                if (!which) continue;
+                if (by_pair && n == 0 && first + 64 * i + __builtin_ctzll(which) != slot) return 0;
+                const int32_t number = n + __builtin_popcountll(which & ((1ull << lane) - 1)) - from;
+                if (is && number >= 0 && number < 16 * COLUMNS) list[number] = (uint16_t)(first + 64 * i + lane);
+                n += __builtin_popcountll(which);
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         return n;
@@ -331,17 +338,17 @@ __global__ __launch_bounds__(256) void experts_kernel(DgExperts p, Rows rows, Wo
             find(column);
         }
         const int32_t here = min(count - column, 16 * COLUMNS);
-        // load i of a wavefront's share of the activations: rows 2 q and 2 q + 1 of the planes behind one another, q = wave + 4 i; place l of a row holds piece l ^ (row % 16)
-        const int piece = (lane & 31) ^ (2 * wave + (lane >> 5));    // (of odd loads, whose rows are 8 further, 8 more: a bit of the piece's)
+        // load i of a wavefront's share of the activations: rows 2 q and 2 q + 1 of the planes behind one another, q = wave + WAVES i; place l of a row holds piece l ^ (row % 16)
+        const auto piece = [&](int i) { return (lane & 31) ^ ((2 * (wave + WAVES * i) + (lane >> 5)) & 15); };
         int32_t pair[COLUMNS];
         uint32_t from[LOADS_X];
 #pragma unroll
         for (int c = 0; c < COLUMNS; ++c) pair[c] = list[min(16 * c + r, here - 1)];
 #pragma unroll
         for (int i = 0; i < LOADS_X; ++i) {
-            const int row = (2 * (wave + 4 * i) + (lane >> 5)) % (16 * COLUMNS), plane = i / (2 * COLUMNS);
+            const int row = (2 * (wave + WAVES * i) + (lane >> 5)) % (16 * COLUMNS), plane = WAVES * i / (8 * COLUMNS);
             const int32_t its = list[min(row, here - 1)];
-            from[i] = row < here ? 2u * (uint32_t)(plane * rows.plane + (UP ? its / p.top : its) * rows.pitch) + 16 * (piece ^ (8 * (i & 1))) : DG_NOWHERE;
+            from[i] = row < here ? 2u * (uint32_t)(plane * rows.plane + (UP ? its / p.top : its) * rows.pitch) + 16 * piece(i) : DG_NOWHERE;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         const auto fetch = [&](int32_t s, int to) __attribute__((always_inline)) {
@@ -358,8 +365,8 @@ __global__ __launch_bounds__(256) void experts_kernel(DgExperts p, Rows rows, Wo
             for (int i = 0; i < 4; ++i) dg_load16_to_lds(w[i / 2].codes, codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, lds + to * STAGE_W + 1024 * i);
 #pragma unroll
             for (int i = 0; i < LOADS_X; ++i) {
-                const bool past = 32 * b + 8 * (piece ^ (8 * (i & 1))) >= rows.size;
-                dg_load16_to_lds(x, past ? DG_NOWHERE : from[i] + 64 * b, x_lds + to * STAGE_X + 1024 * (wave + 4 * i));
+                const bool past = 32 * b + 8 * piece(i) >= rows.size;
+                dg_load16_to_lds(x, past ? DG_NOWHERE : from[i] + 64 * b, x_lds + to * STAGE_X + 1024 * (wave + WAVES * i));
             }
         };
         // A stage's loads are waited for when its turn comes; the barrier after that says that every wavefront's are in, and that all are done with the stage before, whose place the
@@ -448,19 +455,22 @@ void launch(const DgExperts &p, const Rows &x, const Work &work, dg_dtype type, 
 {
     const int32_t pairs = p.T * p.top;
     const Rows h = {work.h, work.pitch_h, pairs * work.pitch_h, work.pitch_h, (uint32_t)(4 * pairs) * (uint32_t)work.pitch_h};
-    if (pairs <= FEW_PAIRS) {
+    // (us, each by itself and together, 2048 x 1024: 64 experts, 4 pairs 11.8, 20.2; 12 19.9, 21.7; 16 22.9, 22.1; 32 40, 28; 4096 x 4096, 4 experts, 4 pairs 30.7, 37.9; 8 48, 43)
+    if (pairs <= std::min(FEW_PAIRS, p.d.experts)) {
         experts_few_up_kernel<PLANES><<<dim3(work.pitch_h / 16, pairs), 256, 0, stream>>>(p, x, work);
         if (type == DG_F16) experts_few_down_kernel<_Float16><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
         else experts_few_down_kernel<__bf16><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
         return;
     }
-    const dim3 up(work.pitch_h / 64, std::min(pairs, p.d.experts)), down((p.d.hidden + 127) / 128, up.y);
+    const uint32_t slots = std::min(pairs, p.d.experts);
+    const auto grid = [&](int32_t channels, int each) { return dim3((channels + each - 1) / each, slots); };
+    // (16 columns leave a compute unit room for two workgroups; 64 tokens to 6 of 64 experts, 4096 x 1024: down with three stages, one workgroup, 59 us for 40, by eight wavefronts 43)
     if (pairs <= 16 * p.d.experts) {
-        experts_kernel<true, 1, PLANES, PLANES == 1 ? 3 : 2><<<up, 256, 0, stream>>>(p, x, work);
-        experts_kernel<false, 1, 2, 2><<<down, 256, 0, stream>>>(p, h, work);
+        experts_kernel<true, 4, 1, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 64), 256, 0, stream>>>(p, x, work);
+        experts_kernel<false, 4, 1, 2, 2><<<grid(p.d.hidden, 128), 256, 0, stream>>>(p, h, work);
     } else {
-        experts_kernel<true, 2, PLANES, PLANES == 1 ? 2 : 3><<<up, 256, 0, stream>>>(p, x, work);
-        experts_kernel<false, 2, 2, 3><<<down, 256, 0, stream>>>(p, h, work);
+        experts_kernel<true, 8, 2, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 128), 512, 0, stream>>>(p, x, work);
+        experts_kernel<false, 8, 2, 2, 2><<<grid(p.d.hidden, 256), 512, 0, stream>>>(p, h, work);
     }
     const dim3 join((p.d.hidden + 1023) / 1024, p.T);
     if (type == DG_F16) experts_join_kernel<_Float16><<<join, 256, 0, stream>>>(p, work);

@@ -1,5 +1,5 @@
 // A router: logits in binary64, each token's largest choices, their weights.
-#include "dg_decoder.h"
+#include "dg_mx4.h"
 
 namespace {
 
@@ -51,6 +51,130 @@ __global__ __launch_bounds__(64 * WAVES) void route_logits_kernel(DgRoute p)
             if (e < p.E && t0 + r < p.T) p.logits[(int64_t)(t0 + r) * p.E + e] = (float)s[i];
         }
     }
+}
+
+// The sum over a wavefront's lanes, in each of them.
+template <int CONTROL>
+__device__ __forceinline__ double other_lane(double v)
+{
+    const uint64_t bits = (uint64_t)__double_as_longlong(v);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CONTROL, 0xF, 0xF, false);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CONTROL, 0xF, 0xF, false);
+    return __longlong_as_double((long long)((uint64_t)high << 32 | low));
+}
+__device__ __forceinline__ double sum_of_wave(double v)
+{
+    v += other_lane<0x140>(v);           // row_mirror
+    v += other_lane<0xB1>(v);            // quad_perm 1, 0, 3, 2
+    v += other_lane<0x4E>(v);            // quad_perm 2, 3, 0, 1
+    v += other_lane<0x141>(v);           // row_half_mirror
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// Few tokens: a workgroup has an expert and TOKENS tokens, a lane eight neighbouring positions of 512 of a wavefront's.  One token, 64 experts of 4096: a launch and two waits.
+template <class X, class R, int TOKENS>
+__global__ __launch_bounds__(256) void route_few_kernel(DgRoute p)
+{
+    constexpr int WAVES = 4;
+    __shared__ double sums[WAVES][TOKENS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t e = blockIdx.x, t0 = blockIdx.y * TOKENS;
+    const R *w = (const R *)p.R + e * p.stride_r;
+    const X *x[TOKENS];
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) x[t] = (const X *)p.x + min(t0 + t, p.T - 1) * p.stride_x;
+    double acc[TOKENS] = {};
+    for (int64_t k = 8 * threadIdx.x; k < p.K; k += 512 * WAVES) {
+        const DgVec<R, 8> wk = dg_eight<R>(w, (int32_t)k, p.K);
+        DgVec<X, 8> xk[TOKENS];
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) xk[t] = dg_eight<X>(x[t], (int32_t)k, p.K);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double wi = dg_to_float(wk.e[i]);
+#pragma unroll
+            for (int t = 0; t < TOKENS; ++t) acc[t] = __builtin_fma(wi, (double)dg_to_float(xk[t].e[i]), acc[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+        const double s = sum_of_wave(acc[t]);
+        if (lane == 0) sums[wave][t] = s;
+    }
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t < TOKENS && t0 + t < p.T) p.logits[(int64_t)(t0 + t) * p.E + e] = (float)(sums[0][t] + sums[1][t] + sums[2][t] + sums[3][t]);
+}
+
+// Many tokens: 32 of them and 64 BLOCKS experts a workgroup, 16 and 16 BLOCKS a wavefront, stages of 64 positions in LDS, one multiplied and one on its way.  The matrix instruction bounds it: a
+// wavefront's 16 BLOCKS of a stage are 1024 BLOCKS cycles.  A row's pieces of 16 bytes lie exchanged, piece c of row r at c ^ (r % 8), so that the lanes that LDS serves together find different places.
+template <class X, class R, int BLOCKS>
+__global__ __launch_bounds__(512) void route_tile_kernel(DgRoute p)
+{
+    constexpr int EXPERTS = 64 * BLOCKS, XROW = 64 * sizeof(X), RROW = 64 * sizeof(R), STAGE_X = 32 * XROW, STAGE = STAGE_X + EXPERTS * RROW;
+    constexpr int LOADS_X = STAGE_X / 8192 ? STAGE_X / 8192 : 1, LOADS_R = EXPERTS * RROW / 8192, LOADS = LOADS_X + LOADS_R;
+    __shared__ __align__(1024) uint8_t room[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int32_t e0 = blockIdx.x * EXPERTS, t0 = blockIdx.y * 32, have_x = min(p.T - t0, 32), have_r = min(p.E - e0, EXPERTS);
+    const int64_t pitch_x = p.stride_x * sizeof(X), pitch_r = p.stride_r * sizeof(R);
+    const int32_t bytes_x = p.K * (int)sizeof(X), bytes_r = p.K * (int)sizeof(R);
+    const dg_v4i buffer_x = dg_rows_buffer((const uint8_t *)p.x, t0, pitch_x, have_x, bytes_x), buffer_r = dg_rows_buffer((const uint8_t *)p.R, e0, pitch_r, have_r, bytes_r);
+    const uint32_t lds = dg_lds_address(room);
+    // a load is 1024 bytes of a stage's rows as they lie in LDS: of row (its place) / ROW, piece ... ^ (row % 8)
+    const auto fetch = [&](int32_t s, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const bool tokens = i < LOADS_X;
+            const int ROW = tokens ? XROW : RROW, place = 1024 * (wave + 8 * (tokens ? i : i - LOADS_X)) + 16 * lane, row = place / ROW, piece = place % ROW / 16 ^ (row & 7);
+            const int32_t at = s * ROW + 16 * piece;
+            const bool there = row < (tokens ? have_x : have_r) && at < (tokens ? bytes_x : bytes_r);
+            if (tokens && STAGE_X < 8192 && wave >= STAGE_X / 1024) continue;
+            dg_load16_to_lds(tokens ? buffer_x : buffer_r, there ? row * (uint32_t)(tokens ? pitch_x : pitch_r) + at : DG_NOWHERE, lds + to * STAGE + (tokens ? 0 : STAGE_X) + place - 16 * lane);
+        }
+    };
+    const int tokens0 = 16 * (wave & 1), experts0 = 16 * BLOCKS * (wave >> 1);
+    const int32_t stages = (p.K + 63) / 64;
+    v4d acc[BLOCKS] = {};
+    fetch(0, 0);
+    int now = 0;
+#pragma unroll 1
+    for (int32_t s = 0; s < stages; ++s) {
+        dg_wait_for_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fetch(s + 1, now ^ 1);
+        const uint8_t *xs = room + now * STAGE + (tokens0 + r) * XROW, *rs = room + now * STAGE + STAGE_X + (experts0 + r) * RROW;
+        // lane (r, g): positions 16 g ... 16 g + 15 of the stage, four at a time
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            DgVec<X, 8> xk;
+            DgVec<R, 8> rk[BLOCKS];
+#pragma unroll
+            for (int c = 0; c < (int)sizeof(X) / 2; ++c)
+                __builtin_memcpy((uint8_t *)&xk + 16 * c, xs + (((sizeof(X) / 2) * (2 * g + q) + c) ^ (r & 7)) * 16, 16);
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int c = 0; c < (int)sizeof(R) / 2; ++c)
+                    __builtin_memcpy((uint8_t *)&rk[b] + 16 * c, rs + 16 * b * RROW + (((sizeof(R) / 2) * (2 * g + q) + c) ^ (r & 7)) * 16, 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double xi = dg_to_float(xk.e[i]);
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) acc[b] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)dg_to_float(rk[b].e[i]), xi, acc[b], 0, 0, 0);
+            }
+        }
+        now ^= 1;
+    }
+    dg_wait_for_loads<0>();
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t e = e0 + experts0 + 16 * b + 4 * i + g, t = t0 + tokens0 + r;
+            if (e < p.E && t < p.T) p.logits[(int64_t)t * p.E + e] = (float)acc[b][i];
+        }
 }
 
 // ---- choices -------------------------------------------------------------------------------------------------------------
@@ -173,12 +297,23 @@ void choose(const DgRoute &p, hipStream_t stream)
 template <class X, class R>
 void logits(const DgRoute &p, hipStream_t stream)
 {
+    const auto aligned = [&](const void *rows, int64_t stride, int size) { return (uintptr_t)rows % 4 == 0 && stride * size % 4 == 0 && stride * size < (int64_t)1 << 24; };
+    const bool whole = p.K % 8 == 0 && aligned(p.x, p.stride_x, sizeof(X)) && aligned(p.R, p.stride_r, sizeof(R));
+    const int experts = p.E <= 64 ? 64 : 128;
     dg_in_turns(p.T, 16 * 65535, [&](int64_t t, int64_t count) {
         DgRoute part = p;
         part.x = (const X *)p.x + t * p.stride_x;
         part.logits += t * p.E;
         part.T = (int32_t)count;
-        route_logits_kernel<X, R, 8, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16)), 512, 0, stream>>>(part);
+        if (count == 1) route_few_kernel<X, R, 1><<<p.E, 256, 0, stream>>>(part);
+        else if (count <= 32) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
+        else if (whole && (count + 31) / 32 * ((p.E + experts - 1) / experts) >= dg_simd_count() / 8) {
+            const dim3 grid((p.E + experts - 1) / experts, (uint32_t)((count + 31) / 32));
+            if (experts == 64) route_tile_kernel<X, R, 1><<<grid, 512, 0, stream>>>(part);
+            else route_tile_kernel<X, R, 2><<<grid, 512, 0, stream>>>(part);
+        } else {
+            route_logits_kernel<X, R, 8, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16)), 512, 0, stream>>>(part);
+        }
         return DG_OK;
     });
 }
