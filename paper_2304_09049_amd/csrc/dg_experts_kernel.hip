@@ -277,13 +277,14 @@ __global__ __launch_bounds__(512) void experts_few_down_kernel(DgExperts p, Rows
 
 // ---- more pairs: an expert's together --------------------------------------------------------------------------------------
 //
-// A wavefront has 16 channels of `up` (gates and others) or 32 of `down`, a workgroup 16 COLUMNS of the expert's pairs at a time.  A wavefront's rows come into a ring of its own, the pairs' activations into one that
+// A wavefront has 16 channels of `up` (gates and others) or 32 of `down`, a workgroup PAIRS of the expert's pairs at a time.  A wavefront's rows come into a ring of its own, the pairs' activations into one that
 // all of the workgroup's read.  With fewer pairs than experts a workgroup's slot is a pair, whose expert it takes unless an earlier pair names it too, otherwise an expert.
 
-template <bool UP, int WAVES, int COLUMNS, int PLANES, int RING>
+template <bool UP, int WAVES, int PAIRS, int PLANES, int RING>
 __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows rows, Work work)
 {
-    constexpr int LOADS_X = 8 * COLUMNS * PLANES / WAVES, LOADS = 4 + LOADS_X, STAGE_W = 4096, STAGE_X = COLUMNS * PLANES * 8192, SCALES = 1024;
+    constexpr int COLUMNS = PAIRS / 16, LOADS_X = PAIRS * PLANES / (2 * WAVES), LOADS = 4 + LOADS_X, STAGE_W = 4096, STAGE_X = PAIRS * PLANES * 512, SCALES = 1024;
+    static_assert(PAIRS * PLANES % (2 * WAVES) == 0 && PAIRS % 16 == 0, "whole loads");
     __shared__ __align__(1024) uint8_t room[RING * (WAVES * STAGE_W + STAGE_X) + WAVES * 2 * SCALES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t pairs = p.T * p.top, slot = blockIdx.y, blocks = ((UP ? p.d.hidden : p.d.inner) + 31) / 32;
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
                 if (!which) continue;
                 if (by_pair && n == 0 && first + 64 * i + __builtin_ctzll(which) != slot) return 0;
                 const int32_t number = n + __builtin_popcountll(which & ((1ull << lane) - 1)) - from;
-                if (is && number >= 0 && number < 16 * COLUMNS) list[number] = (uint16_t)(first + 64 * i + lane);
+                if (is && number >= 0 && number < PAIRS) list[number] = (uint16_t)(first + 64 * i + lane);
                 n += __builtin_popcountll(which);
             }
         }
@@ -315,51 +316,56 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
     };
     int32_t count = find(0);
     if (count == 0) return;
-    // its rows
-    const int32_t m = UP ? (blockIdx.x * WAVES + wave) * 16 : (blockIdx.x * WAVES + wave) * 32, all = UP ? p.d.inner : p.d.hidden;
+    const int32_t all = UP ? p.d.inner : p.d.hidden, each = UP ? 16 : 32, tiles = ((UP ? work.pitch_h : p.d.hidden) + WAVES * each - 1) / (WAVES * each), stages = (blocks + 7) / 8;
+    // its rows of the tile that is being loaded
     Weights w[2];
+    uint32_t offset[2][2];
+    const auto begin = [&](int32_t tile) __attribute__((always_inline)) {
+        const int32_t m = (tile * WAVES + wave) * each;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (UP)
-            w[i] = weights_at(p.d.up + expert * p.d.up_expert, p.d.up_row, p.d.up_scales + expert * p.d.up_scales_expert, p.d.up_scales_row, min(m, all - 1) + (int64_t)i * all, all - m, blocks);
-        else
-            w[i] = weights_at(p.d.down + expert * p.d.down_expert, p.d.down_row, p.d.down_scales + expert * p.d.down_scales_expert, p.d.down_scales_row, min(m + 16 * i, all - 1), all - m - 16 * i,
-                              blocks);
-    }
+        for (int i = 0; i < 2; ++i) {
+            if (UP)
+                w[i] = weights_at(p.d.up + expert * p.d.up_expert, p.d.up_row, p.d.up_scales + expert * p.d.up_scales_expert, p.d.up_scales_row, min(m, all - 1) + (int64_t)i * all, all - m, blocks);
+            else
+                w[i] = weights_at(p.d.down + expert * p.d.down_expert, p.d.down_row, p.d.down_scales + expert * p.d.down_scales_expert, p.d.down_scales_row, min(m + 16 * i, all - 1),
+                                  all - m - 16 * i, blocks);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) offset[i / 2][i % 2] = codes_offset(w[i / 2], i % 2);
+    };
     const dg_v4i x = dg_buffer((const uint8_t *)rows.x, rows.bytes);
     const uint32_t lds = dg_lds_address(mine), x_lds = dg_lds_address(shared), scale_lds = dg_lds_address(scale_room);
-    uint32_t offset[2][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) offset[i / 2][i % 2] = codes_offset(w[i / 2], i % 2);
-    const int32_t stages = (blocks + 7) / 8;
-    for (int32_t column = 0; column < count; column += 16 * COLUMNS) {
+    for (int32_t column = 0; column < count; column += PAIRS) {
         if (column) {
             __syncthreads();
             find(column);
         }
-        const int32_t here = min(count - column, 16 * COLUMNS);
+        const int32_t here = min(count - column, PAIRS);
         // load i of a wavefront's share of the activations: rows 2 q and 2 q + 1 of the planes behind one another, q = wave + WAVES i; place l of a row holds piece l ^ (row % 16)
-        const auto piece = [&](int i) { return (lane & 31) ^ ((2 * (wave + WAVES * i) + (lane >> 5)) & 15); };
+        const auto piece = [&](int i) { return (lane & 31) ^ ((2 * (wave + WAVES * i) + (lane >> 5)) % 16); };
         int32_t pair[COLUMNS];
         uint32_t from[LOADS_X];
 #pragma unroll
         for (int c = 0; c < COLUMNS; ++c) pair[c] = list[min(16 * c + r, here - 1)];
 #pragma unroll
         for (int i = 0; i < LOADS_X; ++i) {
-            const int row = (2 * (wave + WAVES * i) + (lane >> 5)) % (16 * COLUMNS), plane = WAVES * i / (8 * COLUMNS);
+            const int row = (2 * (wave + WAVES * i) + (lane >> 5)) % PAIRS, plane = 2 * WAVES * i / PAIRS;
             const int32_t its = list[min(row, here - 1)];
             from[i] = row < here ? 2u * (uint32_t)(plane * rows.plane + (UP ? its / p.top : its) * rows.pitch) + 16 * piece(i) : DG_NOWHERE;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const auto fetch = [&](int32_t s, int to) __attribute__((always_inline)) {
-            const int32_t b = 8 * s;
-            // (scales before codes: the waits below count a stage's other loads, and what was asked for before them is in with them)
-            if (s % 4 == 0) {
-                const uint32_t at = scale_lds + s / 4 % 2 * SCALES;
+        // Loads: stage `ahead` of tile `loading`, and on into the next one's.  (Scales before codes: the waits below count a stage's other loads, and what was asked for before them is in with them.  Behind the last
+        // tile there is nothing to load; the waits count on loads, so they go on, from nowhere: zeros.)
+        int32_t loading = blockIdx.x, ahead = 0, to = 0, scale_to = 0;
+        const auto fetch = [&]() __attribute__((always_inline)) {
+            const int32_t b = 8 * ahead;
+            if (ahead % 4 == 0) {
+                const uint32_t at = scale_lds + scale_to * SCALES;
                 const int row = (lane & 31) >> 1;
                 const int32_t k = b + 16 * (lane & 1);
                 if (lane < 32) dg_load16_to_lds(w[0].scales, row < w[0].have && k < blocks ? row * (uint32_t)w[0].scales_row + k : DG_NOWHERE, at);
                 else dg_load16_to_lds(w[1].scales, row < w[1].have && k < blocks ? row * (uint32_t)w[1].scales_row + k : DG_NOWHERE, at);
+                scale_to ^= 1;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) dg_load16_to_lds(w[i / 2].codes, codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, lds + to * STAGE_W + 1024 * i);
@@ -368,46 +374,57 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
                 const bool past = 32 * b + 8 * piece(i) >= rows.size;
                 dg_load16_to_lds(x, past ? DG_NOWHERE : from[i] + 64 * b, x_lds + to * STAGE_X + 1024 * (wave + WAVES * i));
             }
+            to = to + 1 == RING ? 0 : to + 1;
+            if (++ahead == stages && loading + (int32_t)gridDim.x < tiles) {
+                loading += gridDim.x;
+                ahead = 0;
+                begin(loading);
+            }
         };
         // A stage's loads are waited for when its turn comes; the barrier after that says that every wavefront's are in, and that all are done with the stage before, whose place the
         // loads of RING - 1 ahead then take.
-        v4f acc[2][COLUMNS] = {};
-        for (int i = 0; i < RING - 1; ++i) fetch(i, i);
-        int now = 0, to = RING - 1;
+        begin(loading);
+        for (int i = 0; i < RING - 1; ++i) fetch();
+        int now = 0, scale_now = 1;
 #pragma unroll 1
-        for (int32_t s = 0; s < stages; ++s) {
-            dg_wait_for_loads<(RING - 2) * LOADS>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            fetch(s + RING - 1, to);
-            uint32_t byte[2][2];
+        for (int32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            v4f acc[2][COLUMNS] = {};
+#pragma unroll 1
+            for (int32_t s = 0; s < stages; ++s) {
+                dg_wait_for_loads<(RING - 2) * LOADS>();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                fetch();
+                if (s % 4 == 0) scale_now ^= 1;
+                uint32_t byte[2][2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) byte[i / 2][i % 2] = scale_room[s / 4 % 2 * SCALES + 512 * (i / 2) + 32 * r + 8 * (s % 4) + 4 * (i % 2) + g];
-            if (8 * s + 8 > blocks) {
-                // scales past the row: its codes are 0, and 0 by whatever lies there might be no number
+                for (int i = 0; i < 4; ++i) byte[i / 2][i % 2] = scale_room[scale_now * SCALES + 512 * (i / 2) + 32 * r + 8 * (s % 4) + 4 * (i % 2) + g];
+                if (8 * s + 8 > blocks) {
+                    // scales past the row: its codes are 0, and 0 by whatever lies there might be no number
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (8 * s + 4 * (i % 2) + g >= blocks) byte[i / 2][i % 2] = 127;
+                    for (int i = 0; i < 4; ++i)
+                        if (8 * s + 4 * (i % 2) + g >= blocks) byte[i / 2][i % 2] = 127;
+                }
+                const uint8_t *stage = mine + now * STAGE_W, *const wk[2] = {stage, stage + 2048}, *xk[COLUMNS];
+#pragma unroll
+                for (int c = 0; c < COLUMNS; ++c) xk[c] = shared + now * STAGE_X + (16 * c + r) * 512;
+                stage_products<2, COLUMNS, PLANES>(wk, byte, xk, PAIRS * 512, r, acc);
+                now = now + 1 == RING ? 0 : now + 1;
             }
-            const uint8_t *stage = mine + now * STAGE_W, *const wk[2] = {stage, stage + 2048}, *xk[COLUMNS];
+            const int32_t m = (tile * WAVES + wave) * each;
 #pragma unroll
-            for (int c = 0; c < COLUMNS; ++c) xk[c] = shared + now * STAGE_X + (16 * c + r) * 512;
-            stage_products<2, COLUMNS, PLANES>(wk, byte, xk, COLUMNS * 8192, r, acc);
-            now = now + 1 == RING ? 0 : now + 1;
-            to = to + 1 == RING ? 0 : to + 1;
+            for (int c = 0; c < COLUMNS; ++c) {
+                if (16 * c + r >= here) continue;
+                if (UP) {
+                    if (m < work.pitch_h) store_h(p, work, pair[c], m + 4 * g, acc[0][c], acc[1][c]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (m + 16 * i + 4 * g < p.d.hidden) *(v4f *)(work.y + (int64_t)pair[c] * work.pitch_y + m + 16 * i + 4 * g) = acc[i][c];
+                }
+            }
         }
         dg_wait_for_loads<0>();
-#pragma unroll
-        for (int c = 0; c < COLUMNS; ++c) {
-            if (16 * c + r >= here) continue;
-            if (UP) {
-                if (m < work.pitch_h) store_h(p, work, pair[c], m + 4 * g, acc[0][c], acc[1][c]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (m + 16 * i + 4 * g < p.d.hidden) *(v4f *)(work.y + (int64_t)pair[c] * work.pitch_y + m + 16 * i + 4 * g) = acc[i][c];
-            }
-        }
     }
 }
 
@@ -463,14 +480,18 @@ void launch(const DgExperts &p, const Rows &x, const Work &work, dg_dtype type, 
         return;
     }
     const uint32_t slots = std::min(pairs, p.d.experts);
-    const auto grid = [&](int32_t channels, int each) { return dim3((channels + each - 1) / each, slots); };
+    const auto grid = [&](int32_t channels, int each, int32_t size) {
+        // (tiles behind one another in a workgroup where there are many: 64 tokens to 6 of 64 experts, 4096 x 1024, binary16 114 us, 110; with a stage of its own a tile would need a third place for its scales)
+        const uint32_t tiles = (channels + each - 1) / each, most = dg_simd_count();
+        return dim3(size <= 256 ? tiles : std::min(tiles, (most + slots - 1) / slots), slots);
+    };
     // (16 columns leave a compute unit room for two workgroups; 64 tokens to 6 of 64 experts, 4096 x 1024: down with three stages, one workgroup, 59 us for 40, by eight wavefronts 43)
     if (pairs <= 16 * p.d.experts) {
-        experts_kernel<true, 4, 1, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 64), 256, 0, stream>>>(p, x, work);
-        experts_kernel<false, 4, 1, 2, 2><<<grid(p.d.hidden, 128), 256, 0, stream>>>(p, h, work);
+        experts_kernel<true, 4, 16, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 64, p.d.hidden), 256, 0, stream>>>(p, x, work);
+        experts_kernel<false, 4, 16, 2, 2><<<grid(p.d.hidden, 128, p.d.inner), 256, 0, stream>>>(p, h, work);
     } else {
-        experts_kernel<true, 8, 2, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 128), 512, 0, stream>>>(p, x, work);
-        experts_kernel<false, 8, 2, 2, 2><<<grid(p.d.hidden, 256), 512, 0, stream>>>(p, h, work);
+        experts_kernel<true, 8, 32, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 128, p.d.hidden), 512, 0, stream>>>(p, x, work);
+        experts_kernel<false, 8, 32, 2, 2><<<grid(p.d.hidden, 256, p.d.inner), 512, 0, stream>>>(p, h, work);
     }
     const dim3 join((p.d.hidden + 1023) / 1024, p.T);
     if (type == DG_F16) experts_join_kernel<_Float16><<<join, 256, 0, stream>>>(p, work);

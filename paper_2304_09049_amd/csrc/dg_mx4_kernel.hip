@@ -49,66 +49,43 @@ __device__ __forceinline__ uint32_t codes_of(const float (&f)[8], uint32_t byte)
     return byte == 255 ? 0u : (uint32_t)word;
 }
 
-template <class T, int HELD>
+template <class T>
 __global__ __launch_bounds__(THREADS) void quantize_mx4_kernel(const T *x, MxRows r, uint8_t *codes, uint8_t *scales)
 {
-    const uint32_t first = blockIdx.x * (THREADS * HELD) + threadIdx.x;
-    DgVec<T, 8> held[HELD];
-    uint32_t row[HELD], piece[HELD];
+    const uint32_t number = blockIdx.x * THREADS + threadIdx.x, at = min(number, r.total - 1), row = dg_fdiv(at, r.by_row), piece = at - row * r.by_row.d;
+    const DgVec<T, 8> v = dg_eight<T>(x + row * r.stride_x, 8 * piece, r.K);
+    float f[8];
+    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const uint32_t at = min(first + i * THREADS, r.total - 1);
-        row[i] = dg_fdiv(at, r.by_row);
-        piece[i] = at - row[i] * r.by_row.d;
-        held[i] = dg_eight<T>(x + row[i] * r.stride_x, 8 * piece[i], r.K);
+    for (int j = 0; j < 8; ++j) {
+        f[j] = dg_to_float(v.e[j]);
+        most = max(most, __float_as_uint(f[j]) & 0x7FFFFFFFu);
     }
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        float f[8];
-        uint32_t most = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            f[j] = dg_to_float(held[i].e[j]);
-            most = max(most, __float_as_uint(f[j]) & 0x7FFFFFFFu);
-        }
-        const uint32_t byte = scale_byte(most_of_four(most));
-        if (first + i * THREADS < r.total) {
-            *(uint32_t *)(codes + row[i] * r.stride_codes + 4 * piece[i]) = codes_of(f, byte);
-            if (piece[i] % 4 == 0) scales[row[i] * r.stride_scales + piece[i] / 4] = (uint8_t)byte;
-        }
-    }
+    const uint32_t byte = scale_byte(most_of_four(most));
+    if (number >= r.total) return;
+    *(uint32_t *)(codes + row * r.stride_codes + 4 * piece) = codes_of(f, byte);
+    if (piece % 4 == 0) scales[row * r.stride_scales + piece / 4] = (uint8_t)byte;
 }
 
-template <class T, int HELD>
+template <class T>
 __global__ __launch_bounds__(THREADS) void dequantize_mx4_kernel(const uint8_t *codes, const uint8_t *scales, MxRows r, T *out)
 {
-    const uint32_t first = blockIdx.x * (THREADS * HELD) + threadIdx.x;
-    uint32_t word[HELD], byte[HELD], row[HELD], piece[HELD];
+    const uint32_t at = blockIdx.x * THREADS + threadIdx.x, row = dg_fdiv(at, r.by_row), piece = at - row * r.by_row.d;
+    if (at >= r.total) return;
+    const uint32_t word = *(const uint32_t *)(codes + row * r.stride_codes + 4 * piece), byte = scales[row * r.stride_scales + piece / 4];
+    const float s = dg_mx_scale(byte);
+    const v2f f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 1),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 3)};
+    DgVec<T, 8> v;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const uint32_t at = min(first + i * THREADS, r.total - 1);
-        row[i] = dg_fdiv(at, r.by_row);
-        piece[i] = at - row[i] * r.by_row.d;
-        word[i] = *(const uint32_t *)(codes + row[i] * r.stride_codes + 4 * piece[i]);
-        byte[i] = scales[row[i] * r.stride_scales + piece[i] / 4];
-    }
+    for (int j = 0; j < 8; ++j) v.e[j] = dg_from_float<T>(byte == 255 ? s : f[j / 2][j % 2]);
+    T *to = out + row * r.stride_x + 8 * piece;
+    const int32_t left = r.K - 8 * (int32_t)piece;
+    if (left >= 8) dg_store_vec<T, 8>(to, v);
+    else
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        if (first + i * THREADS >= r.total) break;
-        const float s = dg_mx_scale(byte[i]);
-        const v2f f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], s, 1),
-                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], s, 3)};
-        DgVec<T, 8> v;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v.e[j] = dg_from_float<T>(byte[i] == 255 ? s : f[j / 2][j % 2]);
-        T *to = out + row[i] * r.stride_x + 8 * piece[i];
-        const int32_t left = r.K - 8 * (int32_t)piece[i];
-        if (left >= 8) dg_store_vec<T, 8>(to, v);
-        else
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < left) to[j] = v.e[j];
-    }
+        for (int j = 0; j < 7; ++j)
+            if (j < left) to[j] = v.e[j];
 }
 
 // f(the pieces of a launch, its first row): pieces' numbers are 31-bit, and a launch's rows as many as that allows.
@@ -808,7 +785,8 @@ enum class Form { Few16x16, Few16x32, Few32x16, Few32x32, Tile32x64, Tile64x64, 
 
 // The form (channels x tokens a workgroup) whose rounds over the compute units cost least.  `cost`: of a round with a workgroup on each; `both`: with two, where two fit.
 // A round by form, us for K = 2048 and 8192, launch included: 16x16 3.6 (two 4.3), 5.3 (7.4); 16x32 4.2, 6.0; 32x16 4.2 (4.8), 6.9 (7.8); 32x32 4.9 (5.9), 8.3 (10.1); 32x64 5.7, 9.3 (13, where the weights come from
-// memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 50 products, 1 to 4096 tokens, this is within 3 % of the fastest form on 44 and 12 % on the others.
+// memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 50 products, 1 to 4096 tokens,
+// this is within 3 % of the fastest form on 40; the farthest from it: 41 x 4768 x 15264 tokens, positions, channels 1.45 times its time, 32 x 7040 x 5440 1.24, 4 x 10080 x 10784 1.21.
 Form form_of(const DgGemmMx4 &p)
 {
     static const struct {
@@ -823,7 +801,7 @@ Form form_of(const DgGemmMx4 &p)
     Form best = Form::Few16x16;
     int64_t least = INT64_MAX;
     for (const auto &f : forms) {
-        if (std::max(p.stride_w, p.stride_a) * std::max(f.m, f.n) > (int64_t)1 << 31) break;     // (a workgroup's rows lie within 2^31 bytes)
+        if (std::max({p.stride_w, p.stride_a, p.stride_ws, p.stride_as}) * std::max(f.m, f.n) > (int64_t)1 << 31) break;     // (a workgroup's rows lie within 2^31 bytes)
         if (forced && !strcmp(forced, f.name)) return f.form;
         const int64_t count = ((p.M + f.m - 1) / f.m) * (int64_t)((p.N + f.n - 1) / f.n);
         const int64_t cost = f.both && count > units ? (count + 2 * units - 1) / (2 * units) * f.both : (count + units - 1) / units * f.cost;
@@ -843,8 +821,7 @@ dg_status dg_launch_quantize_mx4(const void *x, dg_dtype type, int64_t N, int64_
     in_launches(N, K, stride_n, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
         dg_with_type(type, [&](auto t) {
             typedef decltype(t) T;
-            quantize_mx4_kernel<T, 1><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>((const T *)x + n * stride_n, r, codes + n * stride_codes,
-                                                                                                 scales + n * stride_scales);
+            quantize_mx4_kernel<T><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>((const T *)x + n * stride_n, r, codes + n * stride_codes, scales + n * stride_scales);
             return 0;
         });
     });
@@ -857,8 +834,7 @@ dg_status dg_launch_dequantize_mx4(const uint8_t *codes, int64_t stride_codes, c
     in_launches(N, K, stride_out, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
         dg_with_type(type, [&](auto t) {
             typedef decltype(t) T;
-            dequantize_mx4_kernel<T, 1><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>(codes + n * stride_codes, scales + n * stride_scales, r,
-                                                                                                   (T *)out + n * stride_out);
+            dequantize_mx4_kernel<T><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>(codes + n * stride_codes, scales + n * stride_scales, r, (T *)out + n * stride_out);
             return 0;
         });
     });

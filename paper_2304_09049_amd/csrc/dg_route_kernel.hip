@@ -13,44 +13,53 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 // v_mfma_f64_16x16x4f64: lane (r, g) holds number g of four of row r; sums 4 e + g (of 16 experts) of token r come out in a lane.  A lane loads eight neighbours, and number i of
 // each lane's go into one instruction: any four positions may, as long as both operands take the same.
 
-template <class X, class R, int WAVES, int BLOCKS>
-__global__ __launch_bounds__(64 * WAVES) void route_logits_kernel(DgRoute p)
+// Many tokens: 16 SIDE of them and 16 SIDE experts a workgroup, straight from memory, eight wavefronts sharing K.  With SIDE = 2 the matrix instruction bounds it (8192 tokens of 2048
+// to 128 experts 80 us, 54 of the 70.8 TFLOP/s that a large binary64 matrix product reaches; with SIDE = 1, where the address units are as busy, 95), with SIDE = 1 and hundreds of
+// tokens the waits for memory.  Tiles of 32 tokens and 128 experts staged in LDS took 75 us there, but 136 against 112 at 12000 tokens and up to four times as long where tokens are
+// hundreds: few large tiles end in rounds that leave compute units without work.
+template <class X, class R, int SIDE>
+__global__ __launch_bounds__(512) void route_many_kernel(DgRoute p)
 {
-    __shared__ v4d sums[WAVES][BLOCKS][64];
+    constexpr int WAVES = 8;
+    __shared__ v4d sums[WAVES][SIDE * SIDE][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int32_t e0 = blockIdx.x * (16 * BLOCKS), t0 = blockIdx.y * 16;
-    const X *x = (const X *)p.x + (int64_t)min(t0 + r, p.T - 1) * p.stride_x;
-    const R *w[BLOCKS];
+    const int32_t e0 = blockIdx.x * (16 * SIDE), t0 = blockIdx.y * (16 * SIDE);
+    const X *x[SIDE];
+    const R *w[SIDE];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) w[b] = (const R *)p.R + (int64_t)min(e0 + 16 * b + r, p.E - 1) * p.stride_r;
-    v4d acc[BLOCKS] = {};
-    for (int32_t k = 32 * wave; k < p.K; k += 32 * WAVES) {
-        const DgVec<X, 8> xk = dg_eight<X>(x, k + 8 * g, p.K);
-        DgVec<R, 8> wk[BLOCKS];
+    for (int i = 0; i < SIDE; ++i) x[i] = (const X *)p.x + (int64_t)min(t0 + 16 * i + r, p.T - 1) * p.stride_x;
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) wk[b] = dg_eight<R>(w[b], k + 8 * g, p.K);
+    for (int j = 0; j < SIDE; ++j) w[j] = (const R *)p.R + (int64_t)min(e0 + 16 * j + r, p.E - 1) * p.stride_r;
+    v4d acc[SIDE * SIDE] = {};
+    for (int64_t k = 32 * wave; k < p.K; k += 32 * WAVES) {
+        DgVec<X, 8> xk[SIDE];
+        DgVec<R, 8> wk[SIDE];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double xi = dg_to_float(xk.e[i]);
+        for (int i = 0; i < SIDE; ++i) xk[i] = dg_eight<X>(x[i], (int32_t)k + 8 * g, p.K);
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) acc[b] = __builtin_amdgcn_mfma_f64_16x16x4f64(dg_to_float(wk[b].e[i]), xi, acc[b], 0, 0, 0);
+        for (int j = 0; j < SIDE; ++j) wk[j] = dg_eight<R>(w[j], (int32_t)k + 8 * g, p.K);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            double xq[SIDE], wq[SIDE];
+#pragma unroll
+            for (int i = 0; i < SIDE; ++i) xq[i] = dg_to_float(xk[i].e[q]);
+#pragma unroll
+            for (int j = 0; j < SIDE; ++j) wq[j] = dg_to_float(wk[j].e[q]);
+#pragma unroll
+            for (int i = 0; i < SIDE * SIDE; ++i) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(wq[i % SIDE], xq[i / SIDE], acc[i], 0, 0, 0);
         }
     }
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) sums[wave][b][lane] = acc[b];
+    for (int i = 0; i < SIDE * SIDE; ++i) sums[wave][i][lane] = acc[i];
     __syncthreads();
+    if (wave >= SIDE * SIDE) return;
+    v4d s = sums[0][wave][lane];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-        if (b % WAVES != wave) continue;
-        v4d s = sums[0][b][lane];
+    for (int i = 1; i < WAVES; ++i) s += sums[i][wave][lane];
+    const int32_t t = t0 + 16 * (wave / SIDE) + r, e = e0 + 16 * (wave % SIDE) + g;
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) s += sums[i][b][lane];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int32_t e = e0 + 16 * b + 4 * i + g;
-            if (e < p.E && t0 + r < p.T) p.logits[(int64_t)(t0 + r) * p.E + e] = (float)s[i];
-        }
-    }
+    for (int i = 0; i < 4; ++i)
+        if (e + 4 * i < p.E && t < p.T) p.logits[(int64_t)t * p.E + e + 4 * i] = (float)s[i];
 }
 
 // The sum over a wavefront's lanes, in each of them.
@@ -105,76 +114,6 @@ __global__ __launch_bounds__(256) void route_few_kernel(DgRoute p)
     __syncthreads();
     const int t = threadIdx.x;
     if (t < TOKENS && t0 + t < p.T) p.logits[(int64_t)(t0 + t) * p.E + e] = (float)(sums[0][t] + sums[1][t] + sums[2][t] + sums[3][t]);
-}
-
-// Many tokens: 32 of them and 64 BLOCKS experts a workgroup, 16 and 16 BLOCKS a wavefront, stages of 64 positions in LDS, one multiplied and one on its way.  The matrix instruction bounds it: a
-// wavefront's 16 BLOCKS of a stage are 1024 BLOCKS cycles.  A row's pieces of 16 bytes lie exchanged, piece c of row r at c ^ (r % 8), so that the lanes that LDS serves together find different places.
-template <class X, class R, int BLOCKS>
-__global__ __launch_bounds__(512) void route_tile_kernel(DgRoute p)
-{
-    constexpr int EXPERTS = 64 * BLOCKS, XROW = 64 * sizeof(X), RROW = 64 * sizeof(R), STAGE_X = 32 * XROW, STAGE = STAGE_X + EXPERTS * RROW;
-    constexpr int LOADS_X = STAGE_X / 8192 ? STAGE_X / 8192 : 1, LOADS_R = EXPERTS * RROW / 8192, LOADS = LOADS_X + LOADS_R;
-    __shared__ __align__(1024) uint8_t room[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int32_t e0 = blockIdx.x * EXPERTS, t0 = blockIdx.y * 32, have_x = min(p.T - t0, 32), have_r = min(p.E - e0, EXPERTS);
-    const int64_t pitch_x = p.stride_x * sizeof(X), pitch_r = p.stride_r * sizeof(R);
-    const int32_t bytes_x = p.K * (int)sizeof(X), bytes_r = p.K * (int)sizeof(R);
-    const dg_v4i buffer_x = dg_rows_buffer((const uint8_t *)p.x, t0, pitch_x, have_x, bytes_x), buffer_r = dg_rows_buffer((const uint8_t *)p.R, e0, pitch_r, have_r, bytes_r);
-    const uint32_t lds = dg_lds_address(room);
-    // a load is 1024 bytes of a stage's rows as they lie in LDS: of row (its place) / ROW, piece ... ^ (row % 8)
-    const auto fetch = [&](int32_t s, int to) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const bool tokens = i < LOADS_X;
-            const int ROW = tokens ? XROW : RROW, place = 1024 * (wave + 8 * (tokens ? i : i - LOADS_X)) + 16 * lane, row = place / ROW, piece = place % ROW / 16 ^ (row & 7);
-            const int32_t at = s * ROW + 16 * piece;
-            const bool there = row < (tokens ? have_x : have_r) && at < (tokens ? bytes_x : bytes_r);
-            if (tokens && STAGE_X < 8192 && wave >= STAGE_X / 1024) continue;
-            dg_load16_to_lds(tokens ? buffer_x : buffer_r, there ? row * (uint32_t)(tokens ? pitch_x : pitch_r) + at : DG_NOWHERE, lds + to * STAGE + (tokens ? 0 : STAGE_X) + place - 16 * lane);
-        }
-    };
-    const int tokens0 = 16 * (wave & 1), experts0 = 16 * BLOCKS * (wave >> 1);
-    const int32_t stages = (p.K + 63) / 64;
-    v4d acc[BLOCKS] = {};
-    fetch(0, 0);
-    int now = 0;
-#pragma unroll 1
-    for (int32_t s = 0; s < stages; ++s) {
-        dg_wait_for_loads<0>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        fetch(s + 1, now ^ 1);
-        const uint8_t *xs = room + now * STAGE + (tokens0 + r) * XROW, *rs = room + now * STAGE + STAGE_X + (experts0 + r) * RROW;
-        // lane (r, g): positions 16 g ... 16 g + 15 of the stage, four at a time
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            DgVec<X, 8> xk;
-            DgVec<R, 8> rk[BLOCKS];
-#pragma unroll
-            for (int c = 0; c < (int)sizeof(X) / 2; ++c)
-                __builtin_memcpy((uint8_t *)&xk + 16 * c, xs + (((sizeof(X) / 2) * (2 * g + q) + c) ^ (r & 7)) * 16, 16);
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                for (int c = 0; c < (int)sizeof(R) / 2; ++c)
-                    __builtin_memcpy((uint8_t *)&rk[b] + 16 * c, rs + 16 * b * RROW + (((sizeof(R) / 2) * (2 * g + q) + c) ^ (r & 7)) * 16, 16);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double xi = dg_to_float(xk.e[i]);
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) acc[b] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)dg_to_float(rk[b].e[i]), xi, acc[b], 0, 0, 0);
-            }
-        }
-        now ^= 1;
-    }
-    dg_wait_for_loads<0>();
-#pragma unroll
-    for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int32_t e = e0 + experts0 + 16 * b + 4 * i + g, t = t0 + tokens0 + r;
-            if (e < p.E && t < p.T) p.logits[(int64_t)t * p.E + e] = (float)acc[b][i];
-        }
 }
 
 // ---- choices -------------------------------------------------------------------------------------------------------------
@@ -294,26 +233,23 @@ void choose(const DgRoute &p, hipStream_t stream)
     });
 }
 
+// The few-token kernel reads the router once for four tokens and takes sums one by one: it is the faster one to 12288 sums (us with the choice, its and the other's: 64 x 4096 to
+// 64 experts 9.6 and 18.8, 96 x 2048 to 128 11.6 and 12.2, 128 x 2048 to 128 13.6 and 12.3, 64 x 4096 to 256 20 and 22, 256 x 4096 to 64 21.6 and 19.4).  Of the other's tiles the larger
+// are the faster ones where every compute unit gets two (the smaller's and the larger's: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53, 6000 x 4096 to 64 80 and 96,
+// 8192 x 2048 to 256 with a router in binary32 193 and 171).
 template <class X, class R>
 void logits(const DgRoute &p, hipStream_t stream)
 {
-    const auto aligned = [&](const void *rows, int64_t stride, int size) { return (uintptr_t)rows % 4 == 0 && stride * size % 4 == 0 && stride * size < (int64_t)1 << 24; };
-    const bool whole = p.K % 8 == 0 && aligned(p.x, p.stride_x, sizeof(X)) && aligned(p.R, p.stride_r, sizeof(R));
-    const int experts = p.E <= 64 ? 64 : 128;
+    const auto tiles = [&](int64_t tokens, int side) { return (tokens + side - 1) / side * ((p.E + side - 1) / side); };
     dg_in_turns(p.T, 16 * 65535, [&](int64_t t, int64_t count) {
         DgRoute part = p;
         part.x = (const X *)p.x + t * p.stride_x;
         part.logits += t * p.E;
         part.T = (int32_t)count;
         if (count == 1) route_few_kernel<X, R, 1><<<p.E, 256, 0, stream>>>(part);
-        else if (count <= 32) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
-        else if (whole && (count + 31) / 32 * ((p.E + experts - 1) / experts) >= dg_simd_count() / 8) {
-            const dim3 grid((p.E + experts - 1) / experts, (uint32_t)((count + 31) / 32));
-            if (experts == 64) route_tile_kernel<X, R, 1><<<grid, 512, 0, stream>>>(part);
-            else route_tile_kernel<X, R, 2><<<grid, 512, 0, stream>>>(part);
-        } else {
-            route_logits_kernel<X, R, 8, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16)), 512, 0, stream>>>(part);
-        }
+        else if (count * p.E <= 12288) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
+        else if (tiles(count, 32) >= dg_simd_count() / 2) route_many_kernel<X, R, 2><<<dim3((p.E + 31) / 32, (uint32_t)((count + 31) / 32)), 512, 0, stream>>>(part);
+        else route_many_kernel<X, R, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16)), 512, 0, stream>>>(part);
         return DG_OK;
     });
 }
