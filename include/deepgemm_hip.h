@@ -11,7 +11,8 @@
  * lw[4], la[4] are the level tables; LUT[4*w + a] = lw[w] * la[a].
  *
  * The last part is what a quantised decoder layer needs around such products: 8-bit integer products with run-time scales, a
- * paged cache of keys and values in 8 or 4 bits, attention over it.
+ * paged cache of keys and values in 8 or 4 bits, attention over it; then layers in microscaled 4-bit floating point, a router,
+ * and experts whose weights are held in it.
  *
  * Conventions common to every call
  *   - Every function returns a dg_status, never throws, never aborts, never synchronises the
@@ -524,7 +525,7 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
  *             sigmoid(l) / sum over the taken of sigmoid(l) (0 where that is 0)
  * A token with a NaN among its l or choices gets the experts 0 ... top - 1 and weights NaN: whatever is computed from it shows it.
  * x_dev: [T][K] of x_type, rows stride_x elements apart; R_dev: [E][K] of r_type (x_type or DG_F32), stride_r.  ids_dev, weights_dev: contiguous [T][top].
- * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned.  E <= 1024, top <= 64, K < 2^31.
+ * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned.  E <= 1024, top <= 64, K <= 2^24.
  * Errors: DG_ERR_NULL; DG_ERR_SHAPE (T < 0, K, E, top <= 0, top > E, a stride below its row); DG_ERR_RANGE (E, top, K, T * E of 2^31 and more); DG_ERR_UNSUPPORTED; DG_ERR_BUFFER.
  */
 typedef enum { DG_ROUTE_SOFTMAX = 0, DG_ROUTE_SOFTMAX_ALL = 1, DG_ROUTE_SIGMOID = 2 } dg_route_mode;
@@ -548,7 +549,7 @@ typedef struct {
  *     g = gate_e x[t],  u = other_e x[t],  h = g / (1 + exp(-g)) * u,      out[t] = sum_j weights[t][j] * (down_e h)
  * An id that is no expert is skipped (a token of which none is left gives 0); a token may name an expert twice.  x and out are binary16 or bfloat16 and enter exactly; sums are
  * binary32; h is kept to 2^-17 of itself (two bfloat16 numbers); results are rounded once.  A token's results go by its own x, ids and weights only.  Only the weights of experts that are named are
- * read, once for 64 tokens (for few tokens that reading is what a call costs): meant for tokens being decoded; more than a few hundred tokens are worked through in turns.
+ * read, once for 16 or 32 of an expert's tokens (for few tokens that reading is what a call costs): meant for tokens being decoded; more than a few hundred tokens are worked through in turns.
  * x_dev: [T][hidden], rows stride_x elements apart; ids_dev, weights_dev: contiguous [T][top]; out_dev rows stride_out apart.  out_dev must not overlap x_dev.
  * work_dev: dg_experts_mx4_work_bytes(...) bytes, 16-byte aligned.  top <= 64; hidden, inner <= 2^20; experts <= 2^16.
  * Errors: DG_ERR_NULL; DG_ERR_SHAPE (a size <= 0, T < 0, a stride below its row); DG_ERR_RANGE; DG_ERR_UNSUPPORTED (type, reserved); DG_ERR_BUFFER.

@@ -615,6 +615,13 @@ T *vector_here(PyObject *o, at::ScalarType type, int64_t count, const char *name
     return p;
 }
 
+void *work_here(PyObject *o)
+{
+    void *p = device_ptr(o, at::kByte, "work");
+    if (o != Py_None) here(THPVariable_Unpack(o), "work");
+    return p;
+}
+
 // Quantised rows as the binding has them: codes [...][rows][16 * blocks] and scales [...][rows][blocks], uint8; distances in bytes (those that no index takes are of any use to
 // the library's checks only).
 struct Mx4 {
@@ -697,7 +704,7 @@ PyObject *linear_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
         expect((K + 31) / 32 == W.blocks, "x and W must have the same number of columns");
         expect(out.size(0) == N && out.size(1) == W.rows, "out must be [tokens][channels]");
         const float *bias = vector_here<float>(a[3], at::kFloat, W.rows, "bias", true);
-        void *work = device_ptr(a[4], at::kByte, "work");
+        void *work = work_here(a[4]);
         const size_t bytes = bytes_of(a[4]);
         const dg_dtype xt = element_type(x, "x"), type = element_type(out, "out");
         void *s = stream_of(a[6]), *po = out.data_ptr();
@@ -721,7 +728,7 @@ PyObject *route_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t choices = top > 0 && top <= E ? T * top : 0;
         int32_t *ids = vector_here<int32_t>(a[6], at::kInt, choices, "ids");
         float *weights = vector_here<float>(a[7], at::kFloat, choices, "weights");
-        void *work = device_ptr(a[8], at::kByte, "work");
+        void *work = work_here(a[8]);
         const size_t bytes = bytes_of(a[8]);
         void *s = stream_of(a[9]);
         const void *px = x.data_ptr(), *pr = R.data_ptr();
@@ -746,7 +753,7 @@ PyObject *experts_mx4(PyObject *, PyObject *const *a, Py_ssize_t n)
         expect(ids.size(0) == T && ids.is_contiguous(), "ids must be contiguous, [tokens][choices]");
         expect(E <= INT32_MAX && K <= INT32_MAX && F <= INT32_MAX, "too many experts or channels");
         const float *weights = vector_here<float>(a[6], at::kFloat, T * top, "weights");
-        void *work = device_ptr(a[7], at::kByte, "work");
+        void *work = work_here(a[7]);
         const size_t bytes = bytes_of(a[7]);
         void *s = stream_of(a[9]), *po = out.data_ptr();
         const void *px = x.data_ptr();

@@ -143,7 +143,7 @@ dg_status dg_route_tokens(const void *x_dev, dg_dtype x_type, int64_t T, int64_t
     const char *what = "dg_route_tokens";
     if (T < 0 || K <= 0 || E <= 0 || top <= 0 || top > E)
         return dg_fail(DG_ERR_SHAPE, "%s: T=%lld K=%lld, %lld of %lld experts", what, (long long)T, (long long)K, (long long)top, (long long)E);
-    if (E > 1024 || top > 64 || K > MOST_ROWS || T > MOST_ROWS / E)
+    if (E > 1024 || top > 64 || K > MOST_K || T > MOST_ROWS / E)
         return dg_fail(DG_ERR_RANGE, "%s: T=%lld K=%lld, %lld of %lld experts (at most 64 of 1024)", what, (long long)T, (long long)K, (long long)top, (long long)E);
     if (!known_type(x_type) || (r_type != x_type && r_type != DG_F32))
         return dg_fail(DG_ERR_UNSUPPORTED, "%s: element types %d and %d (the router's is the activations' or binary32)", what, (int)x_type, (int)r_type);

@@ -1,5 +1,5 @@
 """A quantised decoder layer out of this library's calls: attention with 8-bit projections over a cache in 8 or 4 bits, and a
-feed-forward part by 2-bit table lookup.
+feed-forward part by 2-bit table lookup, or of experts in microscaled 4-bit floating point.
 
 The layer serves a batch of sequences whose cached keys and values lie in pages of one buffer.  A step takes any number of new
 tokens a sequence -- a prompt, a chunk of one, one decoded token each, mixed -- as the same six calls:
@@ -10,8 +10,14 @@ tokens a sequence -- a prompt, a chunk of one, one decoded token each, mixed -- 
     dg_linear_i8          the attention's output projection
     dg_quantize_pack_activations, dg_gemm_lut   the feed-forward product on 2-bit codes, to float32 with a scale per channel
 
+``ExpertsLayer`` has another feed-forward part, of weights in blocks of 32 with a power of two each (dg_quantize_mx4):
+
+    dg_route_tokens       which experts each token goes to, with what weights
+    dg_experts_mx4        those experts' gated feed-forward, added up
+    dg_linear_mx4         twice: the gated feed-forward that every token passes
+
 ``python -m paper_2304_09049_amd.decoder_layer`` runs a batch through prompts in chunks and some decoded tokens, and prints how far
-the attention part is from float32 with nothing quantised, and what a step of decoded tokens takes with its host work.
+the attention part is from float32 with nothing quantised (with experts, the feed-forward part too), and what a step of decoded tokens takes with its host work.
 """
 from __future__ import annotations
 
@@ -58,13 +64,16 @@ class DecoderLayer:
     LEVELS_W, LEVELS_A = (-2, -1, 0, 1), (-2, -1, 0, 1)
 
     def __init__(self, w_qkv, w_out, w_ff, heads: int, kv_heads: int, dim: int, ff_step: float = 1.0):
-        self.heads, self.kv_heads, self.dim, self.ff_step = heads, kv_heads, dim, ff_step
-        self.qkv, self.qkv_scale = dg.dg_quantize_tokens(w_qkv)
-        self.out, self.out_scale = dg.dg_quantize_tokens(w_out)
-        self.ff_shape = w_ff.shape
+        self.take_attention(w_qkv, w_out, heads, kv_heads, dim)
+        self.ff_step, self.ff_shape = ff_step, w_ff.shape
         codes, self.ff_scale = self.two_bits(w_ff)
         self.ff = dg.dg_pack_weights(codes, *self.ff_shape)
         self.lut = dg.dg_build_lut(self.LEVELS_W, self.LEVELS_A)
+
+    def take_attention(self, w_qkv, w_out, heads, kv_heads, dim):
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
+        self.qkv, self.qkv_scale = dg.dg_quantize_tokens(w_qkv)
+        self.out, self.out_scale = dg.dg_quantize_tokens(w_out)
 
     @staticmethod
     def two_bits(w):
@@ -98,6 +107,39 @@ class DecoderLayer:
         return y.to(h.dtype)
 
 
+class ExpertsLayer(DecoderLayer):
+    """A layer whose feed-forward part is ``top`` of some experts a token and one that every token passes.  router: [experts][hidden] (kept in float32);
+    up: [experts][2 * inner][hidden], the gates first; down: [experts][hidden][inner]; shared_up, shared_down: the same without experts, of an inner size of
+    their own.  bias: [experts] float32 added to what experts are chosen by."""
+
+    def __init__(self, w_qkv, w_out, router, up, down, shared_up, shared_down, heads: int, kv_heads: int, dim: int, top: int, mode="softmax", bias=None):
+        experts, hidden = router.shape
+        inner = down.shape[2]
+        if up.shape != (experts, 2 * inner, hidden) or down.shape != (experts, hidden, inner) or not 0 < top <= experts:
+            raise ValueError(f"{top} of {experts} experts on {hidden} with up {list(up.shape)} and down {list(down.shape)}")
+        if shared_up.shape != (2 * shared_down.shape[1], hidden) or shared_down.shape[0] != hidden:
+            raise ValueError(f"shared up {list(shared_up.shape)} and down {list(shared_down.shape)} on {hidden}")
+        self.take_attention(w_qkv, w_out, heads, kv_heads, dim)
+        self.router, self.top, self.mode, self.bias = router.float(), top, mode, bias
+        self.experts = [t.unflatten(0, w.shape[:2]) for w in (up, down) for t in dg.dg_quantize_mx4(w.flatten(0, 1))]
+        self.shared_up, self.shared_down = dg.dg_quantize_mx4(shared_up), dg.dg_quantize_mx4(shared_down)
+
+    def feed_forward(self, h):
+        ids, weights = dg.dg_route_tokens(h, self.router, self.top, self.mode, self.bias)
+        chosen = dg.dg_experts_mx4(*self.experts, h, ids, weights)
+        gate, other = dg.dg_linear_mx4(*self.shared_up, h).chunk(2, 1)
+        return chosen + dg.dg_linear_mx4(*self.shared_down, torch.nn.functional.silu(gate) * other)
+
+
+def plain_experts_part(h, router, up, down, shared_up, shared_down, top):
+    """What ``ExpertsLayer.feed_forward`` approximates (mode "softmax", no bias), in float32, nothing quantised: every expert on all tokens."""
+    h, weights = h.float(), torch.zeros(h.shape[0], router.shape[0], device=h.device)
+    most, ids = (h @ router.t()).topk(top)
+    weights.scatter_(1, ids, torch.softmax(most, 1))
+    gated = lambda x, up, down: (torch.nn.functional.silu(x @ up[:down.shape[1]].t()) * (x @ up[down.shape[1]:].t())) @ down.t()  # noqa: E731
+    return gated(h, shared_up, shared_down) + sum(weights[:, e, None] * gated(h, up[e], down[e]) for e in range(router.shape[0]))
+
+
 def plain_attention_part(x, w_qkv, w_out, heads, kv_heads, dim):
     """What ``DecoderLayer.attend`` approximates: one sequence from its first token on, in float32, nothing quantised."""
     n = x.shape[0]
@@ -114,8 +156,14 @@ def main():
     hidden, heads, kv_heads, dim, prompt, decoded = 1024, 16, 4, 64, 300, 20
     w_qkv, w_out, w_ff = (torch.randn(n, m, device=device, generator=gen) * m ** -0.5
                           for n, m in (((heads + 2 * kv_heads) * dim, hidden), (hidden, heads * dim), (hidden, hidden)))
-    for bits in (8, 4):
-        layer = DecoderLayer(w_qkv, w_out, w_ff, heads, kv_heads, dim)
+    experts, inner, top = 16, 512, 4
+    parts = [torch.randn(*size, device=device, generator=gen) * size[-1] ** -0.5
+             for size in ((experts, hidden), (experts, 2 * inner, hidden), (experts, hidden, inner), (2 * inner, hidden), (hidden, inner))]
+    for kind, bits in (("tables", 8), ("tables", 4), ("experts", 8)):
+        if kind == "tables":
+            layer = DecoderLayer(w_qkv, w_out, w_ff, heads, kv_heads, dim)
+        else:
+            layer = ExpertsLayer(w_qkv, w_out, *parts, heads, kv_heads, dim, top)
         sequences = PagedSequences(dg.cache_desc(64, 16, kv_heads, dim, bits), 3, device)
         x = torch.randn(3, prompt + decoded, hidden, device=device, generator=gen).bfloat16()
         done, at, took = [[], [], []], [0, 0, 0], []
@@ -136,7 +184,12 @@ def main():
             want = plain_attention_part(x[b, :at[b]], w_qkv, w_out, heads, kv_heads, dim) - x[b, :at[b]].float()
             got = torch.cat(done[b]).float() - x[b, :at[b]].float()
             off = max(off, ((got - want).norm() / want.norm()).item())
-        print(f"{bits}-bit cache: sequences of {at} tokens, attention off by {off:.3f} of its norm, "
+        told = ""
+        if kind == "experts":
+            h = torch.cat([t for parts_done in done for t in parts_done])
+            want = plain_experts_part(h, *parts, top)
+            told = f"feed-forward by {((layer.feed_forward(h).float() - want).norm() / want.norm()).item():.3f}, "
+        print(f"{kind}, {bits}-bit cache: sequences of {at} tokens, attention off by {off:.3f} of its norm, {told}"
               f"a step of decoded tokens {sorted(took)[len(took) // 2] * 1e6:.0f} us")
 
 

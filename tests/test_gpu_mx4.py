@@ -112,6 +112,22 @@ def test_product_by_every_tile(N, M, K, apart, tile, monkeypatch):
     ref.assert_within(dg.dg_gemm_mx4(W, Ws, A, As, bias=bias.to(DEV)), want, off)
 
 
+def test_rows_of_scales_far_apart(monkeypatch):
+    """A workgroup's offsets have 32 bits: rows 2^26 bytes apart are taken by tiles of 32 rows at most, whichever is asked for."""
+    if torch.cuda.mem_get_info()[0] < 6 << 30:
+        pytest.skip("6 GiB")
+    gen = torch.Generator().manual_seed(11)
+    W, Ws, w = held(gen, 64, 256)
+    A, As, a = held(gen, 64, 256)
+    far = torch.as_strided(torch.empty(63 * 2 ** 26 + 8, dtype=torch.uint8, device=DEV), (64, 8), (2 ** 26, 1))
+    far.copy_(Ws)
+    want, off = ref.product(a, w, None, torch.float32)
+    for tile in ("64x64", "128x128", "256x256"):
+        monkeypatch.setenv("DG_GEMM_MX4_TILE", tile)
+        ref.assert_within(dg.dg_gemm_mx4(W, far, A, As), want, off)
+        ref.assert_within(dg.dg_gemm_mx4(A, As, W, far), want.t(), off.t())
+
+
 @pytest.mark.parametrize("N", [1, 20, 200])
 def test_a_block_that_is_none_reaches_its_row_only(N):
     gen = torch.Generator().manual_seed(3)
