@@ -618,7 +618,7 @@ T *vector_here(PyObject *o, at::ScalarType type, int64_t count, const char *name
 void *work_here(PyObject *o)
 {
     void *p = device_ptr(o, at::kByte, "work");
-    if (o != Py_None) here(THPVariable_Unpack(o), "work");
+    if (THPVariable_Check(o)) here(THPVariable_Unpack(o), "work");
     return p;
 }
 
