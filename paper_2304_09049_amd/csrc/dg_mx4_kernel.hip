@@ -21,7 +21,7 @@ constexpr int THREADS = 256;
 struct MxRows {
     int64_t stride_x, stride_codes, stride_scales;       // elements, bytes, bytes
     int32_t K;
-    uint32_t total;                                      // lanes' pieces of 8 elements
+    uint32_t total;                                      // lanes' pieces
     DgFastDiv by_row;                                    // a row's pieces
 };
 
@@ -67,32 +67,36 @@ __global__ __launch_bounds__(THREADS) void quantize_mx4_kernel(const T *x, MxRow
     if (piece % 4 == 0) scales[row * r.stride_scales + piece / 4] = (uint8_t)byte;
 }
 
+// A lane has 16 bytes of the output, so that a store instruction writes whole lines, and they bypass the caches: kept there they cost twice the time (16384 x 8192 to bfloat16 92 us, 48,
+// and with a copy of the output behind it 205 and 167).
 template <class T>
 __global__ __launch_bounds__(THREADS) void dequantize_mx4_kernel(const uint8_t *codes, const uint8_t *scales, MxRows r, T *out)
 {
+    constexpr int COUNT = 16 / sizeof(T);
     const uint32_t at = blockIdx.x * THREADS + threadIdx.x, row = dg_fdiv(at, r.by_row), piece = at - row * r.by_row.d;
     if (at >= r.total) return;
-    const uint32_t word = *(const uint32_t *)(codes + row * r.stride_codes + 4 * piece), byte = scales[row * r.stride_scales + piece / 4];
+    const uint8_t *from = codes + row * r.stride_codes + COUNT / 2 * piece;
+    const uint32_t word = COUNT == 8 ? *(const uint32_t *)from : *(const uint16_t *)from, byte = scales[row * r.stride_scales + piece / (32 / COUNT)];
     const float s = dg_mx_scale(byte);
     const v2f f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 1),
                       __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 3)};
-    DgVec<T, 8> v;
+    DgVec<T, COUNT> v;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v.e[j] = dg_from_float<T>(byte == 255 ? s : f[j / 2][j % 2]);
-    T *to = out + row * r.stride_x + 8 * piece;
-    const int32_t left = r.K - 8 * (int32_t)piece;
-    if (left >= 8) dg_store_vec<T, 8>(to, v);
+    for (int j = 0; j < COUNT; ++j) v.e[j] = dg_from_float<T>(byte == 255 ? s : f[j / 2][j % 2]);
+    T *to = out + row * r.stride_x + COUNT * piece;
+    const int32_t left = r.K - COUNT * (int32_t)piece;
+    if (left >= COUNT) dg_store_past(to, v);
     else
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
+        for (int j = 0; j < COUNT - 1; ++j)
             if (j < left) to[j] = v.e[j];
 }
 
-// f(the pieces of a launch, its first row): pieces' numbers are 31-bit, and a launch's rows as many as that allows.
+// f(the pieces of `per` elements of a launch, its first row): pieces' numbers are 31-bit, and a launch's rows as many as that allows.
 template <class F>
-void in_launches(int64_t N, int64_t K, int64_t stride_x, int64_t stride_codes, int64_t stride_scales, F f)
+void in_launches(int64_t N, int64_t K, int per, int64_t stride_x, int64_t stride_codes, int64_t stride_scales, F f)
 {
-    const int64_t pieces = (K + 31) / 32 * 4;
+    const int64_t pieces = (K + 31) / 32 * (32 / per);
     dg_in_turns(N, std::max<int64_t>(1, ((int64_t)1 << 30) / pieces), [&](int64_t n, int64_t rows) {
         const MxRows r = {stride_x, stride_codes, stride_scales, (int32_t)K, (uint32_t)(rows * pieces), dg_make_div((uint32_t)pieces)};
         f(r, n);
@@ -514,7 +518,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
             DgVec<T, 4> y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) y.e[e] = dg_from_float<T>(p.bias ? sum[e] + bias[e] : sum[e]);
-            if (have >= 4) dg_store_vec<T, 4>(out, y);
+            if (have >= 4) dg_store_past(out, y);
             else
 #pragma unroll
                 for (int e = 0; e < 3; ++e)
@@ -739,7 +743,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_mx4_stream_kernel(TileArgs 
                         const int32_t n = n0 + 32 * (TN * wn + j) + 16 * h + row, channel = m + COUNT * (lane & 7);
                         T *out = (T *)p.out + (int64_t)n * p.stride_out + channel;
                         if (n < p.N && channel + COUNT <= p.M) {
-                            dg_store_vec<T, COUNT>(out, y);
+                            dg_store_past(out, y);
                         } else if (n < p.N) {
 #pragma unroll
                             for (int e = 0; e < COUNT - 1; ++e)
@@ -818,7 +822,7 @@ Form form_of(const DgGemmMx4 &p)
 dg_status dg_launch_quantize_mx4(const void *x, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, uint8_t *codes, int64_t stride_codes,
                                  uint8_t *scales, int64_t stride_scales, hipStream_t stream)
 {
-    in_launches(N, K, stride_n, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
+    in_launches(N, K, 8, stride_n, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
         dg_with_type(type, [&](auto t) {
             typedef decltype(t) T;
             quantize_mx4_kernel<T><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>((const T *)x + n * stride_n, r, codes + n * stride_codes, scales + n * stride_scales);
@@ -831,7 +835,7 @@ dg_status dg_launch_quantize_mx4(const void *x, dg_dtype type, int64_t N, int64_
 dg_status dg_launch_dequantize_mx4(const uint8_t *codes, int64_t stride_codes, const uint8_t *scales, int64_t stride_scales, int64_t N, int64_t K,
                                    void *out, dg_dtype type, int64_t stride_out, hipStream_t stream)
 {
-    in_launches(N, K, stride_out, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
+    in_launches(N, K, 16 / (int)dg_type_size(type), stride_out, stride_codes, stride_scales, [&](const MxRows &r, int64_t n) {
         dg_with_type(type, [&](auto t) {
             typedef decltype(t) T;
             dequantize_mx4_kernel<T><<<(r.total + THREADS - 1) / THREADS, THREADS, 0, stream>>>(codes + n * stride_codes, scales + n * stride_scales, r, (T *)out + n * stride_out);
