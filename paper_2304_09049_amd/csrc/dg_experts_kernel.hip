@@ -89,6 +89,15 @@ __device__ __forceinline__ bool codes_past(int i, int32_t b, int32_t blocks)
     return b + ((lane & 7) ^ ((row >> 1) & 7)) >= blocks;
 }
 
+// ONCE: codes that nothing of this call reads again are not kept in the caches (us, kept and not: 64 tokens to 6 of 64 experts, 4096 x 1024, 100 and 92; one to 4 of 64, 2048 x 1024, 11.7 and
+// 11.0; but 256 to 2 of 8, 4096 x 4096, where they are read again for the next pairs, 184 and 188).
+template <bool ONCE>
+__device__ __forceinline__ void load_codes(const Weights &w, uint32_t offset, uint32_t lds)
+{
+    if (ONCE) dg_load16_once_to_lds(w.codes, offset, lds);
+    else dg_load16_to_lds(w.codes, offset, lds);
+}
+
 // The stage's products for a lane's row blocks and columns: `w` where the 16 rows' codes lie, their scales' bytes, `x` where its column's activations lie (element 0; planes PLANE bytes apart).
 template <int BLOCKS, int COLUMNS, int PLANES>
 __device__ __forceinline__ void stage_products(const uint8_t *const (&w)[BLOCKS], const uint32_t (&byte)[BLOCKS][2], const uint8_t *const (&x)[COLUMNS], int plane, int twist, v4f (&acc)[BLOCKS][COLUMNS])
@@ -140,7 +149,7 @@ __global__ __launch_bounds__(256) void experts_rows_kernel(DgExperts p, Work wor
 // up: a workgroup has 16 channels (their gates' rows and the others') of a pair; four wavefronts share K in chunks of 512 positions and work alone, each with a ring of stages, until their sums meet.
 // down: a workgroup has 16 channels of every token; eight wavefronts take pair after pair, and the pairs' results meet in LDS, so that the choices are added up here, in their order.
 
-template <int PLANES>
+template <int PLANES, bool ONCE>
 __global__ __launch_bounds__(256) void experts_few_up_kernel(DgExperts p, Rows rows, Work work)
 {
     constexpr int WAVES = 4, RING = 3, LOADS = 5, STAGE = LOADS * 1024, SCALES = 512, MINE = RING * STAGE + 2 * SCALES;
@@ -173,7 +182,7 @@ __global__ __launch_bounds__(256) void experts_few_up_kernel(DgExperts p, Rows r
         }
         const uint32_t to = lds + s % RING * STAGE;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dg_load16_to_lds(w[i / 2].codes, codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, to + 1024 * i);
+        for (int i = 0; i < 4; ++i) load_codes<ONCE>(w[i / 2], codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, to + 1024 * i);
         dg_load16_to_lds(x, (PLANES == 2 || lane < 32) && 32 * b + 8 * (lane & 31) < rows.size ? x_offset + 64 * b : DG_NOWHERE, to + 4096);
     };
     const int32_t chunks = (blocks + 15) / 16, stages = chunks > wave ? (chunks - wave + WAVES - 1) / WAVES * 2 : 0;
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(256) void experts_few_up_kernel(DgExperts p, Rows r
     }
 }
 
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(512) void experts_few_down_kernel(DgExperts p, Rows rows)
 {
     constexpr int WAVES = 8, RING = 4, LOADS = 3, STAGE = LOADS * 1024, SCALES = 512, MINE = RING * STAGE + 2 * SCALES;
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(512) void experts_few_down_kernel(DgExperts p, Rows
             }
             const uint32_t to = lds + s % RING * STAGE;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) dg_load16_to_lds(w.codes, codes_past(i, b, blocks) ? DG_NOWHERE : offset[i] + 16 * b, to + 1024 * i);
+            for (int i = 0; i < 2; ++i) load_codes<ONCE>(w, codes_past(i, b, blocks) ? DG_NOWHERE : offset[i] + 16 * b, to + 1024 * i);
             dg_load16_to_lds(h, 32 * b + 8 * (lane & 31) < rows.size ? h_offset + 64 * b : DG_NOWHERE, to + 2048);
         };
         v4f acc[1][1] = {};
@@ -368,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
                 scale_to ^= 1;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dg_load16_to_lds(w[i / 2].codes, codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, lds + to * STAGE_W + 1024 * i);
+            for (int i = 0; i < 4; ++i) load_codes<PAIRS == 16>(w[i / 2], codes_past(i % 2, b, blocks) ? DG_NOWHERE : offset[i / 2][i % 2] + 16 * b, lds + to * STAGE_W + 1024 * i);
 #pragma unroll
             for (int i = 0; i < LOADS_X; ++i) {
                 const bool past = 32 * b + 8 * piece(i) >= rows.size;
@@ -474,9 +483,14 @@ void launch(const DgExperts &p, const Rows &x, const Work &work, dg_dtype type, 
     const Rows h = {work.h, work.pitch_h, pairs * work.pitch_h, work.pitch_h, (uint32_t)(4 * pairs) * (uint32_t)work.pitch_h};
     // (us, each by itself and together, 2048 x 1024: 64 experts, 4 pairs 11.8, 20.2; 12 19.9, 21.7; 16 22.9, 22.1; 32 40, 28; 4096 x 4096, 4 experts, 4 pairs 30.7, 37.9; 8 48, 43)
     if (pairs <= std::min(FEW_PAIRS, p.d.experts)) {
-        experts_few_up_kernel<PLANES><<<dim3(work.pitch_h / 16, pairs), 256, 0, stream>>>(p, x, work);
-        if (type == DG_F16) experts_few_down_kernel<_Float16><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
-        else experts_few_down_kernel<__bf16><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
+        const auto both = [&](auto once) {                           // (a token's choices are different experts as a rule, several tokens' may be the same)
+            constexpr bool ONCE = decltype(once)::value;
+            experts_few_up_kernel<PLANES, ONCE><<<dim3(work.pitch_h / 16, pairs), 256, 0, stream>>>(p, x, work);
+            if (type == DG_F16) experts_few_down_kernel<_Float16, ONCE><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
+            else experts_few_down_kernel<__bf16, ONCE><<<(p.d.hidden + 15) / 16, 512, 0, stream>>>(p, h);
+        };
+        if (p.T == 1) both(std::true_type());
+        else both(std::false_type());
         return;
     }
     const uint32_t slots = std::min(pairs, p.d.experts);
