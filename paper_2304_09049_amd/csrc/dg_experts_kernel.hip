@@ -499,8 +499,9 @@ void launch(const DgExperts &p, const Rows &x, const Work &work, dg_dtype type, 
         const uint32_t tiles = (channels + each - 1) / each, most = dg_simd_count();
         return dim3(size <= 256 ? tiles : std::min(tiles, (most + slots - 1) / slots), slots);
     };
+    // (us, 16 and 32 pairs at a time: 64 tokens to 6 of 64 experts, 4096 x 1024, 92 and 105; 128 tokens 144, 131; 64 to 2 of 8, 4096 x 4096, 91, 76: what an expert has of a batch varies, and a pass behind the first costs as much)
     // (16 columns leave a compute unit room for two workgroups; 64 tokens to 6 of 64 experts, 4096 x 1024: down with three stages, one workgroup, 59 us for 40, by eight wavefronts 43)
-    if (pairs <= 16 * p.d.experts) {
+    if (pairs <= 8 * p.d.experts) {
         experts_kernel<true, 4, 16, PLANES, PLANES == 1 ? 3 : 2><<<grid(work.pitch_h, 64, p.d.hidden), 256, 0, stream>>>(p, x, work);
         experts_kernel<false, 4, 16, 2, 2><<<grid(p.d.hidden, 128, p.d.inner), 256, 0, stream>>>(p, h, work);
     } else {
