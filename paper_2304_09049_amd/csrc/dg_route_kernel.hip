@@ -13,14 +13,14 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 // v_mfma_f64_16x16x4f64: lane (r, g) holds number g of four of row r; sums 4 e + g (of 16 experts) of token r come out in a lane.  A lane loads eight neighbours, and number i of
 // each lane's go into one instruction: any four positions may, as long as both operands take the same.
 
-// Many tokens: 16 SIDE of them and 16 SIDE experts a workgroup, straight from memory, eight wavefronts sharing K.  With SIDE = 2 the matrix instruction bounds it (8192 tokens of 2048
-// to 128 experts 80 us, 54 of the 70.8 TFLOP/s that a large binary64 matrix product reaches; with SIDE = 1, where the address units are as busy, 95), with SIDE = 1 and hundreds of
-// tokens the waits for memory.  Tiles of 32 tokens and 128 experts staged in LDS took 75 us there, but 136 against 112 at 12000 tokens and up to four times as long where tokens are
-// hundreds: few large tiles end in rounds that leave compute units without work.
+// Many tokens: 16 SIDE of them and 16 SIDE experts a workgroup, straight from memory, eight wavefronts sharing K, a step's loads under way while the one before is multiplied (2048 tokens
+// of 4096 to 64 experts 34.7 -> 29.3 us with the choice).  With SIDE = 2 the matrix instruction bounds it, and what the address units take for loads of 16 rows (8192 tokens of 2048 to 128
+// experts 78 us, 55 of the 70.8 TFLOP/s that a large binary64 matrix product reaches; with SIDE = 1 95); with SIDE = 1 and hundreds of tokens the waits for memory.  Tiles of 32 tokens and
+// 128 experts staged in LDS took 75 us there, but 136 against 98 at 12000 tokens and up to four times as long where tokens are hundreds: few large tiles end in rounds that leave compute units without work.
 template <class X, class R, int SIDE>
-__global__ __launch_bounds__(512) void route_many_kernel(DgRoute p)
+__global__ __launch_bounds__(512, 4) void route_many_kernel(DgRoute p)
 {
-    constexpr int WAVES = 8;
+    constexpr int WAVES = 8, COUNT = SIDE == 2 && sizeof(R) == 4 ? 4 : 8, EACH = 4 * COUNT;       // (a lane's neighbouring positions: with eight, two stages of binary32 rows do not fit into the registers)
     __shared__ v4d sums[WAVES][SIDE * SIDE][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t e0 = blockIdx.x * (16 * SIDE), t0 = blockIdx.y * (16 * SIDE);
@@ -31,20 +31,50 @@ __global__ __launch_bounds__(512) void route_many_kernel(DgRoute p)
 #pragma unroll
     for (int j = 0; j < SIDE; ++j) w[j] = (const R *)p.R + (int64_t)min(e0 + 16 * j + r, p.E - 1) * p.stride_r;
     v4d acc[SIDE * SIDE] = {};
-    for (int64_t k = 32 * wave; k < p.K; k += 32 * WAVES) {
-        DgVec<X, 8> xk[SIDE];
-        DgVec<R, 8> wk[SIDE];
+    const auto load = [&](DgVec<X, COUNT> (&xk)[SIDE], DgVec<R, COUNT> (&wk)[SIDE], int32_t k) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < SIDE; ++i) xk[i] = dg_eight<X>(x[i], (int32_t)k + 8 * g, p.K);
+        for (int i = 0; i < SIDE; ++i) xk[i] = dg_load_vec<X, COUNT>(x[i] + k);
 #pragma unroll
-        for (int j = 0; j < SIDE; ++j) wk[j] = dg_eight<R>(w[j], (int32_t)k + 8 * g, p.K);
+        for (int j = 0; j < SIDE; ++j) wk[j] = dg_load_vec<R, COUNT>(w[j] + k);
+    };
+    const auto add = [&](const DgVec<X, COUNT> (&xk)[SIDE], const DgVec<R, COUNT> (&wk)[SIDE]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
+        for (int q = 0; q < COUNT; ++q) {
             double xq[SIDE], wq[SIDE];
 #pragma unroll
             for (int i = 0; i < SIDE; ++i) xq[i] = dg_to_float(xk[i].e[q]);
 #pragma unroll
             for (int j = 0; j < SIDE; ++j) wq[j] = dg_to_float(wk[j].e[q]);
+#pragma unroll
+            for (int i = 0; i < SIDE * SIDE; ++i) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(wq[i % SIDE], xq[i / SIDE], acc[i], 0, 0, 0);
+        }
+    };
+    // (whole steps are loaded one ahead)
+    constexpr int STEP = EACH * WAVES;
+    DgVec<X, COUNT> xk[2][SIDE];
+    DgVec<R, COUNT> wk[2][SIDE];
+    int32_t k = EACH * wave;
+    if (k + EACH <= p.K) load(xk[0], wk[0], k + COUNT * g);
+    while (k + EACH <= p.K) {
+        if (k + STEP + EACH <= p.K) load(xk[1], wk[1], k + STEP + COUNT * g);
+        __builtin_amdgcn_sched_barrier(0);
+        add(xk[0], wk[0]);
+        k += STEP;
+        if (k + EACH > p.K) break;
+        if (k + STEP + EACH <= p.K) load(xk[0], wk[0], k + STEP + COUNT * g);
+        __builtin_amdgcn_sched_barrier(0);
+        add(xk[1], wk[1]);
+        k += STEP;
+    }
+    if (k < p.K) {                                                   // (one by one: unrolled it would take registers that the loop needs)
+#pragma unroll 1
+        for (int q = 0; q < COUNT; ++q) {
+            const int32_t at = k + COUNT * g + q;
+            double xq[SIDE], wq[SIDE];
+#pragma unroll
+            for (int i = 0; i < SIDE; ++i) xq[i] = at < p.K ? dg_to_float(x[i][at]) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < SIDE; ++j) wq[j] = at < p.K ? dg_to_float(w[j][at]) : 0.0f;
 #pragma unroll
             for (int i = 0; i < SIDE * SIDE; ++i) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(wq[i % SIDE], xq[i / SIDE], acc[i], 0, 0, 0);
         }
@@ -235,8 +265,8 @@ void choose(const DgRoute &p, hipStream_t stream)
 
 // The few-token kernel reads the router once for four tokens and takes sums one by one: it is the faster one to 12288 sums (us with the choice, its and the other's: 64 x 4096 to
 // 64 experts 9.6 and 18.8, 96 x 2048 to 128 11.6 and 12.2, 128 x 2048 to 128 13.6 and 12.3, 64 x 4096 to 256 20 and 22, 256 x 4096 to 64 21.6 and 19.4).  Of the other's tiles the larger
-// are the faster ones where every compute unit gets two (the smaller's and the larger's: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53, 6000 x 4096 to 64 80 and 96,
-// 8192 x 2048 to 256 with a router in binary32 193 and 171).
+// are the faster ones where every compute unit gets two (the smaller's and the larger's, before loads ran ahead: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53, 6000 x 4096 to 64 80
+// and 96, 8192 x 2048 to 256 with a router in binary32 193 and 171).
 template <class X, class R>
 void logits(const DgRoute &p, hipStream_t stream)
 {
