@@ -235,6 +235,7 @@ dg_status dg_dequantize(const int32_t *acc_dev, int64_t rows, int64_t C, const f
  *   DG_PERM_PLAN     index of the permute kernel's tile shape
  *   DG_ATTENTION_ROWS  dg_paged_attention's rows a workgroup: "16", "32" or "128"
  *   DG_GEMM_I8_TILE  dg_gemm_i8's tile: "32x64", "64x64", "128x64", "128x128", "256x128" or "256x256" (channels x tokens), whatever the size
+ *   DG_GEMM_MX4_TILE dg_gemm_mx4's tile: those, and "16x16", "16x32", "32x16", "32x32", whatever the size
  */
 typedef enum {
     DG_KERNEL_AUTO = 0,
