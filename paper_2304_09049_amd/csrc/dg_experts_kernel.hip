@@ -496,9 +496,10 @@ void launch(const DgExperts &p, const Rows &x, const Work &work, dg_dtype type, 
     }
     const uint32_t slots = std::min(pairs, p.d.experts);
     const auto grid = [&](int32_t channels, int each, int32_t size) {
-        // (tiles behind one another in a workgroup where there are many: 64 tokens to 6 of 64 experts, 4096 x 1024, binary16 114 us, 110; with a stage of its own a tile would need a third place for its scales)
-        const uint32_t tiles = (channels + each - 1) / each, most = dg_simd_count();
-        return dim3(size <= 256 ? tiles : std::min(tiles, (most + slots - 1) / slots), slots);
+        // (tiles behind one another in a workgroup, as many as leave two workgroups a compute unit, the nearest number; us by that and with one tile each: 64 tokens to 6 of 64 experts, 4096 x 1024, 91 and 96,
+        // 256 to 8 221 and 231, 24 to 4 of 60, 2048 x 1408, 60 and 66; the next larger number instead: 9 to 4 of 64, 2048 x 1024, 40 for 30; with a stage of its own a tile would need a third place for its scales)
+        const uint32_t tiles = (channels + each - 1) / each, room = dg_simd_count() / 2, behind = std::max(1u, (tiles * slots + room / 2) / room);
+        return dim3(size <= 256 ? tiles : (tiles + behind - 1) / behind, slots);
     };
     // (us, 16 and 32 pairs at a time: 64 tokens to 6 of 64 experts, 4096 x 1024, 92 and 105; 128 tokens 144, 131; 64 to 2 of 8, 4096 x 4096, 91, 76: what an expert has of a batch varies, and a pass behind the first costs as much)
     // (16 columns leave a compute unit room for two workgroups; 64 tokens to 6 of 64 experts, 4096 x 1024: down with three stages, one workgroup, 59 us for 40, by eight wavefronts 43)
