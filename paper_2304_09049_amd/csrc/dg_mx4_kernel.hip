@@ -797,8 +797,8 @@ enum class Form { Few16x16, Few16x32, Few32x16, Few32x32, Tile32x64, Tile64x64, 
 
 // The form (channels x tokens a workgroup) whose rounds over the compute units cost least.  `cost`: of a round with a workgroup on each; `both`: with two, where two fit.
 // A round by form, us for K = 2048 and 8192, launch included: 16x16 3.6 (two 4.3), 5.3 (7.4); 16x32 4.2, 6.0; 32x16 4.2 (4.8), 6.9 (7.8); 32x32 4.9 (5.9), 8.3 (10.1); 32x64 5.7, 9.3 (13, where the weights come from
-// memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 50 products, 1 to 4096 tokens,
-// this is within 3 % of the fastest form on 40; the farthest from it: 41 x 4768 x 15264 tokens, positions, channels 1.45 times its time, 32 x 7040 x 5440 1.24, 4 x 10080 x 10784 1.21.
+// memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 239 products drawn (2 to
+// 4096 tokens, weights from memory) this is within 3 % of the fastest form on 209; the farthest from it: 94 x 288 x 4112 tokens, positions, channels 1.19 times its time, 4 x 1216 x 18816 1.16, 498 x 384 x 784 1.15.
 Form form_of(const DgGemmMx4 &p)
 {
     static const struct {
