@@ -222,3 +222,51 @@ def test_binding_shapes():
         dg.dg_route_tokens(x, torch.zeros(2, 32, device=DEV), 1)
     with pytest.raises(ValueError, match="elements"):
         dg.dg_route_tokens(x, torch.zeros(2, 64, device=DEV), 2, ids=ids, weights=w)
+
+
+def test_rows_far_apart():
+    """Offsets of rows pass 32 bits: tokens, the router's rows and results."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("24 GiB")
+    gen = torch.Generator().manual_seed(12)
+    T, E, top, K, F = 70, 40, 3, 96, 64
+    held = make_experts(gen, E, K, F)
+    x, R = torch.randn(T, K, generator=gen).bfloat16(), torch.randn(E, K, generator=gen).bfloat16()
+    apart = (1 << 25) + 6
+    room = torch.empty((T - 1) * apart + K, dtype=torch.bfloat16, device=DEV)
+    far = room.as_strided((T, K), (apart, 1))
+    far.copy_(x)
+    far_R = torch.empty((E - 1) * 2 * apart + K, dtype=torch.bfloat16, device=DEV).as_strided((E, K), (2 * apart, 1))
+    far_R.copy_(R)
+    ids, w = dg.dg_route_tokens(far, far_R, top)
+    near = dg.dg_route_tokens(x.to(DEV), R.to(DEV), top)
+    assert torch.equal(ids, near[0]) and torch.equal(w, near[1])
+    up, ups, _, down, downs, _ = held
+    out = torch.empty((T - 1) * apart + K, dtype=torch.bfloat16, device=DEV).as_strided((T, K), (apart, 1))
+    dg.dg_experts_mx4(up, ups, down, downs, far, ids, w, out=out)
+    assert torch.equal(out, dg.dg_experts_mx4(up, ups, down, downs, x.to(DEV), ids, w))
+    want, off = ref.product(ref.values(*(t.cpu() for t in dg.dg_quantize_mx4(far)), K), held[2][0], None, torch.bfloat16)
+    out = torch.empty((T - 1) * apart + 2 * F, dtype=torch.bfloat16, device=DEV).as_strided((T, 2 * F), (apart, 1))
+    ref.assert_within(dg.dg_linear_mx4(up[0], ups[0], far, out=out), want, off)
+
+
+def test_calls_on_two_streams_at_once():
+    """Workspaces and outputs of their own: whatever else runs, each call's results are those that it gives alone."""
+    gen = torch.Generator().manual_seed(13)
+    E, K, F, top = 24, 512, 256, 4
+    up, ups, _, down, downs, _ = make_experts(gen, E, K, F)
+    R = torch.randn(E, K, generator=gen).to(DEV)
+    batches = [torch.randn(T, K, generator=gen).bfloat16().to(DEV) for T in (3, 40, 200)]
+
+    def layer(x, stream):
+        ids, w = dg.dg_route_tokens(x, R, top, stream=stream)
+        return dg.dg_experts_mx4(up, ups, down, downs, x, ids, w, stream=stream), dg.dg_linear_mx4(up[0], ups[0], x, stream=stream)
+
+    alone = [layer(x, None) for x in batches]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        together = [layer(x, s) for x, s in zip(batches, streams) for _ in range(2)]
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(together):
+            assert torch.equal(a, alone[i // 2][0]) and torch.equal(b, alone[i // 2][1])
