@@ -445,10 +445,21 @@ __global__ __launch_bounds__(256) void experts_join_kernel(DgExperts p, Work wor
     const int32_t m = (blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y, have = min(p.d.hidden - m, 4);
     if (have <= 0) return;
     v4f sum = {};
-#pragma unroll 4
-    for (int32_t j = 0; j < p.top; ++j) {
-        const int32_t pair = t * p.top + j;
-        if ((uint32_t)p.ids[pair] < (uint32_t)p.d.experts) sum += p.weights[pair] * *(const v4f *)(work.y + (int64_t)pair * work.pitch_y + m);
+    constexpr int AT_ONCE = 8;                                       // (all asked for together: what an id that is no expert has in y is loaded and left)
+    for (int32_t first = 0; first < p.top; first += AT_ONCE) {
+        int32_t id[AT_ONCE];
+        float weight[AT_ONCE];
+        v4f y[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int32_t pair = t * p.top + min(first + j, p.top - 1);
+            id[j] = first + j < p.top ? p.ids[pair] : -1;
+            weight[j] = p.weights[pair];
+            y[j] = *(const v4f *)(work.y + (int64_t)pair * work.pitch_y + m);
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+            if ((uint32_t)id[j] < (uint32_t)p.d.experts) sum += weight[j] * y[j];
     }
     T *out = (T *)p.out + t * p.stride_out + m;
     DgVec<T, 4> y;
