@@ -134,7 +134,7 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
     return dg_launch_gemm_mx4(p, out_type, (hipStream_t)hip_stream);
 }
 
-size_t dg_route_tokens_work_bytes(int64_t T, int64_t E) { return route_sizes(T, E) ? (size_t)(4 * T * E) : 0; }
+size_t dg_route_tokens_work_bytes(int64_t T, int64_t E) { return route_sizes(T, E) ? dg_route_work_bytes(T, E) : 0; }
 
 dg_status dg_route_tokens(const void *x_dev, dg_dtype x_type, int64_t T, int64_t K, int64_t stride_x, const void *R_dev, dg_dtype r_type, int64_t E,
                           int64_t stride_r, const float *bias_e_dev, int64_t top, dg_route_mode mode, float factor, int32_t *ids_dev, float *weights_dev,
@@ -154,7 +154,7 @@ dg_status dg_route_tokens(const void *x_dev, dg_dtype x_type, int64_t T, int64_t
     if (!ids_dev || !weights_dev) return dg_fail(DG_ERR_NULL, "%s: NULL output", what);
     s = check_work(what, work_dev, work_bytes, dg_route_tokens_work_bytes(T, E));
     if (s) return s;
-    const DgRoute p = {x_dev, R_dev, stride_x, stride_r, (int32_t)T, (int32_t)K, (int32_t)E, (int32_t)top, bias_e_dev, mode, factor, ids_dev, weights_dev, (float *)work_dev};
+    const DgRoute p = {x_dev, R_dev, stride_x, stride_r, (int32_t)T, (int32_t)K, (int32_t)E, (int32_t)top, bias_e_dev, mode, factor, ids_dev, weights_dev, {(float *)work_dev}};
     return dg_launch_route(p, x_type, r_type, (hipStream_t)hip_stream);
 }
 

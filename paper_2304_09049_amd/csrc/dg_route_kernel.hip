@@ -5,6 +5,8 @@ namespace {
 
 typedef double v4d __attribute__((ext_vector_type(4)));
 
+constexpr int PARTS = 4;                 // of K, where tiles of 16 tokens and 16 experts are fewer than the compute units
+
 // ---- logits --------------------------------------------------------------------------------------------------------------
 //
 // Which experts a token goes to is decided by comparing sums that may lie as close as their rounding errors, and a choice that changes with the order of summation is
@@ -15,7 +17,7 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 
 // Many tokens: 16 SIDE of them and 16 SIDE experts a workgroup, straight from memory, eight wavefronts sharing K, a step's loads under way while the one before is multiplied (2048 tokens
 // of 4096 to 64 experts 34.7 -> 29.3 us with the choice).  With SIDE = 2 the matrix instruction bounds it, and what the address units take for loads of 16 rows (8192 tokens of 2048 to 128
-// experts 78 us, 55 of the 70.8 TFLOP/s that a large binary64 matrix product reaches; with SIDE = 1 95); with SIDE = 1 and hundreds of tokens the waits for memory.  Tiles of 32 tokens and
+// experts 78 us, 55 of the 70.8 TFLOP/s that a large binary64 matrix product reaches; with SIDE = 1 95); with SIDE = 1 and hundreds of tokens what a compute unit multiplies.  Tiles of 32 tokens and
 // 128 experts staged in LDS took 75 us there, but 136 against 98 at 12000 tokens and up to four times as long where tokens are hundreds: few large tiles end in rounds that leave compute units without work.
 template <class X, class R, int SIDE>
 __global__ __launch_bounds__(512, 4) void route_many_kernel(DgRoute p)
@@ -24,6 +26,7 @@ __global__ __launch_bounds__(512, 4) void route_many_kernel(DgRoute p)
     __shared__ v4d sums[WAVES][SIDE * SIDE][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t e0 = blockIdx.x * (16 * SIDE), t0 = blockIdx.y * (16 * SIDE);
+    const int32_t share = (p.K + EACH * gridDim.z - 1) / (EACH * (int32_t)gridDim.z) * EACH, begin = blockIdx.z * share, end = min(p.K, begin + share);       // (whole steps, but for the last part's)
     const X *x[SIDE];
     const R *w[SIDE];
 #pragma unroll
@@ -53,28 +56,28 @@ __global__ __launch_bounds__(512, 4) void route_many_kernel(DgRoute p)
     constexpr int STEP = EACH * WAVES;
     DgVec<X, COUNT> xk[2][SIDE];
     DgVec<R, COUNT> wk[2][SIDE];
-    int32_t k = EACH * wave;
-    if (k + EACH <= p.K) load(xk[0], wk[0], k + COUNT * g);
-    while (k + EACH <= p.K) {
-        if (k + STEP + EACH <= p.K) load(xk[1], wk[1], k + STEP + COUNT * g);
+    int32_t k = begin + EACH * wave;
+    if (k + EACH <= end) load(xk[0], wk[0], k + COUNT * g);
+    while (k + EACH <= end) {
+        if (k + STEP + EACH <= end) load(xk[1], wk[1], k + STEP + COUNT * g);
         __builtin_amdgcn_sched_barrier(0);
         add(xk[0], wk[0]);
         k += STEP;
-        if (k + EACH > p.K) break;
-        if (k + STEP + EACH <= p.K) load(xk[0], wk[0], k + STEP + COUNT * g);
+        if (k + EACH > end) break;
+        if (k + STEP + EACH <= end) load(xk[0], wk[0], k + STEP + COUNT * g);
         __builtin_amdgcn_sched_barrier(0);
         add(xk[1], wk[1]);
         k += STEP;
     }
-    if (k < p.K) {                                                   // (one by one: unrolled it would take registers that the loop needs)
+    if (k < end) {                                                   // (one by one: unrolled it would take registers that the loop needs)
 #pragma unroll 1
         for (int q = 0; q < COUNT; ++q) {
             const int32_t at = k + COUNT * g + q;
             double xq[SIDE], wq[SIDE];
 #pragma unroll
-            for (int i = 0; i < SIDE; ++i) xq[i] = at < p.K ? dg_to_float(x[i][at]) : 0.0f;
+            for (int i = 0; i < SIDE; ++i) xq[i] = at < end ? dg_to_float(x[i][at]) : 0.0f;
 #pragma unroll
-            for (int j = 0; j < SIDE; ++j) wq[j] = at < p.K ? dg_to_float(w[j][at]) : 0.0f;
+            for (int j = 0; j < SIDE; ++j) wq[j] = at < end ? dg_to_float(w[j][at]) : 0.0f;
 #pragma unroll
             for (int i = 0; i < SIDE * SIDE; ++i) acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(wq[i % SIDE], xq[i / SIDE], acc[i], 0, 0, 0);
         }
@@ -89,7 +92,10 @@ __global__ __launch_bounds__(512, 4) void route_many_kernel(DgRoute p)
     const int32_t t = t0 + 16 * (wave / SIDE) + r, e = e0 + 16 * (wave % SIDE) + g;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (e + 4 * i < p.E && t < p.T) p.logits[(int64_t)t * p.E + e + 4 * i] = (float)s[i];
+        if (e + 4 * i < p.E && t < p.T) {
+            if (gridDim.z == 1) p.logits[(int64_t)t * p.E + e + 4 * i] = (float)s[i];
+            else p.sums[((int64_t)blockIdx.z * p.T + t) * p.E + e + 4 * i] = s[i];
+        }
 }
 
 // The sum over a wavefront's lanes, in each of them.
@@ -171,19 +177,34 @@ __device__ __forceinline__ uint64_t key_of(double choice)
     return choice == -__builtin_inf() ? 0 : bits ^ ((uint64_t)((int64_t)bits >> 63) | 0x8000000000000000ull);
 }
 
-template <int HELD, int WAVES>
+template <int HELD, int WAVES, bool PARTED>
 __global__ __launch_bounds__(64 * WAVES) void route_choose_kernel(DgRoute p, int64_t first)
 {
     const int lane = threadIdx.x & 63;
     const int64_t t = first + (int64_t)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= p.T) return;
-    const float *row = p.logits + t * p.E;
     const float none = -__builtin_inff();
     float logit[HELD];
     uint64_t key[HELD];
     bool whole = true;
+    if (PARTED) {
+        double part[HELD][PARTS];
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) logit[i] = lane + 64 * i < p.E ? row[lane + 64 * i] : none;
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) part[i][k] = lane + 64 * i < p.E ? p.sums[((int64_t)k * p.T + t) * p.E + lane + 64 * i] : 0.0;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            double sum = part[i][0];
+#pragma unroll
+            for (int k = 1; k < PARTS; ++k) sum += part[i][k];
+            logit[i] = lane + 64 * i < p.E ? (float)sum : none;
+        }
+    } else {
+        const float *row = p.logits + t * p.E;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) logit[i] = lane + 64 * i < p.E ? row[lane + 64 * i] : none;
+    }
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         const bool there = lane + 64 * i < p.E;
@@ -257,49 +278,60 @@ __global__ __launch_bounds__(64 * WAVES) void route_choose_kernel(DgRoute p, int
 }
 
 template <int HELD>
-void choose(const DgRoute &p, hipStream_t stream)
+void choose(const DgRoute &p, bool parted, hipStream_t stream)
 {
     dg_in_turns(p.T, 1 << 24, [&](int64_t t, int64_t count) {
-        route_choose_kernel<HELD, 4><<<(uint32_t)((count + 3) / 4), 256, 0, stream>>>(p, t);
+        const uint32_t grid = (uint32_t)((count + 3) / 4);
+        if (parted) route_choose_kernel<HELD, 4, true><<<grid, 256, 0, stream>>>(p, t);
+        else route_choose_kernel<HELD, 4, false><<<grid, 256, 0, stream>>>(p, t);
         return DG_OK;
     });
 }
 
-// The few-token kernel reads the router once for four tokens and takes sums one by one: it is the faster one to 12288 sums (us with the choice, its and the other's: 64 x 4096 to
-// 64 experts 9.6 and 18.8, 96 x 2048 to 128 11.6 and 12.2, 128 x 2048 to 128 13.6 and 12.3, 64 x 4096 to 256 20 and 22, 256 x 4096 to 64 21.6 and 19.4).  Of the other's tiles the larger
-// are the faster ones where every compute unit gets two (the smaller's and the larger's, before loads ran ahead: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53, 6000 x 4096 to 64 80
-// and 96, 8192 x 2048 to 256 with a router in binary32 193 and 171).
+int64_t tiles(int64_t T, int64_t E, int side) { return (T + side - 1) / side * ((E + side - 1) / side); }
+// The few-token kernel reads the router once for four tokens and takes sums one by one: it is the faster one to some 2500 sums (us with the choice, its and the others' with K in parts:
+// 64 x 5120 to 16 experts, router in binary32, 8.1 and 9.5, 128 tokens 9.8 and 9.6; 32 x 4096 to 64 7.9 and 8.5, 64 tokens 9.3 and 8.7; 64 x 1352 to 64 7.2 and 7.7; 64 x 2048 to 128 9.7 and 7.8).
+bool few(int64_t T, int64_t E) { return T == 1 || T * E <= 2560; }
+// A tile's products by one compute unit bound what has fewer tiles than there are units, whatever the number of tokens: K in parts, one and four (128 x 4096 to 64 17.4 and 8.8, 512 x 5120 to 16 20.3 and
+// 9.8, 256 x 2048 to 128 12.2 and 9.8, but 1024 x 1352 to 64, 256 tiles, 11.5 and 12.1).  (The work buffer's size goes by this.)
+bool in_parts(int64_t T, int64_t E) { return !few(T, E) && tiles(T, E, 16) <= 192; }
+
+// Of the tiles the larger are the faster ones where every compute unit gets two (us, the smaller's and the larger's, before loads ran ahead: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53,
+// 6000 x 4096 to 64 80 and 96, 8192 x 2048 to 256 with a router in binary32 193 and 171).
 template <class X, class R>
-void logits(const DgRoute &p, hipStream_t stream)
+bool logits(const DgRoute &p, hipStream_t stream)
 {
-    const auto tiles = [&](int64_t tokens, int side) { return (tokens + side - 1) / side * ((p.E + side - 1) / side); };
+    const bool parted = in_parts(p.T, p.E) && p.K >= 1024;
     dg_in_turns(p.T, 16 * 65535, [&](int64_t t, int64_t count) {
         DgRoute part = p;
         part.x = (const X *)p.x + t * p.stride_x;
-        part.logits += t * p.E;
+        if (!parted) part.logits += t * p.E;                        // (parts are of one turn)
         part.T = (int32_t)count;
         if (count == 1) route_few_kernel<X, R, 1><<<p.E, 256, 0, stream>>>(part);
-        else if (count * p.E <= 12288) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
-        else if (tiles(count, 32) >= dg_simd_count() / 2) route_many_kernel<X, R, 2><<<dim3((p.E + 31) / 32, (uint32_t)((count + 31) / 32)), 512, 0, stream>>>(part);
-        else route_many_kernel<X, R, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16)), 512, 0, stream>>>(part);
+        else if (few(count, p.E)) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
+        else if (tiles(count, p.E, 32) >= dg_simd_count() / 2) route_many_kernel<X, R, 2><<<dim3((p.E + 31) / 32, (uint32_t)((count + 31) / 32)), 512, 0, stream>>>(part);
+        else route_many_kernel<X, R, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16), parted ? PARTS : 1), 512, 0, stream>>>(part);
         return DG_OK;
     });
+    return parted;
 }
 
 }   // namespace
 
+size_t dg_route_work_bytes(int64_t T, int64_t E) { return (size_t)(T * E) * (in_parts(T, E) ? PARTS * sizeof(double) : sizeof(float)); }
+
 dg_status dg_launch_route(const DgRoute &p, dg_dtype x_type, dg_dtype r_type, hipStream_t stream)
 {
+    bool parted = false;
     dg_with_type(x_type, [&](auto t) {
         typedef decltype(t) X;
-        if (r_type == DG_F32) logits<X, float>(p, stream);
-        else logits<X, X>(p, stream);
+        parted = r_type == DG_F32 ? logits<X, float>(p, stream) : logits<X, X>(p, stream);
         return 0;
     });
-    if (p.E <= 64) choose<1>(p, stream);
-    else if (p.E <= 128) choose<2>(p, stream);
-    else if (p.E <= 256) choose<4>(p, stream);
-    else if (p.E <= 512) choose<8>(p, stream);
-    else choose<16>(p, stream);
+    if (p.E <= 64) choose<1>(p, parted, stream);
+    else if (p.E <= 128) choose<2>(p, parted, stream);
+    else if (p.E <= 256) choose<4>(p, parted, stream);
+    else if (p.E <= 512) choose<8>(p, parted, stream);
+    else choose<16>(p, parted, stream);
     return dg_check_launch("dg_route_tokens");
 }

@@ -25,7 +25,7 @@ def check_route(x, R, top, mode, bias=None, factor=1.0):
                                                          (17, 1000, 60, 6, "bf16", "f32", True), (16, 64, 128, 8, "f16", "f32", False), (70, 257, 200, 3, "f32", "f32", True),
                                                          (5, 100, 1000, 64, "bf16", "bf16", True), (33, 520, 256, 1, "bf16", "bf16", False), (2, 5000, 300, 8, "f32", "f32", True),
                                                          (600, 96, 31, 7, "f16", "f16", True), (1, 7943, 513, 16, "bf16", "f32", False), (32, 300, 40, 4, "f16", "f16", False), (130, 264, 128, 4, "bf16", "f32", True), (65, 5000, 64, 4, "f16", "f16", False), (40, 72, 300, 4, "f32", "f32", False), (200, 101, 70, 4, "f32", "f32", False),
-                                                         (4100, 200, 60, 4, "bf16", "f32", True), (4097, 64, 130, 3, "f16", "f16", False), (4200, 328, 100, 5, "f32", "f32", True), (4100, 75, 64, 2, "bf16", "bf16", False)])
+                                                         (100, 1024, 33, 4, "bf16", "bf16", True), (257, 1339, 70, 5, "f16", "f32", False), (700, 2080, 20, 2, "f32", "f32", True), (40, 4096, 1000, 9, "bf16", "bf16", False), (6, 1500, 600, 3, "f16", "f16", True), (4100, 200, 60, 4, "bf16", "f32", True), (4097, 64, 130, 3, "f16", "f16", False), (4200, 328, 100, 5, "f32", "f32", True), (4100, 75, 64, 2, "bf16", "bf16", False)])
 def test_route(T, K, E, top, dtype, rdtype, bias, mode):
     gen = torch.Generator().manual_seed(T + K + E)
     x = torch.randn(T, K + 4, generator=gen).to(ref.TYPES[dtype]).to(DEV)[:, (at := T % 2 * 2 + (T % 5 == 3 or T < 20)):K + at]       # (some rows begin on words, others anywhere)
