@@ -115,6 +115,14 @@ def test_experts(T, E, top, K, F, apart, dtype):
     check_experts(held, torch.randn(T, K, generator=gen).to(ref.TYPES[dtype]), *choices(gen, T, E, top))
 
 
+@pytest.mark.parametrize("F", [32, 250, 300, 1100, 4200])
+@pytest.mark.parametrize("T,top", [(1, 1), (2, 1), (1, 3), (2, 2), (5, 1), (1, 6)])
+def test_experts_few_pairs(T, top, F):
+    """Fewer pairs than a workgroup's wavefronts share inner as well."""
+    gen = torch.Generator().manual_seed(T * 64 + top + F)
+    check_experts(make_experts(gen, 6, 72, F), torch.randn(T, 72, generator=gen).bfloat16(), *choices(gen, T, 6, top))
+
+
 @pytest.mark.parametrize("T,top", [(300, 2), (700, 1), (70, 64)])
 def test_experts_in_turns(T, top):
     gen = torch.Generator().manual_seed(T)
