@@ -108,7 +108,7 @@ def choices(gen, T, E, top):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("T,E,top,K,F,apart", [(1, 1, 1, 1, 1, 0), (1, 8, 2, 256, 128, 0), (1, 64, 4, 160, 96, 1), (3, 4, 4, 33, 17, 0), (5, 60, 5, 100, 130, 2), (16, 8, 2, 512, 160, 0),
-                                               (37, 6, 3, 131, 65, 1), (64, 3, 1, 96, 64, 0), (40, 200, 2, 64, 33, 0), (130, 5, 2, 70, 40, 0), (9, 16, 8, 1056, 544, 0)])
+                                               (37, 6, 3, 131, 65, 1), (64, 3, 1, 96, 64, 0), (40, 200, 2, 64, 33, 0), (130, 5, 2, 70, 40, 0), (9, 16, 8, 1056, 544, 0), (200, 4, 4, 140, 300, 0), (256, 2, 1, 288, 96, 1)])
 def test_experts(T, E, top, K, F, apart, dtype):
     gen = torch.Generator().manual_seed(T * 31 + E + K + F)
     held = make_experts(gen, E, K, F, apart)
