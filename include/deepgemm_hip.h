@@ -482,7 +482,7 @@ dg_status dg_paged_attention(const dg_cache_desc *desc, const void *cache_dev, s
  *     value       the element times s; NaN where the byte is 255
  * Layout: element k of a row has the half k % 2 (0: low) of byte k / 2; a row is whole blocks, ceil(K/32) * 16 bytes, codes from K on being 0; its scales are
  * ceil(K/32) bytes.  Rows of codes begin on 16 bytes, rows of scales on 4 (else DG_ERR_BUFFER), at most 2^26 bytes apart (else DG_ERR_RANGE), and a row's last word of scales can be read whole (what is in the
- * bytes past the scales does not matter).
+ * bytes past the scales does not matter).  Rows of codes that begin on 128 bytes are the fastest: others straddle cache lines, and a product takes up to a fifth longer.
  */
 
 /*

@@ -553,10 +553,11 @@ def dg_paged_attention(desc: CacheDesc, cache, q, q_start, ctx_len, table, max_q
 
 def dg_quantize_mx4(x, codes=None, scales=None, stream=None):
     """x: float32, float16 or bfloat16 device tensor [N][K] (rows may lie apart) -> (codes, scales): uint8 [N][16 * blocks], two codes a byte, and uint8
-    [N][blocks], a power of two for each block of 32.  The scales made here are rows of whole words of four bytes (a view)."""
+    [N][blocks], a power of two for each block of 32.  The rows made here are views: scales' of whole words of
+    four bytes, long codes' of whole cache lines (products of rows that begin inside one take up to a fifth longer)."""
     blocks = -(-x.shape[1] // 32)
     if codes is None:
-        codes = _new((x.shape[0], 16 * blocks), "uint8", x.device, stream)
+        codes = _new((x.shape[0], 16 * blocks if blocks <= 64 else -(-blocks // 8) * 128), "uint8", x.device, stream)[:, :16 * blocks]
     if scales is None:
         scales = _new((x.shape[0], -(-blocks // 4) * 4), "uint8", x.device, stream)[:, :blocks]
     status = (_native or _load_native()).quantize_mx4(x, codes, scales, stream)

@@ -11,6 +11,8 @@ constexpr int64_t MOST_STRIDE = (int64_t)1 << 26;        // 32 rows of a product
 bool known_type(dg_dtype t) { return t == DG_F32 || t == DG_F16 || t == DG_BF16; }
 
 int64_t blocks_of(int64_t K) { return (K + 31) / 32; }
+// Rows of tokens: long ones in whole cache lines (1024 x 7360 x 4096 28.0 us with rows of 3680 bytes, 26.3 with 3712; 355 x 7360 x 3456 20.4, 17.2).
+int64_t codes_pitch(int64_t K) { return blocks_of(K) <= 64 ? 16 * blocks_of(K) : (blocks_of(K) + 7) / 8 * 128; }
 int64_t scales_pitch(int64_t K) { return (blocks_of(K) + 3) / 4 * 4; }
 bool aligned(const void *p, int64_t stride, int to) { return (uintptr_t)p % to == 0 && stride % to == 0; }
 
@@ -111,7 +113,7 @@ dg_status dg_gemm_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_s
 
 size_t dg_linear_mx4_work_bytes(int64_t N, int64_t K)
 {
-    return N <= 0 || K <= 0 || N > MOST_ROWS || K > MOST_K ? 0 : (size_t)(N * (16 * blocks_of(K) + scales_pitch(K)));
+    return N <= 0 || K <= 0 || N > MOST_ROWS || K > MOST_K ? 0 : (size_t)(N * (codes_pitch(K) + scales_pitch(K)));
 }
 
 dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_scales_dev, int64_t stride_ws, const void *x_dev, dg_dtype x_type,
@@ -125,8 +127,8 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
     if (s || N == 0) return s;
     s = check_work(what, work_dev, work_bytes, dg_linear_mx4_work_bytes(N, K));
     if (s) return s;
-    uint8_t *codes = (uint8_t *)work_dev, *scales = codes + N * 16 * blocks_of(K);
-    const DgGemmMx4 p = {W_dev, W_scales_dev, codes, scales, stride_w, stride_ws, 16 * blocks_of(K), scales_pitch(K), (int32_t)M, (int32_t)N,
+    uint8_t *codes = (uint8_t *)work_dev, *scales = codes + N * codes_pitch(K);
+    const DgGemmMx4 p = {W_dev, W_scales_dev, codes, scales, stride_w, stride_ws, codes_pitch(K), scales_pitch(K), (int32_t)M, (int32_t)N,
                          (int32_t)blocks_of(K), bias_m_dev, out_dev, stride_out};
     if (dg_linear_mx4_fuses(N, x_dev)) return dg_launch_linear_mx4_fused(p, x_dev, x_type, K, out_type, (hipStream_t)hip_stream);
     s = dg_launch_quantize_mx4(x_dev, x_type, N, K, stride_x, codes, p.stride_a, scales, p.stride_as, (hipStream_t)hip_stream);

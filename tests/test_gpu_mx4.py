@@ -160,7 +160,7 @@ def test_linear_of_one_token(M, K, dtype):
     assert torch.isnan(out).all()
 
 
-@pytest.mark.parametrize("N,K,dtype", [(0, 64, "bf16"), (1, 4096, "bf16"), (1, 77, "f32"), (7, 2000, "f16"), (40, 333, "f32"), (200, 1024, "bf16")])
+@pytest.mark.parametrize("N,K,dtype", [(0, 64, "bf16"), (1, 4096, "bf16"), (1, 77, "f32"), (7, 2000, "f16"), (40, 333, "f32"), (200, 1024, "bf16"), (33, 2500, "f16"), (130, 2085, "bf16")])
 def test_linear_is_quantize_and_product(N, K, dtype):
     gen = torch.Generator().manual_seed(N + K)
     W, Ws, _ = held(gen, 150, K)
