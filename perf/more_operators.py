@@ -217,8 +217,7 @@ def _activations(gen, rows, K, dtype):
 def _weights(gen, rows, K):
     """A layer's weights, each row of its own size, quantised and packed."""
     W = torch.randn(rows, K, device="cuda", generator=gen) * ((0.5 + torch.rand(rows, 1, device="cuda", generator=gen)) / math.sqrt(K))
-    packed, scales = _pack(*_quantize(W))
-    return packed.to(torch.uint8), scales
+    return _pack(*_quantize(W))
 
 
 def _router(case, gen):
@@ -254,8 +253,7 @@ def prepare(case, seed):
         if kind == "linear":
             state["x"] = x
         else:
-            A, state["A_scales"] = _pack(*_quantize(x.float()))
-            state["A"] = A.to(torch.uint8)
+            state["A"], state["A_scales"] = _pack(*_quantize(x.float()))
         return state
     if kind == "experts":
         x = _activations(gen, case["T"], case["K"], case["dtype"])
@@ -296,6 +294,10 @@ def run(state):
             return _experts(state, state["x"], state["ids"], state["weights"])
         ids, weights = _route(state["x"], state["R"], case["top"], case["mode"], state["bias"], state["factor"])
         return (ids, weights) if kind == "route" else (ids, weights, _experts(state, state["x"], ids, weights))
+    else:
+        for name in ("W", "A"):                                  # (a program holds codes as bytes: the library's calls take nothing else)
+            if name in state and state[name].dtype != torch.uint8:
+                state[name] = state[name].to(torch.uint8)
     from paper_2304_09049_amd import binding as dg
     if kind == "quantize":
         dg.dg_quantize_mx4(state["x"], codes=state["codes"], scales=state["scales"])
