@@ -378,6 +378,8 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
         const auto fetch = [&]() __attribute__((always_inline)) {
             const int32_t b = 8 * ahead;
             if (ahead % 4 == 0) {
+                // (this place's last scales are read: the fifth stage of a tile of five has the other place, and the next tile's first comes here two stages ahead)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 const uint32_t at = scale_lds + scale_to * SCALES;
                 const int row = (lane & 31) >> 1;
                 const int32_t k = b + 16 * (lane & 1);
@@ -410,13 +412,15 @@ __global__ __launch_bounds__(64 * WAVES) void experts_kernel(DgExperts p, Rows r
 #pragma unroll 1
             for (int32_t s = 0; s < stages; ++s) {
                 dg_wait_for_loads<(RING - 2) * LOADS>();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (nothing of the stage before is still being read)
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
-                fetch();
+                // (its scales before the loads, which may bring others to their place)
                 if (s % 4 == 0) scale_now ^= 1;
                 uint32_t byte[2][2];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) byte[i / 2][i % 2] = scale_room[scale_now * SCALES + 512 * (i / 2) + 32 * r + 8 * (s % 4) + 4 * (i % 2) + g];
+                fetch();
                 if (8 * s + 8 > blocks) {
                     // scales past the row: its codes are 0, and 0 by whatever lies there might be no number
 #pragma unroll
