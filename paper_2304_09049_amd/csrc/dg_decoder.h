@@ -263,7 +263,6 @@ struct DgRoute {
         double *sums;                                    // of parts of K: [parts][T][E]
     };
 };
-size_t dg_route_work_bytes(int64_t T, int64_t E);
 dg_status dg_launch_route(const DgRoute &p, dg_dtype x_type, dg_dtype r_type, hipStream_t stream);
 
 struct DgExperts {

@@ -1,6 +1,7 @@
 // Host side of the calls around microscaled 4-bit floating point: argument validation.  As in dg_api.hip, everything is checked before anything is launched, and nothing
 // synchronises.
 #include "dg_decoder.h"
+#include "dg_route_rule.h"
 
 namespace {
 

@@ -1,11 +1,12 @@
 // A router: logits in binary64, each token's largest choices, their weights.
 #include "dg_mx4.h"
+#include "dg_route_rule.h"
 
 namespace {
 
 typedef double v4d __attribute__((ext_vector_type(4)));
 
-constexpr int PARTS = 4;                 // of K, where tiles of 16 tokens and 16 experts are fewer than the compute units
+constexpr int PARTS = DG_ROUTE_PARTS;
 
 // ---- logits --------------------------------------------------------------------------------------------------------------
 //
@@ -288,37 +289,30 @@ void choose(const DgRoute &p, bool parted, hipStream_t stream)
     });
 }
 
-int64_t tiles(int64_t T, int64_t E, int side) { return (T + side - 1) / side * ((E + side - 1) / side); }
-// The few-token kernel reads the router once for four tokens and takes sums one by one: it is the faster one to some 2500 sums (us with the choice, its and the others' with K in parts:
-// 64 x 5120 to 16 experts, router in binary32, 8.1 and 9.5, 128 tokens 9.8 and 9.6; 32 x 4096 to 64 7.9 and 8.5, 64 tokens 9.3 and 8.7; 64 x 1352 to 64 7.2 and 7.7; 64 x 2048 to 128 9.7 and 7.8).
-bool few(int64_t T, int64_t E) { return T == 1 || T * E <= 2560; }
-// A tile's products by one compute unit bound what has fewer tiles than there are units, whatever the number of tokens: K in parts, one and four (128 x 4096 to 64 17.4 and 8.8, 512 x 5120 to 16 20.3 and
-// 9.8, 256 x 2048 to 128 12.2 and 9.8, but 1024 x 1352 to 64, 256 tiles, 11.5 and 12.1).  (The work buffer's size goes by this.)
-bool in_parts(int64_t T, int64_t E) { return !few(T, E) && tiles(T, E, 16) <= 192; }
-
-// Of the tiles the larger are the faster ones where every compute unit gets two (us, the smaller's and the larger's, before loads ran ahead: 2048 x 2048 to 128 32.6 and 35, 4096 x 2048 to 128 55 and 53,
-// 6000 x 4096 to 64 80 and 96, 8192 x 2048 to 256 with a router in binary32 193 and 171).
 template <class X, class R>
 bool logits(const DgRoute &p, hipStream_t stream)
 {
-    const bool parted = in_parts(p.T, p.E) && p.K >= 1024;
+    const int64_t units = dg_simd_count() / 4;
+    const bool parted = dg_route_form(p.T, p.E, p.K, units) == DgRouteForm::Parts16;
     dg_in_turns(p.T, 16 * 65535, [&](int64_t t, int64_t count) {
         DgRoute part = p;
         part.x = (const X *)p.x + t * p.stride_x;
         if (!parted) part.logits += t * p.E;                        // (parts are of one turn)
         part.T = (int32_t)count;
-        if (count == 1) route_few_kernel<X, R, 1><<<p.E, 256, 0, stream>>>(part);
-        else if (few(count, p.E)) route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part);
-        else if (tiles(count, p.E, 32) >= dg_simd_count() / 2) route_many_kernel<X, R, 2><<<dim3((p.E + 31) / 32, (uint32_t)((count + 31) / 32)), 512, 0, stream>>>(part);
-        else route_many_kernel<X, R, 1><<<dim3((p.E + 15) / 16, (uint32_t)((count + 15) / 16), parted ? PARTS : 1), 512, 0, stream>>>(part);
+        const dim3 tiles16((p.E + 15) / 16, (uint32_t)((count + 15) / 16), parted ? PARTS : 1);
+        switch (dg_route_form(count, p.E, p.K, units)) {
+        case DgRouteForm::One: route_few_kernel<X, R, 1><<<p.E, 256, 0, stream>>>(part); break;
+        case DgRouteForm::Four: route_few_kernel<X, R, 4><<<dim3(p.E, (uint32_t)((count + 3) / 4)), 256, 0, stream>>>(part); break;
+        case DgRouteForm::Tiles32: route_many_kernel<X, R, 2><<<dim3((p.E + 31) / 32, (uint32_t)((count + 31) / 32)), 512, 0, stream>>>(part); break;
+        case DgRouteForm::Tiles16:
+        case DgRouteForm::Parts16: route_many_kernel<X, R, 1><<<tiles16, 512, 0, stream>>>(part); break;
+        }
         return DG_OK;
     });
     return parted;
 }
 
 }   // namespace
-
-size_t dg_route_work_bytes(int64_t T, int64_t E) { return (size_t)(T * E) * (in_parts(T, E) ? PARTS * sizeof(double) : sizeof(float)); }
 
 dg_status dg_launch_route(const DgRoute &p, dg_dtype x_type, dg_dtype r_type, hipStream_t stream)
 {
