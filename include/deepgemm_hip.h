@@ -526,7 +526,7 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
  *             sigmoid(l) / sum over the taken of sigmoid(l) (0 where that is 0)
  * A token with a NaN among its l or choices gets the experts 0 ... top - 1 and weights NaN: whatever is computed from it shows it.
  * x_dev: [T][K] of x_type, rows stride_x elements apart; R_dev: [E][K] of r_type (x_type or DG_F32), stride_r.  ids_dev, weights_dev: contiguous [T][top].
- * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned.  E <= 1024, top <= 64, K <= 2^24.
+ * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned; what it says never falls as T grows, so a buffer for the largest batch does for the others.  E <= 1024, top <= 64, K <= 2^24.
  * Errors: DG_ERR_NULL; DG_ERR_SHAPE (T < 0, K, E, top <= 0, top > E, a stride below its row); DG_ERR_RANGE (E, top, K, T * E of 2^31 and more); DG_ERR_UNSUPPORTED; DG_ERR_BUFFER.
  */
 typedef enum { DG_ROUTE_SOFTMAX = 0, DG_ROUTE_SOFTMAX_ALL = 1, DG_ROUTE_SIGMOID = 2 } dg_route_mode;

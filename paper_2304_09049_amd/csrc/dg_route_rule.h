@@ -27,5 +27,11 @@ inline DgRouteForm dg_route_form(int64_t T, int64_t E, int64_t K, int64_t units)
     return dg_route_tiles(T, E, 32) >= 2 * units ? DgRouteForm::Tiles32 : DgRouteForm::Tiles16;
 }
 
-// Logits in binary32, or the parts' sums in binary64.
-inline size_t dg_route_work_bytes(int64_t T, int64_t E) { return (size_t)(T * E) * (dg_route_in_parts(T, E) ? DG_ROUTE_PARTS * sizeof(double) : sizeof(float)); }
+// Logits in binary32, or the parts' sums in binary64, whichever a call of so many tokens or of fewer takes more for: a buffer for a program's largest batch suffices for its others.  (What is in parts is at most 192
+// tiles, 1.5 MB of sums; the most tokens that may be are the last before a 193rd.)
+inline size_t dg_route_work_bytes(int64_t T, int64_t E)
+{
+    const int64_t most = 192 / ((E + 15) / 16) * 16, parts = T < most ? T : most;
+    const int64_t whole = T * E * (int64_t)sizeof(float), sums = dg_route_in_parts(parts, E) ? parts * E * DG_ROUTE_PARTS * (int64_t)sizeof(double) : 0;
+    return (size_t)(whole > sums ? whole : sums);
+}

@@ -1,0 +1,30 @@
+"""The router's kernels for many tokens, and one work buffer for batches of all sizes."""
+import pytest
+import torch
+
+import mx4_reference as ref
+from paper_2304_09049_amd import binding as dg
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def operands(gen, T, K, E, dtype, rdtype):
+    x = torch.randn(T, K, generator=gen, device=DEV).to(ref.TYPES[dtype])
+    return x, (torch.randn(E, K, generator=gen, device=DEV) * K ** -0.5).to(ref.TYPES[rdtype])
+
+
+@pytest.mark.parametrize("K,E", [(1024, 64), (1100, 16), (200, 130)])
+def test_one_buffer_for_all_batches(K, E):
+    gen = torch.Generator(device=DEV).manual_seed(E)
+    x, R = operands(gen, 1300, K, E, "bf16", "bf16")
+    work = torch.empty(dg.dg_route_tokens_work_bytes(1300, E), dtype=torch.uint8, device=DEV)
+    for T in (1300, 1, 768, 3, 769, 512, 40, 1024, 200, 41):
+        ids, w = dg.dg_route_tokens(x[:T], R, 4, work=work)
+        alone = dg.dg_route_tokens(x[:T], R, 4)
+        assert torch.equal(ids, alone[0]) and torch.equal(w, alone[1])
+        logits = (x[:T].cpu().double() @ R.cpu().double().t()).float()
+        want = torch.sort(logits, dim=1, descending=True, stable=True)
+        assert torch.equal(ids.cpu().long(), want.indices[:, :4])
+        # a softmax over four: exponents of at most some 10, two exponentials, a sum of 4 and a quotient
+        ref.assert_within(w, torch.softmax(want.values[:, :4].double(), 1), torch.full((T, 4), 64 * 2.0 ** -24, dtype=torch.float64))

@@ -4,6 +4,7 @@ import subprocess
 
 import pytest
 
+from paper_2304_09049_amd import binding as dg
 from paper_2304_09049_amd.build import CSRC
 
 PROGRAM = """
@@ -55,3 +56,18 @@ def test_the_measured_sides(rule):
 def test_what_a_device_of_few_units_would_take_by_both_rules(rule):
     """2560 tokens to 16 experts: 160 tiles of 16 x 16, and 80 of 32 x 32 for 32 units."""
     assert [f for f, _ in rule([(2560, 16, 1024, u) for u in (32, 40, 256)])] == [PARTS16] * 3
+
+
+@pytest.mark.parametrize("E", [1, 2, 7, 8, 16, 17, 33, 60, 64, 128, 200, 256, 1000, 1024])
+def test_a_buffer_for_more_tokens_suffices_for_fewer(E):
+    """A program makes it once, for its largest batch."""
+    sizes = [dg.dg_route_tokens_work_bytes(T, E) for T in range(1, 10000)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    assert sizes[-1] <= max(4 * E * 9999, 32 * 192 * 256)
+
+
+def test_every_form_fits_a_buffer_for_more_tokens(rule):
+    calls = [(T, E, 4096, 256) for E in (1, 8, 60, 64, 100, 1024) for T in range(1, 4000, 7)]
+    for (T, E, _, _), (form, _) in zip(calls, rule(calls)):
+        for more in (0, 1, 100, 5000):
+            assert dg.dg_route_tokens_work_bytes(T + more, E) >= T * E * (32 if form == PARTS16 else 4), (T, E, more)
