@@ -508,7 +508,7 @@ dg_status dg_gemm_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_s
                       const uint8_t *A_scales_dev, int64_t stride_as, int64_t M, int64_t N, int64_t K, const float *bias_m_dev, void *out_dev,
                       dg_dtype out_type, int64_t stride_out, void *hip_stream);
 /*
- * The layer from activations that are not quantised yet: dg_quantize_mx4 and dg_gemm_mx4 as one call, with their results.
+ * The layer from activations that are not quantised yet: dg_quantize_mx4 and dg_gemm_mx4 as one call, with their results bit for bit (a row's sums in the same order).
  * work_dev: work_bytes >= dg_linear_mx4_work_bytes(N, K) (else DG_ERR_BUFFER), 16-byte aligned; its contents are the library's.
  */
 size_t dg_linear_mx4_work_bytes(int64_t N, int64_t K);

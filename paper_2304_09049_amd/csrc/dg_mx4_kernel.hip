@@ -302,8 +302,10 @@ void launch_few(const DgGemmMx4 &p, const X *x, int32_t K, hipStream_t stream)
     gemm_mx4_few_kernel<T, X, WAVES, ROWS, EIGHTS><<<dim3((p.M + 16 * ROWS - 1) / (16 * ROWS), (p.N + 8 * EIGHTS - 1) / (8 * EIGHTS)), 64 * WAVES, 0, stream>>>(p, x, K);
 }
 
-// Whether 16 channels a workgroup are more than two workgroups a compute unit: then 32, by half as many wavefronts (one token, 16384 x 4096 9.7 us for 11.4; 4096 x 14336 11.8 for 9.1).
-bool many_channels(const DgGemmMx4 &p) { return p.M >= 8 * dg_simd_count(); }
+// A single token, quantised before or here: 16 channels a workgroup by four wavefronts, or 32 by two where that leaves more than one and a half workgroups of 16 a compute unit.  One rule for both, so that a token's sums
+// have one order whichever call makes them.  (us, 16 and 32, quantised here: 5120 x 4096 4.7 and 5.5, 6144 x 4096 5.4 and 5.6, 6144 x 8192 8.6 and 7.9, 7168 x 8192 9.5 and 8.4, 16384 x 4096 9.8 and 8.3; 4096 x 14336 8.4 and 11.5, 6144 x 14336
+// 10.8 and 11.6; quantised before: 5120 x 4096 4.5 and 4.8, 6144 x 4096 5.3 and 4.8, 6144 x 8192 8.1 and 7.3.  Tiles of 128 x 64 take 11.8 for 12.9 at 28672 x 4096, and 30 for 28 at 28672 x 8192.)
+bool many_channels(const DgGemmMx4 &p) { return p.M >= 6 * dg_simd_count(); }
 
 // ---- many tokens: tiles --------------------------------------------------------------------------------------------------
 //
@@ -795,7 +797,7 @@ void launch_stream(const DgGemmMx4 &p, hipStream_t stream)
 
 enum class Form { Few16x16, Few16x32, Few32x16, Few32x32, Tile32x64, Tile64x64, Tile128x64, Tile128x128, Tile256x128, Tile256x256 };
 
-// The form (channels x tokens a workgroup) whose rounds over the compute units cost least.  `cost`: of a round with a workgroup on each; `both`: with two, where two fit.
+// The form (channels x tokens a workgroup) whose rounds over the compute units cost least (a single token's: many_channels).  `cost`: of a round with a workgroup on each; `both`: with two, where two fit.
 // A round by form, us for K = 2048 and 8192, launch included: 16x16 3.6 (two 4.3), 5.3 (7.4); 16x32 4.2, 6.0; 32x16 4.2 (4.8), 6.9 (7.8); 32x32 4.9 (5.9), 8.3 (10.1); 32x64 5.7, 9.3 (13, where the weights come from
 // memory); 64x64 6.0, 11 (16); 128x64 7.5, 16 (22); 128x128 10, 27; 256x128 16, 43; 256x256 20, 57.  Of 239 products drawn (2 to
 // 4096 tokens, weights from memory) this is within 3 % of the fastest form on 209; the farthest from it: 94 x 288 x 4112 tokens, positions, channels 1.19 times its time, 4 x 1216 x 18816 1.16, 498 x 384 x 784 1.15.
@@ -809,6 +811,7 @@ Form form_of(const DgGemmMx4 &p)
                  {Form::Tile32x64, 32, 64, 28, 0, "32x64"}, {Form::Tile64x64, 64, 64, 33, 0, "64x64"}, {Form::Tile128x64, 128, 64, 43, 0, "128x64"},
                  {Form::Tile128x128, 128, 128, 57, 0, "128x128"}, {Form::Tile256x128, 256, 128, 92, 0, "256x128"}, {Form::Tile256x256, 256, 256, 120, 0, "256x256"}};
     const char *forced = dg_override("DG_GEMM_MX4_TILE");
+    if (!forced && p.N == 1) return many_channels(p) ? Form::Few32x16 : Form::Few16x16;
     const int64_t units = dg_simd_count() / 4;
     Form best = Form::Few16x16;
     int64_t least = INT64_MAX;
