@@ -28,3 +28,21 @@ def test_one_buffer_for_all_batches(K, E):
         assert torch.equal(ids.cpu().long(), want.indices[:, :4])
         # a softmax over four: exponents of at most some 10, two exponentials, a sum of 4 and a quotient
         ref.assert_within(w, torch.softmax(want.values[:, :4].double(), 1), torch.full((T, 4), 64 * 2.0 ** -24, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("dtype,rdtype", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("T,K,E", [(4100, 200, 128), (4111, 1031, 130), (8200, 72, 64), (2060, 520, 256)])
+def test_tiles_of_32(T, K, E, dtype, rdtype):
+    """512 tiles and more, the last ones ragged."""
+    gen = torch.Generator(device=DEV).manual_seed(T + K)
+    x, R = operands(gen, T, K + 3, E, dtype, rdtype)
+    x, R = x[:, 1:K + 1], R[:, 3:]                                    # (rows that begin anywhere)
+    bias = 0.1 * torch.randn(E, generator=gen, device=DEV)
+    ids, w = dg.dg_route_tokens(x, R, 5, mode="sigmoid", bias=bias)
+    logits = (x.double() @ R.double().t()).float().cpu()
+    choice = torch.sigmoid(logits.double()) + bias.cpu().double()
+    want = torch.sort(choice, dim=1, descending=True, stable=True).indices[:, :5]
+    assert torch.equal(ids.cpu().long(), want)
+    chance = torch.sigmoid(logits.double()).gather(1, want)
+    # five sigmoids, each an exponential, a sum and a quotient, their sum and a quotient, all below 1
+    ref.assert_within(w, chance / chance.sum(1, keepdim=True), torch.full((T, 5), 32 * 2.0 ** -24, dtype=torch.float64))
