@@ -523,7 +523,7 @@ dg_status dg_linear_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W
  *     ids     the experts of the `top` largest choices, the largest first, among equals the lowest expert.  An expert whose choice is -infinity is not taken: where too few
  *             are left the row ends with ids -1 and weights 0
  *     weights (binary32), of the experts taken, times `factor`:   exp(l) / sum over the taken of exp(l);   exp(l) / sum over all of exp(l);
- *             sigmoid(l) / sum over the taken of sigmoid(l) (0 where that is 0)
+ *             sigmoid(l) / sum over the taken of sigmoid(l) (0 where that is 0 in binary64)
  * A token with a NaN among its l or choices gets the experts 0 ... top - 1 and weights NaN: whatever is computed from it shows it.
  * x_dev: [T][K] of x_type, rows stride_x elements apart; R_dev: [E][K] of r_type (x_type or DG_F32), stride_r.  ids_dev, weights_dev: contiguous [T][top].
  * work_dev: dg_route_tokens_work_bytes(T, E) bytes, 16-byte aligned; what it says never falls as T grows, so a buffer for the largest batch does for the others.  E <= 1024, top <= 64, K <= 2^24.

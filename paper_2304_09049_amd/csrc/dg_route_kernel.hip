@@ -252,9 +252,15 @@ __global__ __launch_bounds__(64 * WAVES) void route_choose_kernel(DgRoute p, int
     }
     float w = 0.0f;
     if (p.mode == DG_ROUTE_SIGMOID) {
-        if (mine >= 0) w = 1.0f / (1.0f + expf(-its));
-        const float sum = dg_over_wave(w, DgAdd());
-        w = sum > 0.0f ? w / sum : 0.0f;
+        if (__ballot(mine >= 0 && its < -80.0f)) {
+            // (exp(88.8) is past binary32; below -87 a sigmoid has fewer bits)
+            const double chance = mine >= 0 ? 1.0 / (1.0 + exp(-(double)its)) : 0.0, sum = sum_of_wave(chance);
+            w = sum > 0.0 ? (float)(chance / sum) : 0.0f;
+        } else {
+            if (mine >= 0) w = 1.0f / (1.0f + expf(-its));
+            const float sum = dg_over_wave(w, DgAdd());
+            w = sum > 0.0f ? w / sum : 0.0f;
+        }
     } else {
         float most = its, sum;
         if (p.mode == DG_ROUTE_SOFTMAX_ALL) {

@@ -46,3 +46,20 @@ def test_tiles_of_32(T, K, E, dtype, rdtype):
     chance = torch.sigmoid(logits.double()).gather(1, want)
     # five sigmoids, each an exponential, a sum and a quotient, their sum and a quotient, all below 1
     ref.assert_within(w, chance / chance.sum(1, keepdim=True), torch.full((T, 5), 32 * 2.0 ** -24, dtype=torch.float64))
+
+
+def test_sigmoids_that_binary32_does_not_hold():
+    """Of logits from -60 to -700 too the weights are the sigmoids' shares; of those whose sigmoids are 0 in 64 bits they are 0."""
+    low = torch.tensor([-60.0, -80.5, -87.0, -89.0, -95.0, -103.0, -104.0, -120.0, -300.0, -700.0])
+    R = torch.ones(7, 4)
+    R[1], R[2], R[5] = 1.015625, 0.984375, 2.0                        # (exact: what the logits are is known)
+    x = low[:, None].expand(-1, 4) / 4
+    for scale in (1.0, 2.5):
+        ids, w = dg.dg_route_tokens(x.to(DEV).contiguous(), R.to(DEV), 3, mode="sigmoid", factor=scale)
+        want_ids, want = ref.route(x, R, 3, "sigmoid", None, scale)
+        assert torch.equal(ids.cpu(), want_ids)
+        # three sigmoids in binary32 (an exponential each: a few units), a sum, a quotient and a product
+        ref.assert_within(w, want, 32 * 2.0 ** -24 * want)
+        assert ((w.sum(1) - scale).abs() <= scale * 8 * 2.0 ** -24).all()
+    ids, w = dg.dg_route_tokens(torch.full((2, 4), -300.0, device=DEV), torch.ones(3, 4, device=DEV), 2, mode="sigmoid")
+    assert ids.tolist() == [[0, 1]] * 2 and (w == 0).all()            # exp(-1200)
