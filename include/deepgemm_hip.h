@@ -488,7 +488,7 @@ dg_status dg_paged_attention(const dg_cache_desc *desc, const void *cache_dev, s
 /*
  * x_dev ([N][K] of `type`, rows stride_n elements apart) -> codes_dev (rows stride_codes bytes apart) and scales_dev (stride_scales).  Bytes behind a row's are not
  * written.  1 <= K <= 2^24.
- * Errors: DG_ERR_NULL; DG_ERR_SHAPE (N < 0, K <= 0, a stride below its row); DG_ERR_RANGE (K, N * K beyond 2^58); DG_ERR_UNSUPPORTED (type); DG_ERR_BUFFER.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (N < 0 or beyond 2^31 - 1, K <= 0, a stride below its row); DG_ERR_RANGE (K, a stride of codes or scales); DG_ERR_UNSUPPORTED (type); DG_ERR_BUFFER.
  */
 dg_status dg_quantize_mx4(const void *x_dev, dg_dtype type, int64_t N, int64_t K, int64_t stride_n, uint8_t *codes_dev, int64_t stride_codes,
                           uint8_t *scales_dev, int64_t stride_scales, void *hip_stream);
@@ -502,7 +502,8 @@ dg_status dg_dequantize_mx4(const uint8_t *codes_dev, int64_t stride_codes, cons
  * Products are exact; sums are binary32 (within one instruction's 64 or 128 products what lies 2^28 below the largest may be left off), the bias (binary32, may be NULL)
  * is added and the result rounded once.  A block of scale 255 makes its row's results NaN.  out_dev: [N][M] of out_type, rows stride_out elements apart.
  * The order of the sums goes by the sizes and alignment, so a call gives the same bits each time.
- * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, a stride below its row); DG_ERR_RANGE (K beyond 2^24; M * N of 2^43 and more); DG_ERR_UNSUPPORTED; DG_ERR_BUFFER.
+ * Errors: DG_ERR_NULL; DG_ERR_SHAPE (M, K <= 0, N < 0, M or N beyond 2^31 - 1, a stride below its row); DG_ERR_RANGE (K beyond 2^24; a stride of codes or scales; M * N of 2^43 and more); DG_ERR_UNSUPPORTED;
+ * DG_ERR_BUFFER.
  */
 dg_status dg_gemm_mx4(const uint8_t *W_dev, int64_t stride_w, const uint8_t *W_scales_dev, int64_t stride_ws, const uint8_t *A_dev, int64_t stride_a,
                       const uint8_t *A_scales_dev, int64_t stride_as, int64_t M, int64_t N, int64_t K, const float *bias_m_dev, void *out_dev,
