@@ -550,7 +550,8 @@ typedef struct {
  * The gated feed-forward of each token's experts e = ids[t][j], j < top:
  *     g = gate_e x[t],  u = other_e x[t],  h = g / (1 + exp(-g)) * u,      out[t] = sum_j weights[t][j] * (down_e h)
  * An id that is no expert is skipped (a token of which none is left gives 0); a token may name an expert twice.  x and out are binary16 or bfloat16 and enter exactly; sums are
- * binary32; h is kept to 2^-17 of itself (two bfloat16 numbers); results are rounded once.  Nothing of a token reaches another's results; in which
+ * binary32, weights are taken as binary32 holds them (elements of 2^128 and more, which dg_quantize_mx4 never writes and scale bytes 253 and 254 have, count as infinite);
+ * h is kept to 2^-17 of itself (two bfloat16 numbers); results are rounded once.  Nothing of a token reaches another's results; in which
  * order its sums are added goes by how many tokens a call has.  Only the weights of experts that are named are
  * read, once for 16 or 32 of an expert's tokens (for few tokens that reading is what a call costs): meant for tokens being decoded; more than a few hundred tokens are worked through in turns.
  * x_dev: [T][hidden], rows stride_x elements apart; ids_dev, weights_dev: contiguous [T][top]; out_dev rows stride_out apart.  out_dev must not overlap x_dev.
