@@ -36,7 +36,7 @@ def rule(tmp_path_factory):
 def test_a_form_and_the_buffer_that_it_writes(rule):
     """Parts leave four sums in binary64 for each token and expert, all others a logit: on a device of few units too, where tiles of 32 x 32 suffice as well."""
     calls = [(T, E, K, units) for E in (1, 2, 8, 16, 17, 60, 64, 128, 257, 1024) for K in (64, 1023, 1024, 4096) for units in (1, 16, 32, 48, 64, 128, 256, 304)
-             for T in (1, 2, 3, 16, 40, 63, 100, 161, 512, 768, 769, 1000, 2560, 3072, 3073, 8192, 100000)]
+             for T in (1, 2, 3, 16, 40, 63, 100, 161, 512, 768, 769, 1000, 2560, 2900, 3100, 8192, 100000)]
     forms = set()
     for (T, E, K, units), (form, size) in zip(calls, rule(calls)):
         assert size >= T * E * (32 if form == PARTS16 else 4), (T, E, K, units)
