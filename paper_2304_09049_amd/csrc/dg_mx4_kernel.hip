@@ -543,8 +543,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void gemm_mx4_tile_kernel(TileAr
 // all have read this stage, the next one's first operands are read and this place is loaded anew.
 // Such tiles leave room for one workgroup a compute unit, which would have nothing to multiply while a tile's results leave and the next one's first stages arrive: a workgroup takes tile
 // after tile, and its loads run on into the next tile's stages.
-// 8192 x 8192 x 8192 to bfloat16 274 to 289 us (3.8 to 4.0 POP/s; results kept in the caches 311): the matrix pipe is busy half of the cycles at a clock that falls to 1.87 GHz; its products alone took 206 to 235,
-// the loads alone 137 to 195.
+// 8192 x 8192 x 8192 to bfloat16 274 to 289 us (3.8 to 4.0 POP/s; results kept in the caches 311): the matrix pipe is busy for 143 us of it, at a clock that falls to 1.84 GHz, and a third of the wavefronts' cycles are waits: two places,
+// and all loads waited for at each stage.  Without the loads the loop took 206 to 235, the loads alone 137 to 195.
 
 template <int N>
 using Int = std::integral_constant<int, N>;
